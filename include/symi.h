@@ -12,6 +12,9 @@
  *              symi_expert_bwd_slots + symi_replica_allreduce instead of symi_expert_bwd;
  *              symi_expert_bwd_active + symi_adam_to_replicas_active instead of the plain
  *              pair when many classes get no tokens;
+ *              the ends of the step around the MoE layers: symi_embed_fwd / symi_embed_bwd,
+ *              symi_policy_loss / symi_token_logp, symi_adamw_step for every tensor that
+ *              is no expert's;
  *              host helpers for the multi-rank plan at the end of this file
  *
  * Conventions
@@ -79,7 +82,7 @@ int symi_validate(const symi_cfg* cfg);
  * validated configuration of one MoE layer and optimizer partition (cfg->shard) together with
  * what the library needs to run it on the CURRENT device (queried once: compute units; created
  * once: the helper stream and events of the expert backward, only when the shape makes the two
- * gradient chains worth two streams).  Host function; the only one that creates anything.
+ * gradient chains worth two streams).  Host function; with symi_adamw_create the only one that creates anything.
  *   flags: 0 or an OR of
  *     SYMI_CTX_NO_OVERLAP  every kernel of symi_expert_bwd* stays on the caller's stream
  *                          (default: the weight-gradient chain runs on the helper stream,
@@ -291,6 +294,107 @@ int symi_expert_bwd_slots(const symi_ctx* ctx, const void* dYp, const void* Xp, 
  * class's slots.  In place on dW1_slot [S_tot,2f,d], dW2_slot [S_tot,d,f] f32.          */
 int symi_replica_allreduce(const symi_ctx* ctx, const int32_t* first_slot, float scale,
                            float* dW1_slot, float* dW2_slot, void* stream);
+
+/* ---- the ends of a training step around the MoE layers: what turns tokens into X, what turns the
+ * model's logits into a loss and their gradient, and the optimizer step of every tensor that is no
+ * expert's (the gate network's Wr and b among them).  T, d and dtype are those of the context.
+ * Rows and buffers may start at any element: no alignment beyond the type's own is needed. */
+
+/* Token embedding: X[t] = scale * table[tokens[t]], rounded once; a token outside [0, V) is padding
+ * and gives a row of zeros.   tokens [T] i32, table [V,d] in the activation dtype, X [T,d] out.
+ * 1 <= V <= 2^31 - 1. */
+int symi_embed_fwd(const symi_ctx* ctx, const int32_t* tokens, const void* table, int V, float scale,
+                   void* X, void* stream);
+
+/* Its gradient: dTable[v] = scale * (sum over the tokens t that are v of dX[t]), the sum in fp32 in
+ * an order that only the tokens decide (same bits on every run).   dX [T,d] in the activation
+ * dtype, dTable [V,d] f32.
+ *   accumulate = 0: every row is written, rows without tokens with zeros;
+ *   accumulate = 1: the sums are added to dTable, rows without tokens are not touched (weights tied
+ *                   to the output product, micro-batches).
+ *   ws: symi_embed_workspace_bytes(cfg, V) bytes of scratch, under the rules of symi_workspace_bytes
+ *   (0 if cfg or V is invalid). */
+size_t symi_embed_workspace_bytes(const symi_cfg* cfg, int V);
+int symi_embed_bwd(const symi_ctx* ctx, const int32_t* tokens, const void* dX, int V, float scale,
+                   int accumulate, float* dTable, void* ws, void* stream);
+
+/* Clipped policy loss with a KL term, from the logits of the T tokens of a batch.  For a token with
+ * logits z_j / temperature, chosen token a, advantage A and weight w:
+ *   logp  = log softmax(z / temperature)[a],  r = exp(logp - logp_old)
+ *   pg    = -min(r A, min(max(r, 1 - clip_low), 1 + clip_high) A)
+ *   kl    = exp(logp_ref - logp) - (logp_ref - logp) - 1
+ *   loss  = sum over tokens of w (pg + kl_coef kl)
+ * The caller's weights carry mask and mean: 0 for prompts and padding, 1 / count for a mean. */
+typedef struct symi_policy {
+  float clip_low, clip_high;  /* >= 0, clip_low <= 1 */
+  float kl_coef;              /* >= 0; 0 without logp_ref */
+  float inv_temperature;      /* 1 / temperature, > 0 */
+  float grad_scale;           /* dlogits is multiplied by it (1: the gradient of loss) */
+  int logits_dtype;           /* SYMI_F32 or SYMI_BF16, whatever the activations are */
+} symi_policy;
+
+/* logp [T] f32 out, on its own (what logp_old and logp_ref are made with).
+ *   logits [T,ld] in hp->logits_dtype, of which the first V columns are the vocabulary (V <= ld);
+ *   action [T] i32; weight [T] f32 or NULL.  A token whose weight is 0 or whose action is outside
+ *   [0, V) does not count: its logits are not read, its logp is 0. */
+int symi_token_logp(const symi_ctx* ctx, const symi_policy* hp, const void* logits, int V, int ld,
+                    const int32_t* action, const float* weight, float* logp, void* stream);
+
+/* The loss, and with dlogits its gradient in the same pass: a token's gradient needs no other
+ * token's, so its logits are read once.
+ *   logp_old, advantage, weight [T] f32; logp_ref [T] f32 or NULL (then kl is 0, kl_coef has to be 0).
+ *   logp [T] f32 out as above;  stats [4] f32 out: loss, sum of w pg, sum of w kl, sum of w over the
+ *   tokens whose ratio was clipped (their pg has no gradient).
+ *   dlogits [T,ld] out in hp->logits_dtype, or NULL: the loss alone.  Rows of tokens that do not
+ *   count and the columns from V on are zeros.  May be logits itself.
+ *   ws: symi_policy_workspace_bytes(cfg) bytes of scratch (0 if cfg is invalid). */
+size_t symi_policy_workspace_bytes(const symi_cfg* cfg);
+int symi_policy_loss(const symi_ctx* ctx, const symi_policy* hp, const void* logits, int V, int ld,
+                     const int32_t* action, const float* logp_old, const float* logp_ref,
+                     const float* advantage, const float* weight, float* logp, float* stats,
+                     void* dlogits, void* ws, void* stream);
+
+/* AdamW over many tensors in one launch.  Per element, with g = hp->grad_scale * grad_scale[0] * grad:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   w -= lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + hp->weight_decay decay w)
+ * as symi_adam_to_replicas, and eps > 0.
+ *
+ * state_bits 32: m, v [n] f32.
+ * state_bits 8:  every 256 elements of a tensor (the last ones of it: what is left) share two scales,
+ *   m[i] = m_scale[i / 256] sign(c) (c / 127)^2,  c = the int8 in m, -127..127
+ *   v[i] = v_scale[i / 256] (c / 255)^4,          c = the uint8 in v; 0 only where v is 0
+ *   and a new value becomes one of its two neighbouring codes at random, the nearer one more often, so
+ *   that the mean of what is stored is the value: rounding to the nearest code would lose every
+ *   change of less than half a step, and v decays by 1 - beta2 a step.  The 16 random bits of each are
+ *   a hash of seed, hp->step and the element's place; the weight's update uses the values before
+ *   rounding.  A block whose largest |value| is below 2^-126 is stored as zeros, one with a value that is not finite
+ *   with the scale NaN (all of it reads as NaN).  Zeroed codes and scales are a fresh state.
+ * The tensors' description is copied to the device by symi_adamw_create (host function, allocates
+ * and waits); the memory it points to stays the caller's and has to stay in place until
+ * symi_adamw_destroy.  No two tensors may overlap. */
+typedef struct symi_adamw_tensor {
+  void* param;         /* [n] in param_dtype, in/out */
+  float* master;       /* [n] f32 in/out when param is bf16 (param = master rounded), else NULL */
+  const void* grad;    /* [n] in grad_dtype */
+  void* m;             /* [n] f32, or int8 codes */
+  void* v;             /* [n] f32, or uint8 codes */
+  float* m_scale;      /* [ceil(n / 256)] f32 when state_bits is 8, else NULL */
+  float* v_scale;
+  long long n;         /* >= 0 */
+  float decay;         /* factor on hp->weight_decay: 0 for biases and norms */
+  int param_dtype, grad_dtype;   /* SYMI_F32 or SYMI_BF16 */
+  int state_bits;      /* 32 or 8 */
+} symi_adamw_tensor;
+typedef struct symi_adamw symi_adamw;
+int symi_adamw_create(const symi_adamw_tensor* tensors, int count, symi_adamw** out);
+int symi_adamw_destroy(symi_adamw* opt);   /* NULL: no-op; the caller synchronises first */
+/* One step.  grad_scale [1] f32 on the device (a clip factor, a loss scale) or NULL for 1. */
+int symi_adamw_step(const symi_ctx* ctx, const symi_adamw* opt, const symi_adam* hp,
+                    const float* grad_scale, uint32_t seed, void* stream);
+/* The states of all tensors as the values they stand for: m, v [symi_adamw_values(opt)] f32 out, tensor i
+ * from element 256 * (sum of ceil(n_j / 256) over j < i) on; what lies between is not written. */
+long long symi_adamw_values(const symi_adamw* opt);
+int symi_adamw_decode(const symi_ctx* ctx, const symi_adamw* opt, float* m, float* v, void* stream);
 
 /* ---- host helpers for the multi-rank part of the method (no GPU work; all pointers HOST).
  * Slot q of a placement lives on rank q / s, s = S_tot / N (S_tot must divide by N). */

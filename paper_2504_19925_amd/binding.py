@@ -32,6 +32,9 @@ EXPORTS = [
     "symi_replica_allreduce", "symi_router_fwd", "symi_router_bwd",
     "symi_grad_source", "symi_collect_grads", "symi_rank_group", "symi_comm_cost",
     "symi_timing_reset", "symi_timing_read", "symi_kernel_count", "symi_kernel_name",
+    "symi_embed_fwd", "symi_embed_workspace_bytes", "symi_embed_bwd", "symi_token_logp",
+    "symi_policy_workspace_bytes", "symi_policy_loss", "symi_adamw_create", "symi_adamw_destroy",
+    "symi_adamw_step", "symi_adamw_values", "symi_adamw_decode",
 ]
 
 
@@ -97,6 +100,40 @@ class SymiAdam(ctypes.Structure):
                 ("grad_scale", ctypes.c_float), ("step", ctypes.c_int)]
 
 
+class SymiPolicy(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_float) for n in
+                ("clip_low", "clip_high", "kl_coef", "inv_temperature", "grad_scale")] + [("logits_dtype", ctypes.c_int)]
+
+    @classmethod
+    def make(cls, clip_low=0.2, clip_high=0.2, kl_coef=0.0, temperature=1.0, grad_scale=1.0, dtype="bf16"):
+        return cls(clip_low, clip_high, kl_coef, 1.0 / temperature, grad_scale, {"f32": 0, "bf16": 1}[dtype])
+
+    @property
+    def torch_dtype(self):
+        return torch.bfloat16 if self.logits_dtype == 1 else torch.float32
+
+
+class SymiAdamWTensor(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("param", "master", "grad", "m", "v", "m_scale", "v_scale")] +
+                [("n", ctypes.c_longlong), ("decay", ctypes.c_float), ("param_dtype", ctypes.c_int),
+                 ("grad_dtype", ctypes.c_int), ("state_bits", ctypes.c_int)])
+
+
+class SymiAdamW:
+    """Handle of a symi_adamw (symi_adamw_create); holds the tensors whose memory it describes."""
+
+    def __init__(self, ptr, tensors, device):
+        self.ptr, self.tensors, self.device = ptr, tensors, device
+
+    def __del__(self):
+        try:
+            if self.ptr:
+                torch.cuda.synchronize(self.device)   # a step in flight reads the description
+                symi_adamw_destroy(self)
+        except Exception:
+            pass
+
+
 def lib_path():
     """The in-tree library; SYMI_LIB names another build of it (A/B measurements)."""
     return os.environ.get("SYMI_LIB") or os.path.join(_HERE, "libsymi.so")
@@ -148,6 +185,17 @@ def lib():
             "symi_timing_read": ([ctx, ci, ctypes.POINTER(cd), ctypes.POINTER(ci)], ci),
             "symi_kernel_count": ([], ci),
             "symi_kernel_name": ([ci], ctypes.c_char_p),
+            "symi_embed_fwd": ([ctx, ip, vp, ci, cf, vp, vp], ci),
+            "symi_embed_workspace_bytes": ([cfgp, ci], ctypes.c_size_t),
+            "symi_embed_bwd": ([ctx, ip, vp, ci, cf, ci, fp, vp, vp], ci),
+            "symi_token_logp": ([ctx, ctypes.POINTER(SymiPolicy), vp, ci, ci, ip, fp, fp, vp], ci),
+            "symi_policy_workspace_bytes": ([cfgp], ctypes.c_size_t),
+            "symi_policy_loss": ([ctx, ctypes.POINTER(SymiPolicy), vp, ci, ci, ip, fp, fp, fp, fp, fp, fp, vp, vp, vp], ci),
+            "symi_adamw_create": ([ctypes.POINTER(SymiAdamWTensor), ci, ctypes.POINTER(ctypes.c_void_p)], ci),
+            "symi_adamw_destroy": ([vp], ci),
+            "symi_adamw_step": ([ctx, vp, ctypes.POINTER(SymiAdam), fp, ctypes.c_uint32, vp], ci),
+            "symi_adamw_values": ([vp], ctypes.c_longlong),
+            "symi_adamw_decode": ([ctx, vp, fp, fp, vp], ci),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -173,7 +221,8 @@ def _load_marshal(L):
     except ImportError as e:   # built for another Python or torch
         warnings.warn(f"{path} cannot be loaded, device calls go through ctypes: {e}")
         return {}
-    mod.attach({n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in EXPORTS}, SymiCtx, SymiAdam)
+    mod.attach({n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in EXPORTS}, SymiCtx, SymiAdam,
+               SymiPolicy, SymiAdamW)
     return {n: getattr(mod, n) for n in EXPORTS if hasattr(mod, n)}
 
 
@@ -534,3 +583,109 @@ def symi_adam_to_replicas_active(ctx, hp, dW1_class, dW2_class, master_w, m, v, 
         _dev(first_slot_next, I32, "first_slot_next", ctx.E + 1),
         _dev(W1_slots, dt, "W1_slots", 2 * nw), _dev(W2_slots, dt, "W2_slots", nw), _stream()),
         "symi_adam_to_replicas_active")
+
+
+def symi_embed_workspace_bytes(cfg, V):
+    return lib().symi_embed_workspace_bytes(ctypes.byref(_cfg_of(cfg)), int(V))
+
+
+def symi_policy_workspace_bytes(cfg):
+    return lib().symi_policy_workspace_bytes(ctypes.byref(_cfg_of(cfg)))
+
+
+@_device_call
+def symi_embed_fwd(ctx, tokens, table, V, scale, X):
+    dt = ctx.torch_dtype
+    _check(lib().symi_embed_fwd(ctx.ptr, _dev(tokens, I32, "tokens", ctx.T), _dev(table, dt, "table", int(V) * ctx.d),
+                                int(V), float(scale), _dev(X, dt, "X", ctx.T * ctx.d), _stream()), "symi_embed_fwd")
+
+
+@_device_call
+def symi_embed_bwd(ctx, tokens, dX, V, scale, accumulate, dTable, ws):
+    _check(lib().symi_embed_bwd(
+        ctx.ptr, _dev(tokens, I32, "tokens", ctx.T), _dev(dX, ctx.torch_dtype, "dX", ctx.T * ctx.d), int(V), float(scale),
+        int(accumulate), _dev(dTable, F32, "dTable", int(V) * ctx.d),
+        _dev(ws, torch.uint8, "ws", symi_embed_workspace_bytes(ctx.cfg, V)), _stream()), "symi_embed_bwd")
+
+
+def _rows(t, hp, name, ctx, ld):
+    return _dev(t, hp.torch_dtype, name, ctx.T * int(ld))
+
+
+@_device_call
+def symi_token_logp(ctx, hp, logits, V, ld, action, weight, logp):
+    _check(lib().symi_token_logp(
+        ctx.ptr, ctypes.byref(hp), _rows(logits, hp, "logits", ctx, ld), int(V), int(ld), _dev(action, I32, "action", ctx.T),
+        None if weight is None else _dev(weight, F32, "weight", ctx.T), _dev(logp, F32, "logp", ctx.T), _stream()),
+        "symi_token_logp")
+
+
+@_device_call
+def symi_policy_loss(ctx, hp, logits, V, ld, action, logp_old, logp_ref, advantage, weight, logp, stats, dlogits, ws):
+    _check(lib().symi_policy_loss(
+        ctx.ptr, ctypes.byref(hp), _rows(logits, hp, "logits", ctx, ld), int(V), int(ld), _dev(action, I32, "action", ctx.T),
+        _dev(logp_old, F32, "logp_old", ctx.T), None if logp_ref is None else _dev(logp_ref, F32, "logp_ref", ctx.T),
+        _dev(advantage, F32, "advantage", ctx.T), _dev(weight, F32, "weight", ctx.T), _dev(logp, F32, "logp", ctx.T),
+        _dev(stats, F32, "stats", 4), None if dlogits is None else _rows(dlogits, hp, "dlogits", ctx, ld),
+        _dev(ws, torch.uint8, "ws", symi_policy_workspace_bytes(ctx.cfg)), _stream()), "symi_policy_loss")
+
+
+def _adamw_tensor(i, t):
+    """One entry of symi_adamw_create's list: a dict with the tensors param, grad, m, v, for a bf16 param its master, for
+    8-bit states (m int8, v uint8) m_scale and v_scale, and the factor decay (1)."""
+    unknown = set(t) - {"param", "master", "grad", "m", "v", "m_scale", "v_scale", "decay"}
+    if unknown:
+        raise SymiError(f"tensor {i}: unknown entries {sorted(unknown)}")
+    for name in ("param", "grad", "m", "v"):
+        if not isinstance(t.get(name), torch.Tensor):
+            raise SymiError(f"tensor {i}: {name}: expected a torch tensor")
+    n, name = t["param"].numel(), f"tensor {i}: "
+    kinds = {torch.float32: 0, torch.bfloat16: 1}
+    for what in ("param", "grad"):
+        if t[what].dtype not in kinds:
+            raise SymiError(f"{name}{what}: expected dtype torch.float32 or torch.bfloat16, got {t[what].dtype}")
+    codes = t["m"].dtype == torch.int8
+    if t["grad"].numel() != n:
+        raise SymiError(f"{name}grad: has {t['grad'].numel()} elements, param {n}")
+
+    def at(what, dtype, numel):
+        x = t.get(what)
+        return None if x is None else _dev(x, dtype, name + what, numel).value
+
+    return SymiAdamWTensor(
+        at("param", t["param"].dtype, n), at("master", F32, n), at("grad", t["grad"].dtype, n),
+        at("m", torch.int8 if codes else F32, n), at("v", torch.uint8 if codes else F32, n), at("m_scale", F32, -(-n // 256)),
+        at("v_scale", F32, -(-n // 256)), n, float(t.get("decay", 1.0)), kinds[t["param"].dtype], kinds[t["grad"].dtype],
+        8 if codes else 32)
+
+
+def symi_adamw_create(tensors):
+    tensors = [dict(t) for t in tensors]
+    entries = (SymiAdamWTensor * max(1, len(tensors)))(*[_adamw_tensor(i, t) for i, t in enumerate(tensors)])
+    out = ctypes.c_void_p()
+    _check(lib().symi_adamw_create(entries, len(tensors), ctypes.byref(out)), "symi_adamw_create")
+    return SymiAdamW(out, tensors, torch.cuda.current_device())
+
+
+def symi_adamw_destroy(opt):
+    ptr, opt.ptr = opt.ptr, None
+    if ptr:
+        _check(lib().symi_adamw_destroy(ptr), "symi_adamw_destroy")
+
+
+def symi_adamw_values(opt):
+    return lib().symi_adamw_values(opt.ptr)
+
+
+@_device_call
+def symi_adamw_step(ctx, opt, hp, grad_scale, seed):
+    _check(lib().symi_adamw_step(ctx.ptr, opt.ptr, ctypes.byref(hp),
+                                 None if grad_scale is None else _dev(grad_scale, F32, "grad_scale", 1),
+                                 int(seed) & 0xffffffff, _stream()), "symi_adamw_step")
+
+
+@_device_call
+def symi_adamw_decode(ctx, opt, m, v):
+    n = symi_adamw_values(opt)
+    _check(lib().symi_adamw_decode(ctx.ptr, opt.ptr, _dev(m, F32, "m", n), _dev(v, F32, "v", n), _stream()),
+           "symi_adamw_decode")

@@ -12,7 +12,8 @@ LIB = os.path.join(HERE, "libsymi.so")
 CEILINGS_LIB = os.path.join(HERE, "libsymi_ceilings.so")
 # the binding's argument marshalling (host code against torch's headers)
 MARSHAL_LIB = os.path.join(HERE, "_marshal.so")
-SOURCES = ["api.hip", "route.hip", "place.hip", "dispatch.hip", "gemm.hip", "adam.hip", "comm_plan.hip", "router.hip"]
+SOURCES = ["api.hip", "route.hip", "place.hip", "dispatch.hip", "gemm.hip", "adam.hip", "comm_plan.hip", "router.hip",
+           "embed.hip", "policy.hip", "adamw.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]

@@ -25,7 +25,10 @@ namespace {
   X(symi_dispatch_capacity) X(symi_dispatch_bwd) X(symi_expert_fwd) X(symi_expert_bwd)         \
   X(symi_expert_bwd_slots) X(symi_expert_bwd_active) X(symi_replica_allreduce)                 \
   X(symi_router_fwd) X(symi_router_bwd) X(symi_combine) X(symi_combine_bwd)                    \
-  X(symi_adam_to_replicas) X(symi_adam_to_replicas_active) X(symi_workspace_bytes)
+  X(symi_adam_to_replicas) X(symi_adam_to_replicas_active) X(symi_workspace_bytes)             \
+  X(symi_embed_fwd) X(symi_embed_bwd) X(symi_embed_workspace_bytes) X(symi_token_logp)         \
+  X(symi_policy_loss) X(symi_policy_workspace_bytes) X(symi_adamw_step) X(symi_adamw_values)   \
+  X(symi_adamw_decode)
 
 // entry points of the loaded libsymi.so (addresses handed over by attach)
 struct Entries {
@@ -35,15 +38,19 @@ struct Entries {
 } g;
 PyTypeObject* g_ctx_type = nullptr;    // binding.SymiCtx
 PyTypeObject* g_adam_type = nullptr;   // binding.SymiAdam
+PyTypeObject* g_policy_type = nullptr; // binding.SymiPolicy
+PyTypeObject* g_adamw_type = nullptr;  // binding.SymiAdamW
 PyObject *g_ptr = nullptr, *g_cfg = nullptr;   // interned attribute names
 
 // one argument of a C call: converts to the type of the parameter it is passed for
 struct Val {
   void* p = nullptr;
   int i = 0;
+  uint32_t u = 0;
   float f = 0.f;
   template <class T> operator T*() const { return static_cast<T*>(p); }
   operator int() const { return i; }
+  operator uint32_t() const { return u; }
   operator float() const { return f; }
 };
 
@@ -108,6 +115,31 @@ class Call {
     v.p = &hp_;
     return v;
   }
+  Val word(int i) {
+    Val v;
+    if (!PyLong_CheckExact(a_[i])) { ok = false; return v; }
+    v.u = (uint32_t)PyLong_AsUnsignedLongMask(a_[i]);
+    return v;
+  }
+  Val policy(int i) {
+    Val v;
+    if (Py_TYPE(a_[i]) != g_policy_type || !read_ctypes(a_[i], pp_)) { ok = false; return v; }
+    v.p = &pp_;
+    return v;
+  }
+  // rows of logits, after policy()
+  Val logits(int i, long long ld) { return tensor(i, pp_.logits_dtype == SYMI_BF16 ? at::kBFloat16 : at::kFloat, T * ld); }
+  Val logits_or_none(int i, long long ld) { return a_[i] == Py_None ? Val() : logits(i, ld); }
+  Val bytes(int i, size_t n) { return tensor(i, at::kByte, (long long)n); }
+  Val adamw(int i) {
+    Val v;
+    if (Py_TYPE(a_[i]) != g_adamw_type) { ok = false; return v; }
+    PyObject* p = PyObject_GetAttr(a_[i], g_ptr);
+    ok = ok && p && p != Py_None && read_ctypes(p, v.p) && v.p;
+    Py_XDECREF(p);
+    if (!ok) PyErr_Clear();
+    return v;
+  }
   template <class Fn, size_t N>
   PyObject* operator()(Fn fn, const Val (&v)[N]) {
     if (!ok || !fn) Py_RETURN_NONE;
@@ -146,6 +178,7 @@ class Call {
   PyObject* const* a_;
   symi_ctx* ctx_ = nullptr;
   symi_adam hp_;
+  symi_policy pp_;
 };
 
 #define DEF(name) PyObject* py_##name(PyObject*, PyObject* const* a, Py_ssize_t n)
@@ -266,10 +299,59 @@ DEF(symi_adam_to_replicas_active) {
   return c(g.symi_adam_to_replicas_active, v);
 }
 
-// attach({name: address}, SymiCtx, SymiAdam)
+DEF(symi_embed_fwd) {
+  Call c(a, n, 6);
+  if (!c.ok) Py_RETURN_NONE;
+  const Val V = c.integer(3);
+  const Val v[] = {c.i32(1, c.T), c.act(2, V.i * c.d), V, c.real(4), c.act(5, c.T * c.d)};
+  return c(g.symi_embed_fwd, v);
+}
+DEF(symi_embed_bwd) {
+  Call c(a, n, 8);
+  if (!c.ok) Py_RETURN_NONE;
+  const Val V = c.integer(3);
+  if (!c.ok) Py_RETURN_NONE;
+  const Val v[] = {c.i32(1, c.T), c.act(2, c.T * c.d), V, c.real(4), c.integer(5), c.f32(6, V.i * c.d),
+                   c.bytes(7, g.symi_embed_workspace_bytes(&c.c, V.i))};
+  return c(g.symi_embed_bwd, v);
+}
+DEF(symi_token_logp) {
+  Call c(a, n, 8);
+  if (!c.ok) Py_RETURN_NONE;
+  const Val hp = c.policy(1), V = c.integer(3), ld = c.integer(4);
+  const Val v[] = {hp, c.logits(2, ld.i), V, ld, c.i32(5, c.T), c.f32_or_none(6, c.T), c.f32(7, c.T)};
+  return c(g.symi_token_logp, v);
+}
+DEF(symi_policy_loss) {
+  Call c(a, n, 14);
+  if (!c.ok) Py_RETURN_NONE;
+  const Val hp = c.policy(1), V = c.integer(3), ld = c.integer(4);
+  const Val v[] = {hp, c.logits(2, ld.i), V, ld, c.i32(5, c.T), c.f32(6, c.T), c.f32_or_none(7, c.T), c.f32(8, c.T),
+                   c.f32(9, c.T), c.f32(10, c.T), c.f32(11, 4), c.logits_or_none(12, ld.i),
+                   c.bytes(13, g.symi_policy_workspace_bytes(&c.c))};
+  return c(g.symi_policy_loss, v);
+}
+DEF(symi_adamw_step) {
+  Call c(a, n, 5);
+  if (!c.ok) Py_RETURN_NONE;
+  const Val v[] = {c.adamw(1), c.adam(2), c.f32_or_none(3, 1), c.word(4)};
+  return c(g.symi_adamw_step, v);
+}
+DEF(symi_adamw_decode) {
+  Call c(a, n, 4);
+  if (!c.ok) Py_RETURN_NONE;
+  const Val opt = c.adamw(1);
+  if (!c.ok) Py_RETURN_NONE;
+  const long long values = g.symi_adamw_values(opt);
+  const Val v[] = {opt, c.f32(2, values), c.f32(3, values)};
+  return c(g.symi_adamw_decode, v);
+}
+
+// attach({name: address}, SymiCtx, SymiAdam, SymiPolicy, SymiAdamW)
 PyObject* attach(PyObject*, PyObject* args) {
-  PyObject *addresses, *ctx_type, *adam_type;
-  if (!PyArg_ParseTuple(args, "O!O!O!", &PyDict_Type, &addresses, &PyType_Type, &ctx_type, &PyType_Type, &adam_type))
+  PyObject *addresses, *ctx_type, *adam_type, *policy_type, *adamw_type;
+  if (!PyArg_ParseTuple(args, "O!O!O!O!O!", &PyDict_Type, &addresses, &PyType_Type, &ctx_type, &PyType_Type, &adam_type,
+                        &PyType_Type, &policy_type, &PyType_Type, &adamw_type))
     return nullptr;
   Entries e;
 #define X(name)                                                                       \
@@ -286,6 +368,10 @@ PyObject* attach(PyObject*, PyObject* args) {
 #undef X
   Py_INCREF(ctx_type);
   Py_INCREF(adam_type);
+  Py_INCREF(policy_type);
+  Py_INCREF(adamw_type);
+  g_policy_type = reinterpret_cast<PyTypeObject*>(policy_type);
+  g_adamw_type = reinterpret_cast<PyTypeObject*>(adamw_type);
   g_ctx_type = reinterpret_cast<PyTypeObject*>(ctx_type);
   g_adam_type = reinterpret_cast<PyTypeObject*>(adam_type);
   g = e;
@@ -297,7 +383,8 @@ PyMethodDef methods[] = {
     M(symi_route) M(symi_route_bwd) M(symi_place) M(symi_dispatch) M(symi_dispatch_noalloc) M(symi_dispatch_capacity)
     M(symi_dispatch_bwd) M(symi_expert_fwd) M(symi_expert_bwd) M(symi_expert_bwd_slots) M(symi_expert_bwd_active)
     M(symi_replica_allreduce) M(symi_router_fwd) M(symi_router_bwd) M(symi_combine) M(symi_combine_bwd)
-    M(symi_adam_to_replicas) M(symi_adam_to_replicas_active)
+    M(symi_adam_to_replicas) M(symi_adam_to_replicas_active) M(symi_embed_fwd) M(symi_embed_bwd) M(symi_token_logp)
+    M(symi_policy_loss) M(symi_adamw_step) M(symi_adamw_decode)
     {"attach", attach, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};
