@@ -14,28 +14,81 @@
 
 namespace symi {
 
-constexpr int POLICY_THREADS = 256;
 constexpr int SUM_THREADS = 1024;
 
 struct PolicyScalars {
   float clip_low, clip_high, kl_coef, inv_temp, scale, c;   // c: log2(e) / temperature
 };
 
-template <bool BF16> struct Logit {
+// A 16-byte piece of a row as it lies in memory: 8 bf16 or 4 fp32 logits.
+template <bool BF16> struct Piece {
+  static constexpr int N = BF16 ? 8 : 4;
   using Elem = std::conditional_t<BF16, uint16_t, float>;
-  static __device__ __forceinline__ float get(Elem x) {
-    if constexpr (BF16) return bf16_to_f32(x); else return x;
+  using Vec = std::conditional_t<BF16, u32x4_bf16, f32x4_f32>;
+  typedef uint32_t Raw __attribute__((ext_vector_type(4)));
+  static __device__ __forceinline__ Raw load(const Elem* p) { return __builtin_bit_cast(Raw, *reinterpret_cast<const Vec*>(p)); }
+  static __device__ __forceinline__ void store(Elem* p, Raw r) { *reinterpret_cast<Vec*>(p) = __builtin_bit_cast(Vec, r); }
+  // the first n of its values, the others -inf
+  static __device__ __forceinline__ Raw load_some(const Elem* p, int n) {
+    uint32_t x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (BF16) {
+        const uint32_t lo = 2 * i < n ? p[2 * i] : 0xff80u, hi = 2 * i + 1 < n ? p[2 * i + 1] : 0xff80u;
+        x[i] = lo | hi << 16;
+      } else {
+        x[i] = __float_as_uint(i < n ? p[i] : -INFINITY);
+      }
+    }
+    return Raw{x[0], x[1], x[2], x[3]};
   }
-  static __device__ __forceinline__ Elem put(float x) {
-    if constexpr (BF16) return f32_to_bf16(x); else return x;
+  static __device__ __forceinline__ void store_some(Elem* p, Raw r, int n) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (BF16) {
+        if (2 * i < n) p[2 * i] = (uint16_t)r[i];
+        if (2 * i + 1 < n) p[2 * i + 1] = (uint16_t)(r[i] >> 16);
+      } else if (i < n) {
+        p[i] = __uint_as_float(r[i]);
+      }
+    }
+  }
+  static __device__ __forceinline__ void unpack(Raw r, float (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (BF16) {
+        x[2 * i] = __uint_as_float(r[i] << 16);
+        x[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+      } else {
+        x[i] = __uint_as_float(r[i]);
+      }
+    }
+  }
+  static __device__ __forceinline__ Raw pack(const float (&x)[N]) {
+    uint32_t y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (BF16) y[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]); else y[i] = __float_as_uint(x[i]);
+    }
+    return Raw{y[0], y[1], y[2], y[3]};
+  }
+  static __device__ __forceinline__ Raw none() {
+    const uint32_t x = BF16 ? 0xff80ff80u : 0xff800000u;
+    return Raw{x, x, x, x};
   }
 };
+
+// Makes the compiler unpack a piece again where it is used again, in place of keeping both forms in registers.
+template <class Raw>
+__device__ __forceinline__ void forget(Raw& r) { asm volatile("" : "+v"(r)); }
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }   // below 2^-126: 0
 
 // (m, s) of a set of t: m its largest value, s the sum of 2^(t - m).
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
   const float top = fmaxf(m, m2);
   const float ref = top == -INFINITY ? 0.f : top;   // nothing but -inf so far: 2^(-inf - 0) = 0
-  s = s * exp2f(m - ref) + s2 * exp2f(m2 - ref);
+  s = s * exp2_(m - ref) + s2 * exp2_(m2 - ref);
   m = top;
 }
 
@@ -60,50 +113,125 @@ __device__ __forceinline__ Token token_loss(const PolicyScalars& p, float logp, 
   return k;
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(POLICY_THREADS) void policy_kernel(
+// A workgroup of THREADS takes a row, every thread NV pieces of it at a time: whatever fits is read once and stays in
+// registers from the logits to their gradient.  Of a longer row the last part stays, the ones before it are read again.
+template <bool BF16, bool GRAD, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS) void policy_kernel(
     const void* logits, int V, int ld, const int32_t* __restrict__ action, const float* __restrict__ logp_old,
     const float* __restrict__ logp_ref, const float* __restrict__ advantage, const float* __restrict__ weight,
     float* __restrict__ logp, float4* __restrict__ terms, void* dlogits, PolicyScalars p) {
-  using L = Logit<BF16>;
-  __shared__ float ms[POLICY_THREADS / 64], ss[POLICY_THREADS / 64];
+  using P = Piece<BF16>;
+  constexpr int N = P::N, WAVES = THREADS / 64;
+  __shared__ float ms[WAVES], ss[WAVES], za_s;
+  const int tid = threadIdx.x;
   const long long t = blockIdx.x;
-  const auto* const z = static_cast<const typename L::Elem*>(logits) + t * ld;
-  auto* const dz = static_cast<typename L::Elem*>(dlogits) + (dlogits ? t * ld : 0);
+  const auto* const z = static_cast<const typename P::Elem*>(logits) + t * ld;
+  auto* const dz = static_cast<typename P::Elem*>(dlogits) + (GRAD ? t * ld : 0);
   const int a = action[t];
   const float w = weight ? weight[t] : 1.f;
+  const int whole = V / N;               // pieces that lie in the vocabulary
   if (w == 0.f || (unsigned)a >= (unsigned)V) {
-    if (threadIdx.x == 0) {
+    if (tid == 0) {
       logp[t] = 0.f;
       if (terms) terms[t] = float4{0.f, 0.f, 0.f, 0.f};
     }
-    if (dlogits)
-      for (int j = threadIdx.x; j < ld; j += POLICY_THREADS) dz[j] = L::put(0.f);
+    if (GRAD) {
+      const typename P::Raw zero = {0, 0, 0, 0};
+      for (int q = tid; q < ld / N; q += THREADS) P::store(dz + (long long)q * N, zero);
+      if (tid < ld % N) dz[ld / N * N + tid] = 0;
+    }
     return;
   }
-  const float za = L::get(z[a]);
+  float old = 0.f, ref = 0.f, A = 0.f;   // requested with the row
+  if (terms) {
+    old = logp_old[t];
+    A = advantage[t];
+    if (logp_ref) ref = logp_ref[t];
+  }
+  typename P::Raw r[NV];
+  const auto fetch = [&](int q0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int q = q0 + i * THREADS + tid;
+      r[i] = P::none();
+      if (q < whole) r[i] = P::load(z + (long long)q * N);
+      else if (q == whole) r[i] = P::load_some(z + (long long)q * N, V - whole * N);
+    }
+  };
   float m = -INFINITY, s = 0.f;
-  for (int j = threadIdx.x; j < V; j += POLICY_THREADS) join(m, s, L::get(z[j]) * p.c, 1.f);
+  constexpr int STEP = NV * THREADS;
+  const int last = whole / STEP * STEP;   // where the part that stays begins
+  for (int q0 = 0; q0 <= last; q0 += STEP) {
+    fetch(q0);
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (q0 + i * THREADS > whole) continue;
+      float x[N];
+      P::unpack(r[i], x);
+#pragma unroll
+      for (int j = 0; j < N; ++j) top = fmaxf(top, x[j]);
+      if (q0 + i * THREADS + tid == a / N) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (j == a % N) za_s = x[j];
+      }
+    }
+    top *= p.c;
+    const float base = fmaxf(m, top), from = base == -INFINITY ? 0.f : base;   // nothing but -inf so far
+    s *= exp2_(m - from);
+    m = base;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (q0 + i * THREADS > whole) continue;
+      float x[N];
+      forget(r[i]);
+      P::unpack(r[i], x);
+#pragma unroll
+      for (int j = 0; j < N; ++j) s += exp2_(fmaf(x[j], p.c, -from));
+    }
+  }
 #pragma unroll
   for (int k = 32; k >= 1; k >>= 1) join(m, s, __shfl_xor(m, k, 64), __shfl_xor(s, k, 64));
-  if ((threadIdx.x & 63) == 0) {
-    ms[threadIdx.x >> 6] = m;
-    ss[threadIdx.x >> 6] = s;
+  if ((tid & 63) == 0) {
+    ms[tid >> 6] = m;
+    ss[tid >> 6] = s;
   }
   __syncthreads();
   m = ms[0];
   s = ss[0];
 #pragma unroll
-  for (int k = 1; k < POLICY_THREADS / 64; ++k) join(m, s, ms[k], ss[k]);
-  const float lp = (za * p.c - m) * 0.693147180559945309f - logf(s);
-  if (threadIdx.x == 0) logp[t] = lp;
+  for (int k = 1; k < WAVES; ++k) join(m, s, ms[k], ss[k]);
+  const float lp = fmaf(za_s, p.c, -m) * 0.693147180559945309f - logf(s);
+  if (tid == 0) logp[t] = lp;
   if (!terms) return;
-  const Token k = token_loss(p, lp, logp_old[t], logp_ref != nullptr, logp_ref ? logp_ref[t] : 0.f, advantage[t]);
-  if (threadIdx.x == 0) terms[t] = float4{w * (k.gain + p.kl_coef * k.kl), w * k.gain, w * k.kl, k.clipped ? w : 0.f};
-  if (!dlogits) return;
-  const float u = p.scale * p.inv_temp * w * k.slope, inv_s = 1.f / s;
-  for (int j = threadIdx.x; j < ld; j += POLICY_THREADS)
-    dz[j] = L::put(j < V ? u * ((j == a ? 1.f : 0.f) - exp2f(L::get(z[j]) * p.c - m) * inv_s) : 0.f);
+  const Token k = token_loss(p, lp, old, logp_ref != nullptr, ref, A);
+  if (tid == 0) terms[t] = float4{w * (k.gain + p.kl_coef * k.kl), w * k.gain, w * k.kl, k.clipped ? w : 0.f};
+  if (!GRAD) return;
+  // 2^24 moves from the factor into the exponent, so that the power is no denormal number, which would become 0, where the
+  // gradient in single precision is one that is kept
+  const float u = p.scale * p.inv_temp * w * k.slope, minus = -u / s * 0x1p-24f, from = m - 24.f;
+  for (int q0 = last; q0 >= 0; q0 -= STEP) {
+    if (q0 < last) fetch(q0);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int q = q0 + i * THREADS + tid;
+      if (q0 + i * THREADS > whole) continue;
+      float x[N];
+      forget(r[i]);
+      P::unpack(r[i], x);
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = minus * exp2_(fmaf(x[j], p.c, -from));
+      if (q == a / N) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (j == a % N) x[j] += u;
+      }
+      if (q < whole) P::store(dz + (long long)q * N, P::pack(x));
+      else if (q == whole) P::store_some(dz + (long long)q * N, P::pack(x), V - whole * N);
+    }
+  }
+  for (int j = V + tid; j < ld; j += THREADS) dz[j] = 0;
 }
 
 __global__ __launch_bounds__(SUM_THREADS) void policy_sum_kernel(const float4* __restrict__ terms, int T, float* __restrict__ stats) {
@@ -145,10 +273,23 @@ static int policy_impl(const char* who, const symi_ctx* ctx, const symi_policy* 
   const PolicyScalars p = {hp->clip_low, hp->clip_high, hp->kl_coef, hp->inv_temperature, hp->grad_scale,
                            (float)(1.4426950408889634 * hp->inv_temperature)};
   const int T = ctx->cfg.T, kid = terms ? K_POLICY : K_TOKEN_LOGP;
-  if (hp->logits_dtype == SYMI_BF16)
-    SYMI_TIMED(ctx, kid, st, (policy_kernel<true><<<T, POLICY_THREADS, 0, st>>>(logits, V, ld, action, logp_old, logp_ref, advantage, weight, logp, terms, dlogits, p)));
-  else
-    SYMI_TIMED(ctx, kid, st, (policy_kernel<false><<<T, POLICY_THREADS, 0, st>>>(logits, V, ld, action, logp_old, logp_ref, advantage, weight, logp, terms, dlogits, p)));
+  const bool bf16 = hp->logits_dtype == SYMI_BF16;
+  const int pieces = V / (bf16 ? 8 : 4) + 1;
+#define ROWS(BF16, GRAD, THREADS, NV)                                                                                  \
+  SYMI_TIMED(ctx, kid, st, (policy_kernel<BF16, GRAD, THREADS, NV><<<T, THREADS, 0, st>>>(                             \
+      logits, V, ld, action, logp_old, logp_ref, advantage, weight, logp, terms, dlogits, p)))
+#define SIZES(BF16, GRAD)                                      \
+  if (pieces <= 64 * 4) ROWS(BF16, GRAD, 64, 4);               \
+  else if (pieces <= 256 * 4) ROWS(BF16, GRAD, 256, 4);        \
+  else if (pieces <= 512 * 8) ROWS(BF16, GRAD, 512, 8);        \
+  else if (pieces <= 1024 * 8) ROWS(BF16, GRAD, 1024, 8);      \
+  else ROWS(BF16, GRAD, 1024, 16)
+  if (bf16 && dlogits) { SIZES(true, true); }
+  else if (bf16) { SIZES(true, false); }
+  else if (dlogits) { SIZES(false, true); }
+  else { SIZES(false, false); }
+#undef SIZES
+#undef ROWS
   SYMI_LAUNCH_CHECK(who);
   return SYMI_OK;
 }
