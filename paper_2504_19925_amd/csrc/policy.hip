@@ -26,7 +26,11 @@ template <bool BF16> struct Piece {
   using Elem = std::conditional_t<BF16, uint16_t, float>;
   using Vec = std::conditional_t<BF16, u32x4_bf16, f32x4_f32>;
   typedef uint32_t Raw __attribute__((ext_vector_type(4)));
-  static __device__ __forceinline__ Raw load(const Elem* p) { return __builtin_bit_cast(Raw, *reinterpret_cast<const Vec*>(p)); }
+  template <bool ONCE>   // nobody reads it again
+  static __device__ __forceinline__ Raw load(const Elem* p) {
+    const Vec* const q = reinterpret_cast<const Vec*>(p);
+    return __builtin_bit_cast(Raw, ONCE ? __builtin_nontemporal_load(q) : *q);
+  }
   static __device__ __forceinline__ void store(Elem* p, Raw r) { *reinterpret_cast<Vec*>(p) = __builtin_bit_cast(Vec, r); }
   // the first n of its values, the others -inf
   static __device__ __forceinline__ Raw load_some(const Elem* p, int n) {
@@ -113,134 +117,228 @@ __device__ __forceinline__ Token token_loss(const PolicyScalars& p, float logp, 
   return k;
 }
 
-// A workgroup of THREADS takes a row, every thread NV pieces of it at a time: whatever fits is read once and stays in
-// registers from the logits to their gradient.  Of a longer row the last part stays, the ones before it are read again.
-template <bool BF16, bool GRAD, int THREADS, int NV>
-__global__ __launch_bounds__(THREADS) void policy_kernel(
-    const void* logits, int V, int ld, const int32_t* __restrict__ action, const float* __restrict__ logp_old,
-    const float* __restrict__ logp_ref, const float* __restrict__ advantage, const float* __restrict__ weight,
-    float* __restrict__ logp, float4* __restrict__ terms, void* dlogits, PolicyScalars p) {
+struct PolicyArgs {
+  const void* logits;
+  int V, ld;
+  const int32_t* action;
+  const float *logp_old, *logp_ref, *advantage, *weight;
+  float* logp;
+  float4* terms;
+  void* dlogits;
+  PolicyScalars p;
+};
+
+// What a workgroup does with a row of logits, every thread NV pieces of it at a time.
+template <bool BF16, bool ONCE, int THREADS, int NV>
+struct Row {
   using P = Piece<BF16>;
-  constexpr int N = P::N, WAVES = THREADS / 64;
-  __shared__ float ms[WAVES], ss[WAVES], za_s;
-  const int tid = threadIdx.x;
-  const long long t = blockIdx.x;
-  const auto* const z = static_cast<const typename P::Elem*>(logits) + t * ld;
-  auto* const dz = static_cast<typename P::Elem*>(dlogits) + (GRAD ? t * ld : 0);
-  const int a = action[t];
-  const float w = weight ? weight[t] : 1.f;
-  const int whole = V / N;               // pieces that lie in the vocabulary
-  if (w == 0.f || (unsigned)a >= (unsigned)V) {
-    if (tid == 0) {
-      logp[t] = 0.f;
-      if (terms) terms[t] = float4{0.f, 0.f, 0.f, 0.f};
-    }
-    if (GRAD) {
-      const typename P::Raw zero = {0, 0, 0, 0};
-      for (int q = tid; q < ld / N; q += THREADS) P::store(dz + (long long)q * N, zero);
-      if (tid < ld % N) dz[ld / N * N + tid] = 0;
-    }
-    return;
-  }
-  float old = 0.f, ref = 0.f, A = 0.f;   // requested with the row
-  if (terms) {
-    old = logp_old[t];
-    A = advantage[t];
-    if (logp_ref) ref = logp_ref[t];
-  }
+  using Elem = typename P::Elem;
+  static constexpr int N = P::N, STEP = NV * THREADS;
+  const Elem* z;
+  int V, whole, a, tid;   // whole: pieces that lie in the vocabulary; a: the chosen token; tid: of THREADS
+  float c;
   typename P::Raw r[NV];
-  const auto fetch = [&](int q0) {
+
+  __device__ __forceinline__ Row(const PolicyArgs& g, long long t, int tid)
+      : z(static_cast<const Elem*>(g.logits) + t * g.ld), V(g.V), whole(g.V / N), a(g.action[t]), tid(tid), c(g.p.c) {}
+
+  // the pieces q0 + tid, q0 + THREADS + tid, ... below `end`
+  __device__ __forceinline__ void fetch(int q0, int end) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int q = q0 + i * THREADS + tid;
       r[i] = P::none();
-      if (q < whole) r[i] = P::load(z + (long long)q * N);
-      else if (q == whole) r[i] = P::load_some(z + (long long)q * N, V - whole * N);
+      if (q < end) {
+        if (q < whole) r[i] = P::template load<ONCE>(z + (long long)q * N);
+        else r[i] = P::load_some(z + (long long)q * N, V - whole * N);
+      }
     }
-  };
-  float m = -INFINITY, s = 0.f;
-  constexpr int STEP = NV * THREADS;
-  const int last = whole / STEP * STEP;   // where the part that stays begins
-  for (int q0 = 0; q0 <= last; q0 += STEP) {
-    fetch(q0);
+  }
+  // adds what is held to the thread's (m, s); the chosen token's logit goes to *chosen
+  __device__ __forceinline__ void take(int q0, int end, float& m, float& s, float* chosen) {
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      if (q0 + i * THREADS > whole) continue;
+      if (q0 + i * THREADS >= end) continue;
       float x[N];
       P::unpack(r[i], x);
 #pragma unroll
       for (int j = 0; j < N; ++j) top = fmaxf(top, x[j]);
-      if (q0 + i * THREADS + tid == a / N) {
+      if (q0 + i * THREADS + tid == a / N && a / N < end) {
 #pragma unroll
         for (int j = 0; j < N; ++j)
-          if (j == a % N) za_s = x[j];
+          if (j == a % N) *chosen = x[j];
       }
     }
-    top *= p.c;
+    top *= c;
     const float base = fmaxf(m, top), from = base == -INFINITY ? 0.f : base;   // nothing but -inf so far
     s *= exp2_(m - from);
     m = base;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      if (q0 + i * THREADS > whole) continue;
+      if (q0 + i * THREADS >= end) continue;
       float x[N];
       forget(r[i]);
       P::unpack(r[i], x);
 #pragma unroll
-      for (int j = 0; j < N; ++j) s += exp2_(fmaf(x[j], p.c, -from));
+      for (int j = 0; j < N; ++j) s += exp2_(fmaf(x[j], c, -from));
     }
   }
-#pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) join(m, s, __shfl_xor(m, k, 64), __shfl_xor(s, k, 64));
-  if ((tid & 63) == 0) {
-    ms[tid >> 6] = m;
-    ss[tid >> 6] = s;
-  }
-  __syncthreads();
-  m = ms[0];
-  s = ss[0];
-#pragma unroll
-  for (int k = 1; k < WAVES; ++k) join(m, s, ms[k], ss[k]);
-  const float lp = fmaf(za_s, p.c, -m) * 0.693147180559945309f - logf(s);
-  if (tid == 0) logp[t] = lp;
-  if (!terms) return;
-  const Token k = token_loss(p, lp, old, logp_ref != nullptr, ref, A);
-  if (tid == 0) terms[t] = float4{w * (k.gain + p.kl_coef * k.kl), w * k.gain, w * k.kl, k.clipped ? w : 0.f};
-  if (!GRAD) return;
-  // 2^24 moves from the factor into the exponent, so that the power is no denormal number, which would become 0, where the
-  // gradient in single precision is one that is kept
-  const float u = p.scale * p.inv_temp * w * k.slope, minus = -u / s * 0x1p-24f, from = m - 24.f;
-  for (int q0 = last; q0 >= 0; q0 -= STEP) {
-    if (q0 < last) fetch(q0);
+  // writes the gradient of what is held
+  __device__ __forceinline__ void give(int q0, int end, Elem* dz, float u, float minus, float from) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int q = q0 + i * THREADS + tid;
-      if (q0 + i * THREADS > whole) continue;
+      if (q0 + i * THREADS >= end) continue;
       float x[N];
       forget(r[i]);
       P::unpack(r[i], x);
 #pragma unroll
-      for (int j = 0; j < N; ++j) x[j] = minus * exp2_(fmaf(x[j], p.c, -from));
+      for (int j = 0; j < N; ++j) x[j] = minus * exp2_(fmaf(x[j], c, -from));
       if (q == a / N) {
 #pragma unroll
         for (int j = 0; j < N; ++j)
           if (j == a % N) x[j] += u;
       }
-      if (q < whole) P::store(dz + (long long)q * N, P::pack(x));
-      else if (q == whole) P::store_some(dz + (long long)q * N, P::pack(x), V - whole * N);
+      if (q < end) {
+        if (q < whole) P::store(dz + (long long)q * N, P::pack(x));
+        else P::store_some(dz + (long long)q * N, P::pack(x), V - whole * N);
+      }
     }
   }
-  for (int j = V + tid; j < ld; j += THREADS) dz[j] = 0;
+};
+
+__device__ __forceinline__ void join_wave(float& m, float& s) {
+#pragma unroll
+  for (int k = 32; k >= 1; k >>= 1) join(m, s, __shfl_xor(m, k, 64), __shfl_xor(s, k, 64));
+}
+// (m, s) of a workgroup, in every thread.
+template <int THREADS>
+__device__ __forceinline__ void join_threads(float& m, float& s) {
+  __shared__ float ms[THREADS / 64], ss[THREADS / 64];
+  join_wave(m, s);
+  if (THREADS > 64 && (threadIdx.x & 63) == 0) {
+    ms[threadIdx.x >> 6] = m;
+    ss[threadIdx.x >> 6] = s;
+  }
+  __syncthreads();
+  if (THREADS == 64) return;
+  m = ms[0];
+  s = ss[0];
+#pragma unroll
+  for (int k = 1; k < THREADS / 64; ++k) join(m, s, ms[k], ss[k]);
 }
 
-__global__ __launch_bounds__(SUM_THREADS) void policy_sum_kernel(const float4* __restrict__ terms, int T, float* __restrict__ stats) {
-  __shared__ double part[SUM_THREADS / 64][4];
-  double sum[4] = {};
-  for (long long t = threadIdx.x; t < T; t += SUM_THREADS) {
-    const float4 x = terms[t];
-    sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+template <typename Elem>
+__device__ __forceinline__ void clear_row(Elem* dz, int from, int ld, int threads) {
+  for (int j = from + threadIdx.x; j < ld; j += threads) dz[j] = 0;
+}
+
+// The gradient of a logit is minus 2^(t - from), with u more for the chosen token.  2^24 moves from the factor into the
+// exponent: the power is then no denormal number, which would become 0, where the gradient in single precision is not 0.
+struct Slope {
+  float u, minus, from;
+};
+__device__ __forceinline__ Slope slope_of(const PolicyScalars& p, float w, float slope, float m, float s) {
+  const float u = p.scale * p.inv_temp * w * slope;
+  return {u, -u / s * 0x1p-24f, m - 24.f};
+}
+__device__ __forceinline__ float4 terms_of(const PolicyScalars& p, float w, const Token& k) {
+  return float4{w * (k.gain + p.kl_coef * k.kl), w * k.gain, w * k.kl, k.clipped ? w : 0.f};
+}
+__device__ __forceinline__ float logp_of(const PolicyScalars& p, float za, float m, float s) {
+  return fmaf(za, p.c, -m) * 0.693147180559945309f - logf(s);
+}
+
+// A workgroup of THREADS takes a row.  What fits is read once and stays in registers from the logits to their gradient; of a
+// longer row the last STEP pieces stay and the ones before them are read again.
+template <bool BF16, bool GRAD, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS) void policy_kernel(PolicyArgs g) {
+  using R = Row<BF16, !GRAD, THREADS, NV>;
+  __shared__ float chosen;
+  const int tid = threadIdx.x;
+  const long long t = blockIdx.x;
+  R row(g, t, tid);
+  auto* const dz = static_cast<typename R::Elem*>(g.dlogits) + (GRAD ? t * g.ld : 0);
+  const float w = g.weight ? g.weight[t] : 1.f;
+  if (w == 0.f || (unsigned)row.a >= (unsigned)g.V) {
+    if (tid == 0) {
+      g.logp[t] = 0.f;
+      if (g.terms) g.terms[t] = float4{0.f, 0.f, 0.f, 0.f};
+    }
+    if (GRAD) {
+      const typename R::P::Raw zero = {0, 0, 0, 0};
+      for (int q = tid; q < g.ld / R::N; q += THREADS) R::P::store(dz + (long long)q * R::N, zero);
+      clear_row(dz, g.ld / R::N * R::N, g.ld, THREADS);
+    }
+    return;
   }
+  float old = 0.f, ref = 0.f, A = 0.f;   // requested with the row
+  if (g.terms) {
+    old = g.logp_old[t];
+    A = g.advantage[t];
+    if (g.logp_ref) ref = g.logp_ref[t];
+  }
+  const int end = (g.V + R::N - 1) / R::N, last = end > R::STEP ? end - R::STEP : 0;   // from `last` on pieces stay
+  float m = -INFINITY, s = 0.f;
+  for (int q0 = 0; q0 < last; q0 += R::STEP) {
+    row.fetch(q0, min(q0 + R::STEP, last));
+    row.take(q0, min(q0 + R::STEP, last), m, s, &chosen);
+  }
+  row.fetch(last, end);
+  row.take(last, end, m, s, &chosen);
+  join_threads<THREADS>(m, s);
+  const float lp = logp_of(g.p, chosen, m, s);
+  if (tid == 0) g.logp[t] = lp;
+  if (!g.terms) return;
+  const Token k = token_loss(g.p, lp, old, g.logp_ref != nullptr, ref, A);
+  if (tid == 0) g.terms[t] = terms_of(g.p, w, k);
+  if (!GRAD) return;
+  const Slope d = slope_of(g.p, w, k.slope, m, s);
+  row.give(last, end, dz, d.u, d.minus, d.from);
+  for (int q0 = 0; q0 < last; q0 += R::STEP) {
+    row.fetch(q0, min(q0 + R::STEP, last));
+    row.give(q0, min(q0 + R::STEP, last), dz, d.u, d.minus, d.from);
+  }
+  clear_row(dz, g.V, g.ld, THREADS);
+}
+
+// Few rows: every wavefront that policy_kernel would give a row is a workgroup of its own, in two launches.  The first
+// leaves each wavefront's (m, s) and the chosen logit; the second joins them, reads the logits again and writes their
+// gradient.  Which pieces a thread takes and how sums are joined is that of policy_kernel, so a row's bits do not
+// depend on the number of rows.  The first workgroup of the second launch takes the sums over the tokens.
+constexpr int SUM_SPLIT_THREADS = 256;
+constexpr int PART_MAX = 16;         // wavefronts of a row
+constexpr int PART_ROWS_MAX = 256;   // rows of a batch that is split
+
+struct Parts {
+  float2* ms;      // [T, wavefronts]
+  float* chosen;   // [T]
+};
+
+template <bool BF16, int THREADS, int NV>
+__global__ __launch_bounds__(64) void policy_part_kernel(PolicyArgs g, Parts parts) {
+  using R = Row<BF16, false, THREADS, NV>;
+  constexpr int WAVES = THREADS / 64;
+  const int wave = blockIdx.x % WAVES;
+  const long long t = blockIdx.x / WAVES;
+  R row(g, t, wave * 64 + threadIdx.x);
+  if (g.weight[t] == 0.f || (unsigned)row.a >= (unsigned)g.V) return;
+  const int end = (g.V + R::N - 1) / R::N, last = end > R::STEP ? end - R::STEP : 0;
+  float m = -INFINITY, s = 0.f;
+  for (int q0 = 0; q0 < last; q0 += R::STEP) {
+    row.fetch(q0, min(q0 + R::STEP, last));
+    row.take(q0, min(q0 + R::STEP, last), m, s, parts.chosen + t);
+  }
+  row.fetch(last, end);
+  row.take(last, end, m, s, parts.chosen + t);
+  join_wave(m, s);
+  if (threadIdx.x == 0) parts.ms[t * WAVES + wave] = float2{m, s};
+}
+
+template <int THREADS>
+__device__ __forceinline__ void add_terms(double (&sum)[4], float* __restrict__ stats) {
+  __shared__ double part[THREADS / 64][4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
 #pragma unroll
@@ -250,9 +348,81 @@ __global__ __launch_bounds__(SUM_THREADS) void policy_sum_kernel(const float4* _
   __syncthreads();
   if (threadIdx.x < 4) {
     double all = 0.;
-    for (int w = 0; w < SUM_THREADS / 64; ++w) all += part[w][threadIdx.x];
+    for (int w = 0; w < THREADS / 64; ++w) all += part[w][threadIdx.x];
     stats[threadIdx.x] = (float)all;
   }
+}
+
+// m and s of a row: those of its wavefronts, joined in order.
+template <int WAVES, class Load>
+__device__ __forceinline__ void join_waves(float& m, float& s, Load load) {
+  float2 x = load(0);
+  m = x.x;
+  s = x.y;
+#pragma unroll
+  for (int k = 1; k < WAVES; ++k) {
+    x = load(k);
+    join(m, s, x.x, x.y);
+  }
+}
+
+template <bool BF16, int THREADS, int NV>
+__global__ __launch_bounds__(SUM_SPLIT_THREADS) void policy_apply_kernel(PolicyArgs g, Parts parts, int T, float* __restrict__ stats) {
+  using R = Row<BF16, true, THREADS, NV>;
+  constexpr int WAVES = THREADS / 64;
+  float m, s;
+  if (blockIdx.x == 0) {
+    double sum[4] = {};
+    for (int t = threadIdx.x; t < T; t += SUM_SPLIT_THREADS) {
+      const float w = g.weight[t];
+      float lp = 0.f;
+      if (w != 0.f && (unsigned)g.action[t] < (unsigned)g.V) {
+        join_waves<WAVES>(m, s, [&](int k) { return parts.ms[(long long)t * WAVES + k]; });
+        lp = logp_of(g.p, parts.chosen[t], m, s);
+        const Token k = token_loss(g.p, lp, g.logp_old[t], g.logp_ref != nullptr, g.logp_ref ? g.logp_ref[t] : 0.f, g.advantage[t]);
+        const float4 x = terms_of(g.p, w, k);
+        sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+      }
+      g.logp[t] = lp;
+    }
+    add_terms<SUM_SPLIT_THREADS>(sum, stats);
+    return;
+  }
+  if (threadIdx.x >= 64) return;   // the other workgroups are a wavefront
+  const int wave = (blockIdx.x - 1) % WAVES;
+  const long long t = (blockIdx.x - 1) / WAVES;
+  R row(g, t, wave * 64 + threadIdx.x);
+  auto* const dz = static_cast<typename R::Elem*>(g.dlogits) + t * g.ld;
+  const float w = g.weight[t];
+  const int end = (g.V + R::N - 1) / R::N;
+  if (wave == 0) clear_row(dz, g.V, g.ld, 64);
+  if (w == 0.f || (unsigned)row.a >= (unsigned)g.V) {
+    const typename R::P::Raw zero = {0, 0, 0, 0};
+    for (int q = row.tid; q < end; q += THREADS) {
+      if (q < row.whole) R::P::store(dz + (long long)q * R::N, zero);
+      else R::P::store_some(dz + (long long)q * R::N, zero, g.V - row.whole * R::N);
+    }
+    return;
+  }
+  row.fetch(0, end);
+  join_waves<WAVES>(m, s, [&](int k) { return parts.ms[t * WAVES + k]; });
+  const float lp = logp_of(g.p, parts.chosen[t], m, s);
+  const Token k = token_loss(g.p, lp, g.logp_old[t], g.logp_ref != nullptr, g.logp_ref ? g.logp_ref[t] : 0.f, g.advantage[t]);
+  const Slope d = slope_of(g.p, w, k.slope, m, s);
+  for (int q0 = 0;;) {
+    row.give(q0, end, dz, d.u, d.minus, d.from);
+    if ((q0 += R::STEP) >= end) break;
+    row.fetch(q0, end);
+  }
+}
+
+__global__ __launch_bounds__(SUM_THREADS) void policy_sum_kernel(const float4* __restrict__ terms, int T, float* __restrict__ stats) {
+  double sum[4] = {};
+  for (long long t = threadIdx.x; t < T; t += SUM_THREADS) {
+    const float4 x = terms[t];
+    sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+  }
+  add_terms<SUM_THREADS>(sum, stats);
 }
 
 static int check_policy(const char* who, const symi_policy* hp, int V, int ld) {
@@ -267,31 +437,73 @@ static int check_policy(const char* who, const symi_policy* hp, int V, int ld) {
   return SYMI_OK;
 }
 
-static int policy_impl(const char* who, const symi_ctx* ctx, const symi_policy* hp, const void* logits, int V, int ld,
-                       const int32_t* action, const float* logp_old, const float* logp_ref, const float* advantage,
-                       const float* weight, float* logp, float4* terms, void* dlogits, hipStream_t st) {
-  const PolicyScalars p = {hp->clip_low, hp->clip_high, hp->kl_coef, hp->inv_temperature, hp->grad_scale,
-                           (float)(1.4426950408889634 * hp->inv_temperature)};
-  const int T = ctx->cfg.T, kid = terms ? K_POLICY : K_TOKEN_LOGP;
-  const bool bf16 = hp->logits_dtype == SYMI_BF16;
-  const int pieces = V / (bf16 ? 8 : 4) + 1;
-#define ROWS(BF16, GRAD, THREADS, NV)                                                                                  \
-  SYMI_TIMED(ctx, kid, st, (policy_kernel<BF16, GRAD, THREADS, NV><<<T, THREADS, 0, st>>>(                             \
-      logits, V, ld, action, logp_old, logp_ref, advantage, weight, logp, terms, dlogits, p)))
-#define SIZES(BF16, GRAD)                                      \
-  if (pieces <= 64 * 4) ROWS(BF16, GRAD, 64, 4);               \
-  else if (pieces <= 256 * 4) ROWS(BF16, GRAD, 256, 4);        \
-  else if (pieces <= 512 * 8) ROWS(BF16, GRAD, 512, 8);        \
-  else if (pieces <= 1024 * 8) ROWS(BF16, GRAD, 1024, 8);      \
-  else ROWS(BF16, GRAD, 1024, 16)
-  if (bf16 && dlogits) { SIZES(true, true); }
-  else if (bf16) { SIZES(true, false); }
-  else if (dlogits) { SIZES(false, true); }
-  else { SIZES(false, false); }
-#undef SIZES
+struct PolicyWs {
+  size_t terms, ms, chosen, total;
+};
+static PolicyWs policy_ws(const symi_cfg* c) {
+  PolicyWs L;
+  const size_t rows = std::min(c->T, PART_ROWS_MAX);
+  L.terms = 0;
+  L.ms = align_up((size_t)c->T * sizeof(float4), 256);
+  L.chosen = L.ms + align_up(rows * PART_MAX * sizeof(float2), 256);
+  L.total = L.chosen + align_up(rows * sizeof(float), 256) + 256;
+  return L;
+}
+
+static PolicyScalars scalars(const symi_policy* hp) {
+  return {hp->clip_low, hp->clip_high, hp->kl_coef, hp->inv_temperature, hp->grad_scale, (float)(1.4426950408889634 * hp->inv_temperature)};
+}
+
+template <bool BF16>
+static void launch_rows(const symi_ctx* ctx, int kid, const PolicyArgs& g, hipStream_t st) {
+  const int T = ctx->cfg.T, pieces = cdiv(g.V, Piece<BF16>::N);
+#define ROWS(GRAD, THREADS, NV) SYMI_TIMED(ctx, kid, st, (policy_kernel<BF16, GRAD, THREADS, NV><<<T, THREADS, 0, st>>>(g)))
+  // With the gradient: the smallest workgroup that holds the row, four pieces a thread first (bf16, 16384 rows of 2000: 64
+  // threads 41 us, 256 52, 1024 202; 8192 of 12000: 512 threads of four 84, 256 of eight 85), then up to 16 (8192 of
+  // 50001: 512 of 16 389, in two parts 413 - 450).  Longer rows are read again in part, most of it from the memory-side
+  // cache, and two workgroups a unit of 64 registers are faster than one of 128 that holds all (16384 of 131072, a quarter
+  // masked: 1567 against 1718).  Without it nothing has to stay: eight pieces of 256 threads at a time (8192 of 32000 81), on few
+  // rows 512 threads (300 of 131072: 21.7 against 25.5) or 1024 (16 of 128000: 10.3 against 11.0).
+  if (g.dlogits) {
+    if (pieces <= 64 * 4) ROWS(true, 64, 4);
+    else if (pieces <= 256 * 4) ROWS(true, 256, 4);
+    else if (pieces <= 512 * 4) ROWS(true, 512, 4);
+    else if (pieces <= 512 * 8) ROWS(true, 512, 8);
+    else if (pieces <= 512 * 16) ROWS(true, 512, 16);
+    else ROWS(true, 1024, 8);
+  } else {
+    if (pieces <= 64 * 4) ROWS(false, 64, 4);
+    else if (pieces <= 256 * 4) ROWS(false, 256, 4);
+    else if (T <= ctx->cus / 4 && pieces > 8192) ROWS(false, 1024, 8);
+    else if (T < 4 * ctx->cus) ROWS(false, 512, 4);
+    else ROWS(false, 256, 8);
+  }
 #undef ROWS
-  SYMI_LAUNCH_CHECK(who);
-  return SYMI_OK;
+}
+
+// Whether a row's wavefronts are workgroups of their own: while all of them together are at most four for each
+// compute unit.  us with the gradient, one workgroup a row : split.  bf16 V = 131072: 16 rows 22.0 : 14.2, 64 23.8 : 20.4, 128
+// 26.3 : 27.3; V = 50001: 1 row 13.2 : 11.4, 64 15.9 : 14.3, 128 16.8 : 17.8; V = 16000: 16 rows 8.7 : 6.8, 128 9.2 : 8.5, 256
+// 10.4 : 11.4; V = 4000: 16 rows 7.3 : 6.2, 256 7.6 : 6.9; fp32 V = 32003: 16 rows 11.9 : 11.5, 256 18.1 : 23.6.
+static bool wants_parts(const symi_ctx* ctx, int pieces) {
+  const int T = ctx->cfg.T, waves = pieces <= 64 * 4 ? 1 : pieces <= 256 * 4 ? 4 : pieces <= 512 * 16 ? 8 : 16;
+  return T >= 1 && T <= PART_ROWS_MAX && waves > 1 && T * waves <= 4 * ctx->cus;
+}
+template <bool BF16>
+static void launch_parts(const symi_ctx* ctx, const PolicyArgs& g, const Parts& parts, float* stats, hipStream_t st) {
+  const int T = ctx->cfg.T, pieces = cdiv(g.V, Piece<BF16>::N);
+#define PARTS(THREADS, NV)                                                                                                        \
+  do {                                                                                                                            \
+    SYMI_TIMED(ctx, K_POLICY, st, (policy_part_kernel<BF16, THREADS, NV><<<T * (THREADS / 64), 64, 0, st>>>(g, parts)));          \
+    SYMI_TIMED(ctx, K_POLICY_SUM, st, (policy_apply_kernel<BF16, THREADS, NV><<<T * (THREADS / 64) + 1, SUM_SPLIT_THREADS, 0, st>>>( \
+        g, parts, T, stats)));                                                                                                    \
+  } while (0)
+  if (pieces <= 256 * 4) PARTS(256, 4);
+  else if (pieces <= 512 * 4) PARTS(512, 4);
+  else if (pieces <= 512 * 8) PARTS(512, 8);
+  else if (pieces <= 512 * 16) PARTS(512, 16);
+  else PARTS(1024, 8);
+#undef PARTS
 }
 
 }  // namespace symi
@@ -300,7 +512,7 @@ using namespace symi;
 
 extern "C" size_t symi_policy_workspace_bytes(const symi_cfg* cfg) {
   if (check_cfg(cfg, "symi_policy_workspace_bytes") != SYMI_OK) return 0;
-  return align_up((size_t)cfg->T * sizeof(float4), 256) + 256;
+  return policy_ws(cfg).total;
 }
 
 extern "C" int symi_token_logp(const symi_ctx* ctx, const symi_policy* hp, const void* logits, int V, int ld,
@@ -310,7 +522,11 @@ extern "C" int symi_token_logp(const symi_ctx* ctx, const symi_policy* hp, const
   if (int rc = check_policy(who, hp, V, ld)) return rc;
   if (cfg->T == 0) return SYMI_OK;
   SYMI_REQUIRE(logits && action && logp, who, "NULL pointer");
-  return policy_impl(who, ctx, hp, logits, V, ld, action, nullptr, nullptr, nullptr, weight, logp, nullptr, nullptr, as_stream(stream));
+  const PolicyArgs g = {logits, V, ld, action, nullptr, nullptr, nullptr, weight, logp, nullptr, nullptr, scalars(hp)};
+  if (hp->logits_dtype == SYMI_BF16) launch_rows<true>(ctx, K_TOKEN_LOGP, g, as_stream(stream));
+  else launch_rows<false>(ctx, K_TOKEN_LOGP, g, as_stream(stream));
+  SYMI_LAUNCH_CHECK(who);
+  return SYMI_OK;
 }
 
 extern "C" int symi_policy_loss(const symi_ctx* ctx, const symi_policy* hp, const void* logits, int V, int ld,
@@ -320,13 +536,23 @@ extern "C" int symi_policy_loss(const symi_ctx* ctx, const symi_policy* hp, cons
   const char* const who = "symi_policy_loss";
   SYMI_ENTER(ctx, who);
   if (int rc = check_policy(who, hp, V, ld)) return rc;
-  SYMI_REQUIRE(cfg->T == 0 || logp_ref || hp->kl_coef == 0.f, who, "kl_coef needs logp_ref");
-  SYMI_REQUIRE(stats && ws && (cfg->T == 0 || (logits && action && logp_old && advantage && weight && logp)), who, "NULL pointer");
+  const int T = cfg->T;
+  SYMI_REQUIRE(T == 0 || logp_ref || hp->kl_coef == 0.f, who, "kl_coef needs logp_ref");
+  SYMI_REQUIRE(stats && ws && (T == 0 || (logits && action && logp_old && advantage && weight && logp)), who, "NULL pointer");
   hipStream_t st = as_stream(stream);
-  float4* const terms = reinterpret_cast<float4*>(align_up(reinterpret_cast<size_t>(ws), 256));
-  if (cfg->T)
-    if (int rc = policy_impl(who, ctx, hp, logits, V, ld, action, logp_old, logp_ref, advantage, weight, logp, terms, dlogits, st)) return rc;
-  SYMI_TIMED(ctx, K_POLICY_SUM, st, (policy_sum_kernel<<<1, SUM_THREADS, 0, st>>>(terms, cfg->T, stats)));
+  const PolicyWs L = policy_ws(cfg);
+  char* const w = reinterpret_cast<char*>(align_up(reinterpret_cast<size_t>(ws), 256));
+  const PolicyArgs g = {logits, V, ld, action, logp_old, logp_ref, advantage, weight, logp, reinterpret_cast<float4*>(w + L.terms), dlogits, scalars(hp)};
+  const bool bf16 = hp->logits_dtype == SYMI_BF16;
+  if (dlogits && wants_parts(ctx, cdiv(V, bf16 ? 8 : 4))) {
+    const Parts parts = {reinterpret_cast<float2*>(w + L.ms), reinterpret_cast<float*>(w + L.chosen)};
+    if (bf16) launch_parts<true>(ctx, g, parts, stats, st);
+    else launch_parts<false>(ctx, g, parts, stats, st);
+  } else {
+    if (T && bf16) launch_rows<true>(ctx, K_POLICY, g, st);
+    else if (T) launch_rows<false>(ctx, K_POLICY, g, st);
+    SYMI_TIMED(ctx, K_POLICY_SUM, st, (policy_sum_kernel<<<1, SUM_THREADS, 0, st>>>(g.terms, T, stats)));
+  }
   SYMI_LAUNCH_CHECK(who);
   return SYMI_OK;
 }
