@@ -18,7 +18,7 @@ enum KernelId {
   K_FILL = 0, K_ROUTE, K_ROUTE_BWD, K_PLACE, K_CHUNK_COUNT, K_CHUNK_SCAN, K_CHUNK_RANK, K_GATHER,
   K_TILE_MAP, K_GEMM_FWD1, K_GEMM_FWD2, K_GEMM_BWD_DH, K_GEMM_BWD_DX, K_GEMM_WGRAD2, K_GEMM_WGRAD1,
   K_COMBINE, K_COMBINE_BWD, K_DISPATCH_BWD, K_ADAM, K_REPLICA_AR, K_ROUTER_FWD, K_ROUTER_DX, K_ROUTER_DW, K_SLICE_SUM,
-  K_DISPATCH_ONE, K_EMBED_FWD, K_EMBED_SORT, K_EMBED_SUM, K_TOKEN_LOGP, K_POLICY, K_POLICY_SUM, K_ADAMW, K_ADAMW_DECODE, K_COUNT
+  K_DISPATCH_ONE, K_EMBED_FWD, K_EMBED_SORT, K_EMBED_SUM, K_EMBED_JOIN, K_TOKEN_LOGP, K_POLICY, K_POLICY_SUM, K_ADAMW, K_ADAMW_DECODE, K_COUNT
 };
 struct TimedLaunch { int kid; hipEvent_t a, b; };
 

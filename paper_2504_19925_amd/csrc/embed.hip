@@ -1,10 +1,11 @@
 // symi_embed_fwd / symi_embed_bwd: the token embedding X[t] = scale * table[tokens[t]] and its gradient
 // dTable[v] = scale * sum of dX[t] over the tokens t that are v, in fp32.
 //
-// The gradient needs the tokens of a row together and in an order that is the same on every run.  One launch sorts: a
-// workgroup owns R consecutive rows of the table, reads all tokens, counts the ones below its rows (where its part of
-// the sorted order begins) and packs the ones of its own rows in token order; its wavefronts then give each row's tokens
-// their places.  Counts are integer sums and places come from ballots, so nothing depends on the order of atomics.
+// The gradient needs the tokens of a row together and in an order that is the same on every run.  One launch sorts: the
+// rows of the table are dealt out to workgroups like cards (the most frequent tokens are neighbours in many vocabularies),
+// and each workgroup reads all tokens twice: it counts the ones of the workgroups before it, where its part of the sorted order
+// begins, and its own by row and wavefront, then gives every token its place.  Counts are integer sums and places come from
+// ballots, so nothing depends on the order of the additions in LDS.
 #include <algorithm>
 #include <type_traits>
 
@@ -13,27 +14,26 @@
 namespace symi {
 
 constexpr int EMBED_THREADS = 256;
-constexpr int SORT_THREADS = 1024;
-constexpr int SORT_WAVES = SORT_THREADS / 64;
-constexpr int SORT_ROWS_MAX = 8192;   // rows that one workgroup of the sort counts in LDS
-constexpr int SORT_GROUPS = 256;
+constexpr int SORT_ROWS_MAX = 1024;   // rows that one workgroup of the sort counts in LDS, for each wavefront
+constexpr int SORT_GROUPS = 256;      // workgroups, unless the rows are more
 
 // A 16-byte piece of a row: 8 bf16 or 4 fp32 values.
 template <bool BF16> struct Piece {
   static constexpr int N = BF16 ? 8 : 4;
   using Elem = std::conditional_t<BF16, uint16_t, float>;
-  static __device__ __forceinline__ void load(const void* base, long long at, float (&x)[N]) {
-    if constexpr (BF16) {
-      const u32x4_bf16 q = *reinterpret_cast<const u32x4_bf16*>(static_cast<const uint16_t*>(base) + at);
+  using Raw = std::conditional_t<BF16, u32x4_bf16, f32x4_f32>;
+  static __device__ __forceinline__ Raw load(const void* base, long long at) {
+    return *reinterpret_cast<const Raw*>(static_cast<const Elem*>(base) + at);
+  }
+  static __device__ __forceinline__ void unpack(Raw q, float (&x)[N]) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (BF16) {
         x[2 * i] = __uint_as_float(q[i] << 16);
         x[2 * i + 1] = __uint_as_float(q[i] & 0xffff0000u);
+      } else {
+        x[i] = q[i];
       }
-    } else {
-      const f32x4_f32 q = *reinterpret_cast<const f32x4_f32*>(static_cast<const float*>(base) + at);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = q[i];
     }
   }
   static __device__ __forceinline__ void store(void* base, long long at, const float (&x)[N]) {
@@ -64,168 +64,416 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_fwd_kernel(const int32_t*
   const bool inside = (unsigned)v < (unsigned)V;
   for (int c = lane; c < pieces; c += 1 << lg) {
     float x[P::N];
-    if (inside) P::load(table, (long long)v * d + c * P::N, x);
+    if (inside) P::unpack(P::load(table, (long long)v * d + c * P::N), x);
 #pragma unroll
     for (int i = 0; i < P::N; ++i) x[i] = inside ? x[i] * scale : 0.f;
     P::store(X, t * d + c * P::N, x);
   }
 }
 
-// Workgroup b: rows [b R, b R + R) of the table.  offs [V+1]: where each row's tokens begin in `order` [T], which lists
-// the tokens (their places in the batch, ascending) row by row; packed and packed_key are its scratch.
-__global__ __launch_bounds__(SORT_THREADS) void embed_sort_kernel(const int32_t* __restrict__ tokens, int T, int V, int R,
-                                                                  int32_t* __restrict__ offs, int32_t* __restrict__ order,
-                                                                  int32_t* packed, int32_t* packed_key) {
-  __shared__ int32_t cursor[SORT_ROWS_MAX];
-  __shared__ int32_t wave_less[SORT_WAVES], wave_own[SORT_WAVES], wave_sum[SORT_WAVES];
-  constexpr int U = 8;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long long v0 = (long long)blockIdx.x * R;
-  const int rows = (int)(v0 + R < V ? R : V - v0);
-  for (int r = threadIdx.x; r < rows; r += SORT_THREADS) cursor[r] = 0;
-  // every wavefront reads a stretch of consecutive tokens
-  const long long stretch = (((long long)T + SORT_WAVES - 1) / SORT_WAVES + 63) / 64 * 64;
-  const long long lo = wave * stretch, hi = lo + stretch < T ? lo + stretch : T;
-  const auto row_of = [&](long long i) -> int { return i < hi ? tokens[i] : -1; };
-  const auto is_own = [&](int v) { return v >= 0 && (unsigned)v - (unsigned)v0 < (unsigned)rows; };
+// Workgroup b of 2^lg: the rows v with v mod 2^lg = b.  span [V]: where each row's tokens begin and end in `order`, which lists
+// the tokens (their places in the batch) row by row, in the order of the wavefronts; rows_of: the rows of the same list; total: its length.
+constexpr int SORT_KEEP = 512;   // own tokens that a wavefront keeps from the first reading; with more it reads again
+template <int WAVES, int U>
+__global__ __launch_bounds__(WAVES * 64) void embed_sort_kernel(const int32_t* __restrict__ tokens, int T, int V, int lg,
+                                                                int2* __restrict__ span, int32_t* __restrict__ order,
+                                                                int32_t* __restrict__ rows_of, int32_t* __restrict__ total) {
+  extern __shared__ int32_t count[];   // [WAVES, rows]: of a wavefront's tokens, then the place of its next one
+  __shared__ int32_t wave_less[WAVES], wave_sum[WAVES];
+  __shared__ int2 kept[WAVES][SORT_KEEP];   // place in the batch, row
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned b = blockIdx.x, low = (1u << lg) - 1;
+  const int rows = (int)(((unsigned)V + low - b) >> lg);
+  for (int i = threadIdx.x; i < WAVES * rows; i += WAVES * 64) count[i] = 0;
+  __syncthreads();
+  int32_t* const mine = count + wave * rows;
+  // a wavefront reads every WAVES-th 64 U tokens
+  constexpr int AHEAD = WAVES * 64 * U;
+  const int lo = wave * 64 * U, hi = T;
+  // 64 U tokens from i0 on; padding becomes 2^32 - 1
+  const auto fetch = [&](long long i0, unsigned (&v)[U]) {
+    const int32_t* const from = tokens + i0;
+    if (i0 + 64 * U <= hi) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = (unsigned)from[u * 64 + lane];
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = u * 64 + lane < hi - i0 ? (unsigned)from[u * 64 + lane] : 0xffffffffu;
+    }
+  };
   int less = 0, own = 0;
-  for (long long i = lo + lane; i < hi; i += 64 * U) {
-    int v[U];
+  unsigned v[U], ahead[U];
+  if (lo < hi) fetch(lo, ahead);
+  for (long long i0 = lo; i0 < hi; i0 += AHEAD) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = row_of(i + u * 64);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      less += (unsigned)v[u] < (unsigned)v0;
-      own += is_own(v[u]);
-    }
-  }
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) {
-    less += __shfl_xor(less, m, 64);
-    own += __shfl_xor(own, m, 64);
-  }
-  if (lane == 0) {
-    wave_less[wave] = less;
-    wave_own[wave] = own;
-  }
-  __syncthreads();
-  int base = 0, count = 0, at = 0;
-#pragma unroll
-  for (int w = 0; w < SORT_WAVES; ++w) {
-    base += wave_less[w];
-    at += w < wave ? wave_own[w] : 0;
-    count += wave_own[w];
-  }
-  at += base;
-  for (long long i0 = lo; own && i0 < hi; i0 += 64 * U) {   // a wavefront without any skips it
-    int v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = row_of(i0 + lane + u * 64);
+    for (int u = 0; u < U; ++u) v[u] = ahead[u] < (unsigned)V ? ahead[u] : 0xffffffffu;
+    if (i0 + AHEAD < hi) fetch(i0 + AHEAD, ahead);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const bool mine = is_own(v[u]);
-      const unsigned long long mask = __ballot(mine);
-      if (mine) {
-        const int to = at + __popcll(mask & ((1ull << lane) - 1));
-        packed[to] = (int)(i0 + lane + u * 64);
-        packed_key[to] = v[u] - (int)v0;
-        atomicAdd(&cursor[v[u] - (int)v0], 1);
-      }
-      at += __popcll(mask);
+      const unsigned w = v[u] & low;   // of padding: the last workgroup's, but no row of it
+      less += w < b;
+      const bool is_own = w == b && v[u] != 0xffffffffu;
+      const unsigned long long mask = __ballot(is_own);
+      if (!mask) continue;
+      const int to = own + __popcll(mask & ((1ull << lane) - 1));
+      if (is_own && to < SORT_KEEP) kept[wave][to] = int2{(int)i0 + u * 64 + lane, (int)v[u]};
+      if (is_own && to >= SORT_KEEP) atomicAdd(&mine[v[u] >> lg], 1);
+      own += __popcll(mask);
     }
   }
+  for (int k = lane; k < min(own, SORT_KEEP); k += 64) atomicAdd(&mine[(unsigned)kept[wave][k].y >> lg], 1);
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) less += __shfl_xor(less, m, 64);
+  if (lane == 0) wave_less[wave] = less;
   __syncthreads();
-  // counts of the rows -> where their tokens begin
-  const int each = (rows + SORT_THREADS - 1) / SORT_THREADS, r0 = threadIdx.x * each;
+  // counts -> where the tokens of a row and wavefront begin
+  const int each = (rows + WAVES * 64 - 1) / (WAVES * 64), r0 = threadIdx.x * each;
   int sum = 0;
-  for (int r = r0; r < r0 + each && r < rows; ++r) sum += cursor[r];
-  int before = sum;
+  for (int r = r0; r < r0 + each && r < rows; ++r)
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) sum += count[w * rows + r];
+  int at = sum;
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) {
-    const int x = __shfl_up(before, m, 64);
-    if (lane >= m) before += x;
+    const int x = __shfl_up(at, m, 64);
+    if (lane >= m) at += x;
   }
-  if (lane == 63) wave_sum[wave] = before;
+  if (lane == 63) wave_sum[wave] = at;
   __syncthreads();
-  before += base - sum;
+  at -= sum;
 #pragma unroll
-  for (int w = 0; w < SORT_WAVES; ++w) before += w < wave ? wave_sum[w] : 0;
+  for (int w = 0; w < WAVES; ++w) at += wave_less[w] + (w < wave ? wave_sum[w] : 0);
   for (int r = r0; r < r0 + each && r < rows; ++r) {
-    const int n = cursor[r];
-    cursor[r] = before;
-    offs[v0 + r] = before;
-    before += n;
+    const int begin = at;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const int n = count[w * rows + r];
+      count[w * rows + r] = at;
+      at += n;
+    }
+    span[((long long)r << lg) + b] = int2{begin, at};
   }
-  if (v0 + rows == V && threadIdx.x == 0) offs[V] = base + count;
+  if (b == low && threadIdx.x == WAVES * 64 - 1) *total = at;
   __syncthreads();
-  volatile int32_t* const at_row = cursor;   // a row's place is one wavefront's alone
-  // wavefront w places the tokens of the rows w, w + 16, ...
-  for (int i0 = 0; i0 < count; i0 += 64) {
-    const bool there = i0 + lane < count;
-    const int r = there ? packed_key[base + i0 + lane] : 0;
-    const int t = there ? packed[base + i0 + lane] : 0;
-    const bool mine = there && (r & (SORT_WAVES - 1)) == wave;
-    unsigned long long left = __ballot(mine);
-    while (left) {
-      const int row = __builtin_amdgcn_readlane(r, (int)__builtin_ctzll(left));
-      const unsigned long long same = __ballot(mine && r == row);
-      const int to = at_row[row];
-      if (mine && r == row) order[to + __popcll(same & ((1ull << lane) - 1))] = t;
-      if (lane == 0) at_row[row] = to + __popcll(same);
+  volatile int32_t* const next = mine;
+  // 64 tokens, the workgroup's own among them: equal ones take consecutive places
+  const auto place = [&](bool is_own, unsigned v, int i) {
+    int rank = 0;          // among the equal ones
+    bool final = false;    // the last of them
+    for (unsigned long long left = __ballot(is_own); left;) {
+      const unsigned row = (unsigned)__builtin_amdgcn_readlane((int)v, (int)__builtin_ctzll(left));
+      const unsigned long long same = __ballot(is_own && v == row);
+      if (is_own && v == row) {
+        rank = __popcll(same & ((1ull << lane) - 1));
+        final = same >> lane == 1;
+      }
       left &= ~same;
+    }
+    if (!is_own) return;
+    const int p = next[v >> lg] + rank;
+    order[p] = i;
+    rows_of[p] = (int)v;
+    if (final) next[v >> lg] = p + 1;
+  };
+  if (own <= SORT_KEEP) {
+    for (int k = 0; k < own; k += 64) {
+      const int2 x = kept[wave][min(k + lane, SORT_KEEP - 1)];
+      place(k + lane < own, (unsigned)x.y, x.x);
+    }
+    return;
+  }
+  for (long long i0 = lo; i0 < hi; i0 += AHEAD) {
+    fetch(i0, v);
+#pragma unroll
+    for (int u = 0; u < U; ++u) place((v[u] & low) == b && v[u] < (unsigned)V, v[u], (int)i0 + u * 64 + lane);
+  }
+}
+
+// Sums: the sorted tokens are cut into chunks of C, whatever their rows, so that a row that half the batch chose is as much
+// parallel work as any other.  A wavefront takes 64 pieces of the rows of a chunk.  A run of at most 2 C tokens of one row is all of
+// it the work of the chunk in which it begins.  Of a longer one every chunk sums its share and leaves it in `partial`
+// [chunks, 2, d]: in slot 1 where the run begins, in slot 0 of the chunks after it; embed_join adds them up in order.
+constexpr int SUM_ROWS = 8;   // rows that a wavefront has in flight
+
+__device__ __forceinline__ void put_row(float* to, const float* x, float scale) {
+  f32x4_f32 y;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) y[j] = x[j] * scale;
+  *reinterpret_cast<f32x4_f32*>(to) = y;
+}
+__device__ __forceinline__ void put_row(float* to, const float* x, float scale, f32x4_f32 old) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) old[j] = x[j] * scale + old[j];
+  *reinterpret_cast<f32x4_f32*>(to) = old;
+}
+
+template <bool BF16, bool ADD>
+__global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(
+    const void* __restrict__ dX, const int2* __restrict__ span, const int32_t* __restrict__ order,
+    const int32_t* __restrict__ rows_of, const int32_t* __restrict__ total_of, int size, int V, int d, int parts, int C, int units,
+    float scale, float* __restrict__ dTable, float* __restrict__ partial, long long sum_groups) {
+  using P = Piece<BF16>;
+  constexpr int N = P::N;
+  const int lane = threadIdx.x & 63;
+  const long long group = (long long)blockIdx.y * gridDim.x + blockIdx.x;
+  if (group >= sum_groups) {   // rows without tokens: 1024 pieces of four values each
+    const long long first = (group - sum_groups) * 1024, all = (long long)V * (d / 4);
+    const int per = d / 4;
+    const long long v = first / per;
+    const int begin = (int)(first - v * per);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = k * EMBED_THREADS + threadIdx.x;
+      if (first + i >= all) return;
+      const int2 s = span[v + (begin + i) / per];
+      if (s.x == s.y) *reinterpret_cast<f32x4_f32*>(dTable + (first + i) * 4) = f32x4_f32{0.f, 0.f, 0.f, 0.f};
+    }
+    return;
+  }
+  const int unit = __builtin_amdgcn_readfirstlane((int)(group * (EMBED_THREADS / 64)) + (threadIdx.x >> 6));
+  const int total = *total_of, chunk = unit / parts, lo = chunk * C;
+  // the places around the chunk's, requested before anything about them is known (there are `size` of them)
+  int row = rows_of[min(lo + lane, size - 1)], token = order[min(lo + lane, size - 1)];
+  int begin = lo, end = min(lo + C, total);
+  if (unit >= units || begin >= end) return;
+  const int c = ((unit % parts) * 64 + lane) * N;
+  const bool live = c < d;
+  int head = 0, tail = 0;   // tokens of long runs that began before / that go on behind
+  {
+    const int2 a = span[__builtin_amdgcn_readlane(row, 0)], z = span[__builtin_amdgcn_readlane(row, end - 1 - lo)];
+    if (z.y > end) {
+      if (z.y - z.x <= 2 * C) end = z.y;
+      else tail = end - max(z.x, begin);
+    }
+    if (a.x < begin) {
+      if (a.y - a.x <= 2 * C) begin = a.y;
+      else head = min(a.y, lo + C) - begin;
+    }
+    if (head && tail == end - begin) tail = 0;   // nothing but the middle of one run
+  }
+  const int first_own = begin + head, last_own = end - tail;
+  float sum[N] = {};
+  for (int w0 = lo; w0 < end; w0 += 64) {   // lane i holds place w0 + i
+    const int n = min(64, end - w0);
+    if (w0 > lo) {
+      row = rows_of[min(w0 + lane, size - 1)];
+      token = order[min(w0 + lane, size - 1)];
+    }
+    // a run ends where the next token's row is another
+    const int next = __shfl_down(row, 1, 64);
+    const bool last = lane < n && (w0 + lane + 1 == end || (lane == 63 ? rows_of[w0 + 64] : next) != row);
+    const unsigned long long ends = __ballot(last);
+    for (int i0 = max(begin - w0, 0); i0 < n; i0 += SUM_ROWS) {
+      typename P::Raw x[SUM_ROWS];
+      f32x4_f32 old[SUM_ROWS][N / 4];
+#pragma unroll
+      for (int u = 0; u < SUM_ROWS; ++u) {
+        const int i = i0 + u;
+        if (i >= n) continue;
+        if (live) x[u] = P::load(dX, (long long)__builtin_amdgcn_readlane(token, i) * d + c);
+        if (ADD && live && (ends >> i & 1) && w0 + i >= first_own && w0 + i < last_own)
+#pragma unroll
+          for (int h = 0; h < N / 4; ++h)
+            old[u][h] = *reinterpret_cast<const f32x4_f32*>(dTable + (long long)__builtin_amdgcn_readlane(row, i) * d + c + 4 * h);
+      }
+#pragma unroll
+      for (int u = 0; u < SUM_ROWS; ++u) {
+        const int i = i0 + u;
+        if (i >= n) continue;
+        float y[N];
+        P::unpack(x[u], y);
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] += y[j];
+        if (!(ends >> i & 1)) continue;
+        if (live && w0 + i >= first_own && w0 + i < last_own) {
+          float* const to = dTable + (long long)__builtin_amdgcn_readlane(row, i) * d + c;
+#pragma unroll
+          for (int h = 0; h < N / 4; ++h) {
+            if (ADD) put_row(to + 4 * h, sum + 4 * h, scale, old[u][h]);
+            else put_row(to + 4 * h, sum + 4 * h, scale);
+          }
+        } else if (live) {
+          float* const to = partial + ((long long)chunk * 2 + (w0 + i >= first_own)) * d + c;
+#pragma unroll
+          for (int h = 0; h < N / 4; ++h) put_row(to + 4 * h, sum + 4 * h, 1.f);
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] = 0.f;
+      }
     }
   }
 }
 
-// A wavefront sums 64 pieces of one row over the row's tokens.
-template <bool BF16>
-__global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(const void* __restrict__ dX,
-                                                                  const int32_t* __restrict__ offs,
-                                                                  const int32_t* __restrict__ order, int V, int d,
-                                                                  int parts, float scale, int accumulate,
-                                                                  float* __restrict__ dTable) {
-  using P = Piece<BF16>;
-  const long long id = (long long)blockIdx.y * gridDim.x + blockIdx.x;
-  const long long unit = id * (EMBED_THREADS / 64) + (threadIdx.x >> 6);
-  const long long v = unit / parts;
-  const int c = ((int)(unit % parts) * 64 + (threadIdx.x & 63)) * P::N;
-  if (v >= V || c >= d) return;
-  const int lo = offs[v], hi = offs[v + 1];
-  if (lo == hi && accumulate) return;
-  float sum[P::N] = {};
-  for (int i = lo; i < hi; ++i) {
-    float x[P::N];
-    P::load(dX, (long long)order[i] * d + c, x);
+// A workgroup: 256 columns of the long runs that begin in one of JOIN_CHUNKS chunks.
+constexpr int JOIN_WAVES = 8, JOIN_ROWS = 8, JOIN_CHUNKS = 16;
+template <bool ADD>
+__global__ __launch_bounds__(JOIN_WAVES * 64) void embed_join_kernel(const int2* __restrict__ span, const int32_t* __restrict__ rows_of,
+                                                                     const int32_t* __restrict__ total_of, const float* __restrict__ partial,
+                                                                     int d, int C, float scale, float* __restrict__ dTable) {
+  __shared__ float4 share[JOIN_WAVES][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int total = *total_of;
+  // the last run of a chunk
+  const long long hi = ((long long)blockIdx.x * JOIN_CHUNKS + lane + 1) * C;
+  const bool there = lane < JOIN_CHUNKS && hi < total;
+  const int row_of = there ? rows_of[hi - 1] : 0;
+  const int2 s = there ? span[row_of] : int2{0, 0};
+  unsigned long long todo = __ballot(there && s.y > hi && s.x >= hi - C && s.y - s.x > 2 * C);
+  const int c = (blockIdx.y * 64 + lane) * 4;
+  const bool live = c < d;
+  for (; todo; todo &= todo - 1) {
+    const int i = (int)__builtin_ctzll(todo), row = __builtin_amdgcn_readlane(row_of, i), stop = __builtin_amdgcn_readlane(s.y, i);
+    const int chunk = blockIdx.x * JOIN_CHUNKS + i;
+    const int count = (stop - 1) / C - chunk + 1;   // shares: slot 1 of this chunk, slot 0 of the next ones
+    const int each = (count + JOIN_WAVES - 1) / JOIN_WAVES, begin = wave * each, end = min(begin + each, count);
+    float4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = begin; k0 < end && live; k0 += JOIN_ROWS) {
+      float4 x[JOIN_ROWS];
 #pragma unroll
-    for (int j = 0; j < P::N; ++j) sum[j] += x[j];
-  }
-  float* const to = dTable + v * d + c;
+      for (int u = 0; u < JOIN_ROWS; ++u)
+        if (k0 + u < end) x[u] = *reinterpret_cast<const float4*>(partial + ((long long)(chunk + k0 + u) * 2 + (k0 + u == 0)) * d + c);
 #pragma unroll
-  for (int h = 0; h < P::N; h += 4) {
-    float y[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = sum[h + j] * scale;
-    if (accumulate) {
-      float old[4];
-      Piece<false>::load(to, h, old);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] += old[j];
+      for (int u = 0; u < JOIN_ROWS; ++u)
+        if (k0 + u < end) { sum.x += x[u].x; sum.y += x[u].y; sum.z += x[u].z; sum.w += x[u].w; }
     }
-    Piece<false>::store(to, h, y);
+    share[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && live) {
+      float y[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+      for (int w = 1; w < JOIN_WAVES; ++w) {
+        const float4 o = share[w][lane];
+        y[0] += o.x; y[1] += o.y; y[2] += o.z; y[3] += o.w;
+      }
+      float* const to = dTable + (long long)row * d + c;
+      if (ADD) put_row(to, y, scale, *reinterpret_cast<const f32x4_f32*>(to));
+      else put_row(to, y, scale);
+    }
+    __syncthreads();
   }
+}
+
+// Small batches, in one launch without a sort: a workgroup takes 64 pieces of one token's row.  It reads all tokens and does
+// the work of the row if its token is the first of it: every wavefront sums the row's tokens of its part of the batch.  The
+// workgroups behind those look which of their rows of the table the batch has and write zeros to the others.
+constexpr int FEW_MAX = 2048;   // tokens
+template <bool BF16, bool ADD, int WAVES, int STEPS>
+__global__ __launch_bounds__(WAVES * 64) void embed_few_kernel(const int32_t* __restrict__ tokens, const void* __restrict__ dX, int T,
+                                                                  int V, int d, int parts, float scale, float* __restrict__ dTable) {
+  using P = Piece<BF16>;
+  constexpr int N = P::N, THREADS = WAVES * 64;
+  __shared__ float share[WAVES][64 * N];
+  __shared__ int32_t has[1024 / 2 + 2];   // rows that 1024 pieces of four values touch, at least two pieces each
+  __shared__ int32_t earlier;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const long long group = (long long)blockIdx.y * gridDim.x + blockIdx.x;
+  if (group >= (long long)T * parts) {
+    const long long first = (group - (long long)T * parts) * 1024, all = (long long)V * (d / 4);
+    if (first >= all) return;
+    const int per = d / 4;
+    const long long v0 = first / per;
+    const int begin = (int)(first - v0 * per), rows = (begin + 1023) / per + 1;
+    for (int r = tid; r < rows; r += THREADS) has[r] = 0;
+    __syncthreads();
+    for (int t = tid; t < T; t += THREADS) {
+      const long long r = tokens[t] - v0;
+      if (r >= 0 && r < rows) has[r] = 1;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 1024 / THREADS; ++k) {
+      const int i = k * THREADS + tid;
+      if (first + i < all && !has[(begin + i) / per]) *reinterpret_cast<f32x4_f32*>(dTable + (first + i) * 4) = f32x4_f32{0.f, 0.f, 0.f, 0.f};
+    }
+    return;
+  }
+  const int t0 = (int)(group / parts), c = ((int)(group % parts) * 64 + lane) * N;
+  const int row = tokens[t0];
+  if ((unsigned)row >= (unsigned)V) return;
+  const bool live = c < d;
+  if (tid == 0) earlier = 0;
+  // a wavefront's part of the batch: STEPS times 64 tokens
+  unsigned long long same[STEPS];
+  bool before = false;
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) {
+    const int t = (wave * STEPS + k) * 64 + lane;
+    const bool is = t < T && tokens[t] == row;
+    same[k] = __ballot(is);
+    before |= is && t < t0;
+  }
+  __syncthreads();
+  if (before) earlier = 1;
+  __syncthreads();
+  if (earlier) return;
+  f32x4_f32 old[N / 4];
+  float* const to = dTable + (long long)row * d + c;
+  if (ADD && wave == 0 && live)
+#pragma unroll
+    for (int h = 0; h < N / 4; ++h) old[h] = *reinterpret_cast<const f32x4_f32*>(to + 4 * h);
+  float sum[N] = {};
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) {
+    unsigned long long left = same[k];
+    while (left) {
+      typename P::Raw x[SUM_ROWS];
+      unsigned long long now = left;
+#pragma unroll
+      for (int u = 0; u < SUM_ROWS; ++u) {
+        if (!now) continue;
+        if (live) x[u] = P::load(dX, (long long)((wave * STEPS + k) * 64 + (int)__builtin_ctzll(now)) * d + c);
+        now &= now - 1;
+      }
+#pragma unroll
+      for (int u = 0; u < SUM_ROWS; ++u) {
+        if (!left) continue;
+        float y[N];
+        P::unpack(x[u], y);
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] += y[j];
+        left &= left - 1;
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) share[wave][j * 64 + lane] = sum[j];
+  __syncthreads();
+  if (wave != 0 || !live) return;
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w)
+#pragma unroll
+    for (int j = 0; j < N; ++j) sum[j] += share[w][j * 64 + lane];
+#pragma unroll
+  for (int h = 0; h < N / 4; ++h) {
+    if (ADD) put_row(to + 4 * h, sum + 4 * h, scale, old[h]);
+    else put_row(to + 4 * h, sum + 4 * h, scale);
+  }
+}
+
+// Tokens of a chunk: many chunks keep the chip busy, but every chunk of a long run leaves a row in fp32, and one workgroup
+// adds up what a run left.
+static int embed_chunk(const symi_cfg* c, int parts) {
+  int C = 8;
+  while (C < 64 && ((long long)c->T * parts > 16384LL * C || c->T > 2048 * C)) C *= 2;
+  return C;
 }
 
 struct EmbedWs {
-  size_t offs, order, packed, packed_key, total;
+  size_t span, order, rows_of, count, partial, total;
+  int parts, chunk, chunks;   // wavefronts across a row of dX; tokens of a chunk; chunks
 };
 static EmbedWs embed_ws(const symi_cfg* c, int V) {
   EmbedWs L;
   size_t off = 0;
   const auto take = [&](size_t bytes) { const size_t at = off; off += align_up(bytes, 256); return at; };
-  L.offs = take(((size_t)V + 1) * sizeof(int32_t));
+  L.span = take((size_t)V * sizeof(int2));
   L.order = take((size_t)c->T * sizeof(int32_t));
-  L.packed = take((size_t)c->T * sizeof(int32_t));
-  L.packed_key = take((size_t)c->T * sizeof(int32_t));
+  L.rows_of = take((size_t)c->T * sizeof(int32_t));
+  L.count = take(sizeof(int32_t));
+  L.parts = cdiv(c->d, 64 * (c->dtype == SYMI_BF16 ? 8 : 4));
+  L.chunk = embed_chunk(c, L.parts);
+  L.chunks = cdiv(c->T, L.chunk);
+  L.partial = take((size_t)L.chunks * 2 * c->d * sizeof(float));
   L.total = off + 256;
   return L;
 }
@@ -275,20 +523,57 @@ extern "C" int symi_embed_bwd(const symi_ctx* ctx, const int32_t* tokens, const 
   const EmbedWs L = embed_ws(cfg, V);
   char* const w = reinterpret_cast<char*>(align_up(reinterpret_cast<size_t>(ws), 256));
   const auto ints = [&](size_t at) { return reinterpret_cast<int32_t*>(w + at); };
-  const int R = std::min(std::max(cdiv(V, SORT_GROUPS), 1), SORT_ROWS_MAX);
+  int2* const span = reinterpret_cast<int2*>(w + L.span);
   hipStream_t st = as_stream(stream);
-  SYMI_TIMED(ctx, K_EMBED_SORT, st, (embed_sort_kernel<<<cdiv(V, R), SORT_THREADS, 0, st>>>(
-      tokens, cfg->T, V, R, ints(L.offs), ints(L.order), ints(L.packed), ints(L.packed_key))));
-  const int parts = cdiv(cfg->d, 64 * (bf16 ? 8 : 4));
-  const long long groups = ((long long)V * parts + 3) / 4;
+  const long long fill_groups = accumulate ? 0 : ((long long)V * (cfg->d / 4) + 1023) / 1024;
   // workgroups over two dimensions: the threads of one end at 2^32
-  const dim3 grid((unsigned)std::min(groups, 1LL << 20), (unsigned)((groups + (1LL << 20) - 1) >> 20));
-  if (bf16)
-    SYMI_TIMED(ctx, K_EMBED_SUM, st, (embed_sum_kernel<true><<<grid, EMBED_THREADS, 0, st>>>(
-        dX, ints(L.offs), ints(L.order), V, cfg->d, parts, scale, accumulate, dTable)));
-  else
-    SYMI_TIMED(ctx, K_EMBED_SUM, st, (embed_sum_kernel<false><<<grid, EMBED_THREADS, 0, st>>>(
-        dX, ints(L.offs), ints(L.order), V, cfg->d, parts, scale, accumulate, dTable)));
+  const auto grid_of = [](long long groups) { return dim3((unsigned)std::min(groups, 1LL << 20), (unsigned)((groups + (1LL << 20) - 1) >> 20)); };
+  if (cfg->T <= FEW_MAX) {
+    const long long groups = (long long)cfg->T * L.parts + fill_groups;
+    if (groups == 0) return SYMI_OK;
+#define FEW_(BF16, ADD, WAVES, STEPS)                                                                                   \
+  SYMI_TIMED(ctx, K_EMBED_SUM, st, (embed_few_kernel<BF16, ADD, WAVES, STEPS><<<grid_of(groups), WAVES * 64, 0, st>>>(  \
+      tokens, dX, cfg->T, V, cfg->d, L.parts, scale, dTable)))
+#define FEW(BF16, ADD) do { if (cfg->T <= 512) FEW_(BF16, ADD, 4, 2); else FEW_(BF16, ADD, 8, 4); } while (0)
+    if (bf16 && accumulate) FEW(true, true);
+    else if (bf16) FEW(true, false);
+    else if (accumulate) FEW(false, true);
+    else FEW(false, false);
+#undef FEW
+#undef FEW_
+    SYMI_LAUNCH_CHECK(who);
+    return SYMI_OK;
+  }
+  int lg = 0;
+  while ((1LL << lg) < V && ((1 << lg) < SORT_GROUPS || cdiv(V, 1 << lg) > SORT_ROWS_MAX)) ++lg;
+  const int rows = cdiv(V, 1 << lg);
+#define SORT(WAVES, U)                                                                                                     \
+  SYMI_TIMED(ctx, K_EMBED_SORT, st, (embed_sort_kernel<WAVES, U><<<1 << lg, WAVES * 64, WAVES * rows * sizeof(int32_t), st>>>( \
+      tokens, cfg->T, V, lg, span, ints(L.order), ints(L.rows_of), ints(L.count))))
+  if (cfg->T <= 4 * 64 * 8) SORT(4, 8);
+  else SORT(16, 8);
+#undef SORT
+  float* const partial = reinterpret_cast<float*>(w + L.partial);
+  const int units = L.chunks * L.parts;
+  const long long sum_groups = (units + 3) / 4;
+  const dim3 grid = grid_of(sum_groups + fill_groups);
+#define SUM(BF16, ADD)                                                                                                      \
+  SYMI_TIMED(ctx, K_EMBED_SUM, st, (embed_sum_kernel<BF16, ADD><<<grid, EMBED_THREADS, 0, st>>>(                            \
+      dX, span, ints(L.order), ints(L.rows_of), ints(L.count), cfg->T, V, cfg->d, L.parts, L.chunk, units, scale, dTable, partial, sum_groups)))
+  if (bf16 && accumulate) SUM(true, true);
+  else if (bf16) SUM(true, false);
+  else if (accumulate) SUM(false, true);
+  else SUM(false, false);
+#undef SUM
+  {
+    const dim3 grid((unsigned)cdiv(L.chunks, JOIN_CHUNKS), (unsigned)cdiv(cfg->d, 256));
+#define JOIN(ADD)                                                                                         \
+  SYMI_TIMED(ctx, K_EMBED_JOIN, st, (embed_join_kernel<ADD><<<grid, JOIN_WAVES * 64, 0, st>>>(            \
+      span, ints(L.rows_of), ints(L.count), partial, cfg->d, L.chunk, scale, dTable)))
+    if (accumulate) JOIN(true);
+    else JOIN(false);
+#undef JOIN
+  }
   SYMI_LAUNCH_CHECK(who);
   return SYMI_OK;
 }
