@@ -51,36 +51,47 @@ template <bool BF16> struct Piece {
   }
 };
 
-// lanes = 2^lg lanes share a token's row and walk it in pieces.
-template <bool BF16>
+// 2^lg lanes share a token's row and walk it in pieces, R rows at a time.
+template <bool BF16, int R>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_fwd_kernel(const int32_t* __restrict__ tokens,
                                                                   const void* __restrict__ table, void* __restrict__ X,
                                                                   int T, int V, int d, float scale, int lg) {
   using P = Piece<BF16>;
-  const long long t = ((long long)blockIdx.x * EMBED_THREADS + threadIdx.x) >> lg;
-  if (t >= T) return;
+  const long long t0 = (((long long)blockIdx.x * EMBED_THREADS + threadIdx.x) >> lg) * R;
+  if (t0 >= T) return;
   const int lane = threadIdx.x & ((1 << lg) - 1), pieces = d / P::N;
-  const int v = tokens[t];
-  const bool inside = (unsigned)v < (unsigned)V;
-  for (int c = lane; c < pieces; c += 1 << lg) {
-    float x[P::N];
-    if (inside) P::unpack(P::load(table, (long long)v * d + c * P::N), x);
+  int v[R];
 #pragma unroll
-    for (int i = 0; i < P::N; ++i) x[i] = inside ? x[i] * scale : 0.f;
-    P::store(X, t * d + c * P::N, x);
+  for (int r = 0; r < R; ++r) v[r] = t0 + r < T ? tokens[t0 + r] : -1;
+  for (int c = lane; c < pieces; c += 1 << lg) {
+    typename P::Raw x[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if ((unsigned)v[r] < (unsigned)V) x[r] = P::load(table, (long long)v[r] * d + c * P::N);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (R > 1 && t0 + r >= T) continue;
+      const bool inside = (unsigned)v[r] < (unsigned)V;
+      float y[P::N];
+      P::unpack(x[r], y);
+#pragma unroll
+      for (int i = 0; i < P::N; ++i) y[i] = inside ? y[i] * scale : 0.f;
+      P::store(X, (t0 + r) * d + c * P::N, y);
+    }
   }
 }
 
 // Workgroup b of 2^lg: the rows v with v mod 2^lg = b.  span [V]: where each row's tokens begin and end in `order`, which lists
 // the tokens (their places in the batch) row by row, in the order of the wavefronts; rows_of: the rows of the same list; total: its length.
-constexpr int SORT_KEEP = 512;   // own tokens that a wavefront keeps from the first reading; with more it reads again
+constexpr int SORT_KEEP = 1408;       // own tokens that a wavefront keeps from the first reading; with more it reads again
+constexpr int SORT_KEEP_T = 1 << 22;  // in batches of at most this many: place in the batch and place among the own rows in 32 bits
 template <int WAVES, int U>
 __global__ __launch_bounds__(WAVES * 64) void embed_sort_kernel(const int32_t* __restrict__ tokens, int T, int V, int lg,
                                                                 int2* __restrict__ span, int32_t* __restrict__ order,
                                                                 int32_t* __restrict__ rows_of, int32_t* __restrict__ total) {
   extern __shared__ int32_t count[];   // [WAVES, rows]: of a wavefront's tokens, then the place of its next one
   __shared__ int32_t wave_less[WAVES], wave_sum[WAVES];
-  __shared__ int2 kept[WAVES][SORT_KEEP];   // place in the batch, row
+  __shared__ uint32_t kept[WAVES][SORT_KEEP];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned b = blockIdx.x, low = (1u << lg) - 1;
   const int rows = (int)(((unsigned)V + low - b) >> lg);
@@ -101,6 +112,7 @@ __global__ __launch_bounds__(WAVES * 64) void embed_sort_kernel(const int32_t* _
       for (int u = 0; u < U; ++u) v[u] = u * 64 + lane < hi - i0 ? (unsigned)from[u * 64 + lane] : 0xffffffffu;
     }
   };
+  const int keep = T <= SORT_KEEP_T ? SORT_KEEP : 0;
   int less = 0, own = 0;
   unsigned v[U], ahead[U];
   if (lo < hi) fetch(lo, ahead);
@@ -116,12 +128,14 @@ __global__ __launch_bounds__(WAVES * 64) void embed_sort_kernel(const int32_t* _
       const unsigned long long mask = __ballot(is_own);
       if (!mask) continue;
       const int to = own + __popcll(mask & ((1ull << lane) - 1));
-      if (is_own && to < SORT_KEEP) kept[wave][to] = int2{(int)i0 + u * 64 + lane, (int)v[u]};
-      if (is_own && to >= SORT_KEEP) atomicAdd(&mine[v[u] >> lg], 1);
+      if (is_own) {
+        if (to < keep) kept[wave][to] = ((unsigned)i0 + u * 64 + lane) << 10 | v[u] >> lg;
+        else atomicAdd(&mine[v[u] >> lg], 1);
+      }
       own += __popcll(mask);
     }
   }
-  for (int k = lane; k < min(own, SORT_KEEP); k += 64) atomicAdd(&mine[(unsigned)kept[wave][k].y >> lg], 1);
+  for (int k = lane; k < min(own, keep); k += 64) atomicAdd(&mine[kept[wave][k] & 1023u], 1);
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) less += __shfl_xor(less, m, 64);
   if (lane == 0) wave_less[wave] = less;
@@ -175,10 +189,10 @@ __global__ __launch_bounds__(WAVES * 64) void embed_sort_kernel(const int32_t* _
     rows_of[p] = (int)v;
     if (final) next[v >> lg] = p + 1;
   };
-  if (own <= SORT_KEEP) {
+  if (own <= keep) {
     for (int k = 0; k < own; k += 64) {
-      const int2 x = kept[wave][min(k + lane, SORT_KEEP - 1)];
-      place(k + lane < own, (unsigned)x.y, x.x);
+      const uint32_t x = kept[wave][min(k + lane, SORT_KEEP - 1)];
+      place(k + lane < own, (x & 1023u) << lg | b, (int)(x >> 10));
     }
     return;
   }
@@ -207,27 +221,33 @@ __device__ __forceinline__ void put_row(float* to, const float* x, float scale, 
   *reinterpret_cast<f32x4_f32*>(to) = old;
 }
 
+// Zeros to rows without tokens: FILL_PIECES pieces of four values from `first` on, below `all`.
+constexpr int FILL_PIECES = 2048;
+template <int THREADS>
+__device__ __forceinline__ void fill_rows(const int2* __restrict__ span, long long first, long long all, int d, float* __restrict__ dTable) {
+  const int per = d / 4;
+  const long long v = first / per;
+  const int begin = (int)(first - v * per);
+#pragma unroll
+  for (int k = 0; k < FILL_PIECES / THREADS; ++k) {
+    const int i = k * THREADS + threadIdx.x;
+    if (first + i >= all) return;
+    const int2 s = span[v + (begin + i) / per];
+    if (s.x == s.y) *reinterpret_cast<f32x4_f32*>(dTable + (first + i) * 4) = f32x4_f32{0.f, 0.f, 0.f, 0.f};
+  }
+}
+
 template <bool BF16, bool ADD>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(
     const void* __restrict__ dX, const int2* __restrict__ span, const int32_t* __restrict__ order,
-    const int32_t* __restrict__ rows_of, const int32_t* __restrict__ total_of, int size, int V, int d, int parts, int C, int units,
-    float scale, float* __restrict__ dTable, float* __restrict__ partial, long long sum_groups) {
+    const int32_t* __restrict__ rows_of, const int32_t* __restrict__ total_of, int size, int d, int parts, int C, int units, float scale,
+    float* __restrict__ dTable, float* __restrict__ partial, long long sum_groups, long long fill_to) {
   using P = Piece<BF16>;
   constexpr int N = P::N;
   const int lane = threadIdx.x & 63;
   const long long group = (long long)blockIdx.y * gridDim.x + blockIdx.x;
-  if (group >= sum_groups) {   // rows without tokens: 1024 pieces of four values each
-    const long long first = (group - sum_groups) * 1024, all = (long long)V * (d / 4);
-    const int per = d / 4;
-    const long long v = first / per;
-    const int begin = (int)(first - v * per);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int i = k * EMBED_THREADS + threadIdx.x;
-      if (first + i >= all) return;
-      const int2 s = span[v + (begin + i) / per];
-      if (s.x == s.y) *reinterpret_cast<f32x4_f32*>(dTable + (first + i) * 4) = f32x4_f32{0.f, 0.f, 0.f, 0.f};
-    }
+  if (group >= sum_groups) {
+    fill_rows<EMBED_THREADS>(span, (group - sum_groups) * FILL_PIECES, fill_to, d, dTable);
     return;
   }
   const int unit = __builtin_amdgcn_readfirstlane((int)(group * (EMBED_THREADS / 64)) + (threadIdx.x >> 6));
@@ -304,26 +324,34 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(
   }
 }
 
-// A workgroup: 256 columns of the long runs that begin in one of JOIN_CHUNKS chunks.
+// A workgroup: 256 columns of the long runs that begin in one of JOIN_CHUNKS chunks.  The workgroups behind those fill rows.
 constexpr int JOIN_WAVES = 8, JOIN_ROWS = 8, JOIN_CHUNKS = 16;
 template <bool ADD>
 __global__ __launch_bounds__(JOIN_WAVES * 64) void embed_join_kernel(const int2* __restrict__ span, const int32_t* __restrict__ rows_of,
                                                                      const int32_t* __restrict__ total_of, const float* __restrict__ partial,
-                                                                     int d, int C, float scale, float* __restrict__ dTable) {
+                                                                     int size, int d, int C, int joins, int columns, long long fill_from,
+                                                                     long long fill_to, float scale,
+                                                                     float* __restrict__ dTable) {
   __shared__ float4 share[JOIN_WAVES][64];
+  const long long group = (long long)blockIdx.y * gridDim.x + blockIdx.x;
+  if (group >= (long long)joins * columns) {
+    fill_rows<JOIN_WAVES * 64>(span, fill_from + (group - (long long)joins * columns) * FILL_PIECES, fill_to, d, dTable);
+    return;
+  }
+  const int block = (int)(group / columns), column = (int)(group % columns);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int total = *total_of;
   // the last run of a chunk
-  const long long hi = ((long long)blockIdx.x * JOIN_CHUNKS + lane + 1) * C;
+  const long long hi = ((long long)block * JOIN_CHUNKS + lane + 1) * C;
+  const int row_of = rows_of[min(hi, (long long)size) - 1];   // beyond the total: anything
   const bool there = lane < JOIN_CHUNKS && hi < total;
-  const int row_of = there ? rows_of[hi - 1] : 0;
   const int2 s = there ? span[row_of] : int2{0, 0};
   unsigned long long todo = __ballot(there && s.y > hi && s.x >= hi - C && s.y - s.x > 2 * C);
-  const int c = (blockIdx.y * 64 + lane) * 4;
+  const int c = (column * 64 + lane) * 4;
   const bool live = c < d;
   for (; todo; todo &= todo - 1) {
     const int i = (int)__builtin_ctzll(todo), row = __builtin_amdgcn_readlane(row_of, i), stop = __builtin_amdgcn_readlane(s.y, i);
-    const int chunk = blockIdx.x * JOIN_CHUNKS + i;
+    const int chunk = block * JOIN_CHUNKS + i;
     const int count = (stop - 1) / C - chunk + 1;   // shares: slot 1 of this chunk, slot 0 of the next ones
     const int each = (count + JOIN_WAVES - 1) / JOIN_WAVES, begin = wave * each, end = min(begin + each, count);
     float4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -453,7 +481,7 @@ __global__ __launch_bounds__(WAVES * 64) void embed_few_kernel(const int32_t* __
 // Tokens of a chunk: many chunks keep the chip busy, but every chunk of a long run leaves a row in fp32, and one workgroup
 // adds up what a run left.
 static int embed_chunk(const symi_cfg* c, int parts) {
-  int C = 8;
+  int C = 4;
   while (C < 64 && ((long long)c->T * parts > 16384LL * C || c->T > 2048 * C)) C *= 2;
   return C;
 }
@@ -502,12 +530,18 @@ extern "C" int symi_embed_fwd(const symi_ctx* ctx, const int32_t* tokens, const 
   const int pieces = cfg->d / (bf16 ? 8 : 4);
   int lg = 0;
   while (lg < 8 && (1 << lg) < pieces) ++lg;
-  const int grid = cdiv((long long)cfg->T << lg, EMBED_THREADS);
   hipStream_t st = as_stream(stream);
-  if (bf16)
-    SYMI_TIMED(ctx, K_EMBED_FWD, st, (embed_fwd_kernel<true><<<grid, EMBED_THREADS, 0, st>>>(tokens, table, X, cfg->T, V, cfg->d, scale, lg)));
-  else
-    SYMI_TIMED(ctx, K_EMBED_FWD, st, (embed_fwd_kernel<false><<<grid, EMBED_THREADS, 0, st>>>(tokens, table, X, cfg->T, V, cfg->d, scale, lg)));
+  // Two rows at a time where every unit still has four workgroups: 65536 rows of d = 4096, bf16 157 -> 149 us (1.07 GB, 0.7 of them
+  // distinct), 30000 of d = 1000, fp32 47 -> 36; four rows 152 and 38, eight 154 and 39.
+  const bool many = cfg->T >= 8 * ctx->cus * (EMBED_THREADS >> lg);
+#define FWD(BF16, R)                                                                                                       \
+  SYMI_TIMED(ctx, K_EMBED_FWD, st, (embed_fwd_kernel<BF16, R><<<cdiv((long long)cdiv(cfg->T, R) << lg, EMBED_THREADS), EMBED_THREADS, 0, st>>>( \
+      tokens, table, X, cfg->T, V, cfg->d, scale, lg)))
+  if (bf16 && many) FWD(true, 2);
+  else if (bf16) FWD(true, 1);
+  else if (many) FWD(false, 2);
+  else FWD(false, 1);
+#undef FWD
   SYMI_LAUNCH_CHECK(who);
   return SYMI_OK;
 }
@@ -525,11 +559,10 @@ extern "C" int symi_embed_bwd(const symi_ctx* ctx, const int32_t* tokens, const 
   const auto ints = [&](size_t at) { return reinterpret_cast<int32_t*>(w + at); };
   int2* const span = reinterpret_cast<int2*>(w + L.span);
   hipStream_t st = as_stream(stream);
-  const long long fill_groups = accumulate ? 0 : ((long long)V * (cfg->d / 4) + 1023) / 1024;
   // workgroups over two dimensions: the threads of one end at 2^32
   const auto grid_of = [](long long groups) { return dim3((unsigned)std::min(groups, 1LL << 20), (unsigned)((groups + (1LL << 20) - 1) >> 20)); };
   if (cfg->T <= FEW_MAX) {
-    const long long groups = (long long)cfg->T * L.parts + fill_groups;
+    const long long groups = (long long)cfg->T * L.parts + (accumulate ? 0 : ((long long)V * (cfg->d / 4) + 1023) / 1024);
     if (groups == 0) return SYMI_OK;
 #define FEW_(BF16, ADD, WAVES, STEPS)                                                                                   \
   SYMI_TIMED(ctx, K_EMBED_SUM, st, (embed_few_kernel<BF16, ADD, WAVES, STEPS><<<grid_of(groups), WAVES * 64, 0, st>>>(  \
@@ -556,20 +589,26 @@ extern "C" int symi_embed_bwd(const symi_ctx* ctx, const int32_t* tokens, const 
   float* const partial = reinterpret_cast<float*>(w + L.partial);
   const int units = L.chunks * L.parts;
   const long long sum_groups = (units + 3) / 4;
-  const dim3 grid = grid_of(sum_groups + fill_groups);
+  // Rows without tokens get their zeros behind the sums (together they run at the rate of a copy; one after the other the
+  // sums alone took 225 us and the zeros 145, in one launch 330), the last eighth of the table beside the joins, which are few
+  // and wait for memory: c5's took 20 us by themselves.
+  const long long pieces = accumulate ? 0 : (long long)V * (cfg->d / 4), fill_sum = pieces - pieces / 8;
+  const auto fills = [](long long n) { return (n + FILL_PIECES - 1) / FILL_PIECES; };
+  const dim3 grid = grid_of(sum_groups + fills(fill_sum));
 #define SUM(BF16, ADD)                                                                                                      \
   SYMI_TIMED(ctx, K_EMBED_SUM, st, (embed_sum_kernel<BF16, ADD><<<grid, EMBED_THREADS, 0, st>>>(                            \
-      dX, span, ints(L.order), ints(L.rows_of), ints(L.count), cfg->T, V, cfg->d, L.parts, L.chunk, units, scale, dTable, partial, sum_groups)))
+      dX, span, ints(L.order), ints(L.rows_of), ints(L.count), cfg->T, cfg->d, L.parts, L.chunk, units, scale, dTable, partial, sum_groups, fill_sum)))
   if (bf16 && accumulate) SUM(true, true);
   else if (bf16) SUM(true, false);
   else if (accumulate) SUM(false, true);
   else SUM(false, false);
 #undef SUM
   {
-    const dim3 grid((unsigned)cdiv(L.chunks, JOIN_CHUNKS), (unsigned)cdiv(cfg->d, 256));
+    const int joins = cdiv(L.chunks, JOIN_CHUNKS), columns = cdiv(cfg->d, 256);
+    const dim3 grid = grid_of((long long)joins * columns + fills(pieces - fill_sum));
 #define JOIN(ADD)                                                                                         \
   SYMI_TIMED(ctx, K_EMBED_JOIN, st, (embed_join_kernel<ADD><<<grid, JOIN_WAVES * 64, 0, st>>>(            \
-      span, ints(L.rows_of), ints(L.count), partial, cfg->d, L.chunk, scale, dTable)))
+      span, ints(L.rows_of), ints(L.count), partial, cfg->T, cfg->d, L.chunk, joins, columns, fill_sum, pieces, scale, dTable)))
     if (accumulate) JOIN(true);
     else JOIN(false);
 #undef JOIN
