@@ -13,6 +13,7 @@
 #include <math.h>
 
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "common.h"
@@ -43,7 +44,7 @@ struct AdamwChunk {
 };
 
 struct AdamwScalars {
-  float lr, beta1, keep1, beta2, keep2, eps, wd, gscale, fix1, fix2;
+  float lr, beta1, keep1, beta2, keep2, eps, wd, gscale, fix1, fix2, root2;
   uint32_t key;
 };
 
@@ -70,116 +71,251 @@ __device__ __forceinline__ float v_value(float c, float a) {
 template <class Value>
 __device__ __forceinline__ float code_between(float x, float a, float guess, float top, float u, Value value) {
 #pragma clang fp contract(off)
-  float lo = fminf(fmaxf(floorf(guess), 0.f), top - 1.f);
+  float lo = fminf(floorf(guess), top - 1.f);
   float below = value(lo, a), above = value(lo + 1.f, a);
-  if (below > x) {
-    lo -= 1.f;
-    above = below;
+  const bool under = below > x, over = above <= x && lo < top - 1.f;
+  if (__builtin_expect(__ballot(under || over) != 0, 0)) {   // about one block in forty
+    lo += under ? -1.f : over ? 1.f : 0.f;
     below = value(lo, a);
-  } else if (above <= x && lo < top - 1.f) {
-    lo += 1.f;
-    below = above;
     above = value(lo + 1.f, a);
   }
   return x - below > u * (above - below) ? lo + 1.f : lo;
 }
 
 // Bits of the largest |value| of a wavefront: of floats without their sign the order is that of their bits, NaN on top.
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_with(uint32_t x) {
+  const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+  return x > y ? x : y;
+}
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) {
-    const uint32_t y = (uint32_t)__shfl_xor((int)x, m, 64);
-    x = x > y ? x : y;
-  }
-  return x;
+  x = max_with<0xb1>(x);    // lanes 1, 0, 3, 2 of four
+  x = max_with<0x4e>(x);    // 2, 3, 0, 1
+  x = max_with<0x141>(x);   // eight mirrored
+  x = max_with<0x140>(x);   // sixteen mirrored
+  x = max_with<0x142>(x);   // the last lane of each sixteen to the next sixteen
+  x = max_with<0x143>(x);   // lane 31 to the upper half
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 // 0 for a block of nothing but denormal numbers, NaN for one that is not finite
 __device__ __forceinline__ float scale_of(uint32_t bits) {
   return bits < 0x00800000u ? 0.f : bits < 0x7f800000u ? __uint_as_float(bits) : __uint_as_float(0x7fc00000u);
 }
 
-// What a lane holds of an array: the values from `at` on that lie below n (`full`: all four, as one access).
-template <bool BF16>
-__device__ __forceinline__ void load4(const void* p, long long at, long long n, float (&x)[4]) {
+// Four values of a lane, as they lie in memory at any alignment.
+typedef uint32_t u32x2_bf16 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32_codes __attribute__((aligned(1)));
+template <bool BF16> struct Four {
+  using Vec = std::conditional_t<BF16, u32x2_bf16, f32x4_f32>;
+  using Elem = std::conditional_t<BF16, uint16_t, float>;
+  static __device__ __forceinline__ Vec load(const void* p, long long at) { return *reinterpret_cast<const Vec*>(static_cast<const Elem*>(p) + at); }
+  static __device__ __forceinline__ void store(void* p, long long at, const float (&x)[4]) {
+    Vec v;
+    if constexpr (BF16) {
+      v[0] = pack_bf16x2(x[0], x[1]);
+      v[1] = pack_bf16x2(x[2], x[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = x[i];
+    }
+    *reinterpret_cast<Vec*>(static_cast<Elem*>(p) + at) = v;
+  }
+  static __device__ __forceinline__ void unpack(Vec v, float (&x)[4]) {
+    if constexpr (BF16) {
+      x[0] = __uint_as_float(v[0] << 16);
+      x[1] = __uint_as_float(v[0] & 0xffff0000u);
+      x[2] = __uint_as_float(v[1] << 16);
+      x[3] = __uint_as_float(v[1] & 0xffff0000u);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = v[i];
+    }
+  }
+  // the first `n` of them (the others 0), and back
+  static __device__ __forceinline__ Vec load_some(const void* p, long long at, long long n) {
+    const Elem* const q = static_cast<const Elem*>(p) + at;
+    Vec v;
+    if constexpr (BF16) {
+      v[0] = (n > 0 ? q[0] : 0u) | (n > 1 ? q[1] : 0u) << 16;
+      v[1] = (n > 2 ? q[2] : 0u) | (n > 3 ? q[3] : 0u) << 16;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = i < n ? q[i] : 0.f;
+    }
+    return v;
+  }
+  static __device__ __forceinline__ void store_some(void* p, long long at, long long n, const float (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) {
+        if constexpr (BF16) static_cast<uint16_t*>(p)[at + i] = f32_to_bf16(x[i]); else static_cast<float*>(p)[at + i] = x[i];
+      }
+  }
+};
+__device__ __forceinline__ uint32_t load_codes(const void* p, long long at) { return *reinterpret_cast<const u32_codes*>(static_cast<const uint8_t*>(p) + at); }
+__device__ __forceinline__ uint32_t load_codes_some(const void* p, long long at, long long n) {
+  uint32_t x = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x |= (i < n ? (uint32_t)static_cast<const uint8_t*>(p)[at + i] : 0u) << (8 * i);
+  return x;
+}
+__device__ __forceinline__ void store_codes(void* p, long long at, uint32_t x) { *reinterpret_cast<u32_codes*>(static_cast<uint8_t*>(p) + at) = x; }
+__device__ __forceinline__ void store_codes_some(void* p, long long at, long long n, uint32_t x) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    x[i] = at + i >= n ? 0.f : BF16 ? bf16_to_f32(static_cast<const uint16_t*>(p)[at + i]) : static_cast<const float*>(p)[at + i];
+    if (i < n) static_cast<uint8_t*>(p)[at + i] = (uint8_t)(x >> (8 * i));
 }
-template <bool BF16>
-__device__ __forceinline__ void store4(void* p, long long at, long long n, const float (&x)[4]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (at + i < n) {
-      if (BF16) static_cast<uint16_t*>(p)[at + i] = f32_to_bf16(x[i]);
-      else static_cast<float*>(p)[at + i] = x[i];
-    }
-}
-
-template <bool PARAM16, bool GRAD16, bool CODES>
-__device__ __forceinline__ void adamw_block(const AdamwTensor& t, const AdamwScalars& h, float gscale, long long block, int lane) {
-  const long long at = block * ADAMW_BLOCK + lane * 4;
-  float g[4], w[4], m[4], v[4];
-  float* const weights = PARAM16 ? t.master : static_cast<float*>(t.param);
-  load4<GRAD16>(t.grad, at, t.n, g);
-  load4<false>(weights, at, t.n, w);
-  if (CODES) {
-    const float am = t.m_scale[block], av = t.v_scale[block];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float cm = at + i < t.n ? (float)static_cast<const int8_t*>(t.m)[at + i] : 0.f;
-      const float cv = at + i < t.n ? (float)static_cast<const uint8_t*>(t.v)[at + i] : 0.f;
-      m[i] = copysignf(m_value(cm, am), cm);
-      v[i] = v_value(cv, av);
-    }
-  } else {
-    load4<false>(t.m, at, t.n, m);
-    load4<false>(t.v, at, t.n, v);
-  }
-  uint32_t big_m = 0, big_v = 0;
-  {
-#pragma clang fp contract(off)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float gr = g[i] * gscale;
-      m[i] = m[i] * h.beta1 + gr * h.keep1;
-      v[i] = v[i] * h.beta2 + gr * h.keep2 * gr;
-      big_m = max(big_m, __float_as_uint(m[i]) & 0x7fffffffu);
-      big_v = max(big_v, __float_as_uint(v[i]) & 0x7fffffffu);
-    }
-  }
-  const float wd = t.decay * h.wd;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] -= h.lr * (m[i] * h.fix1 / (sqrtf(v[i] * h.fix2) + h.eps) + wd * w[i]);
-  store4<false>(weights, at, t.n, w);
-  if (PARAM16) store4<true>(t.param, at, t.n, w);
-  if (!CODES) {
-    store4<false>(t.m, at, t.n, m);
-    store4<false>(t.v, at, t.n, v);
-    return;
-  }
-  const float am = scale_of(wave_max(big_m)), av = scale_of(wave_max(big_v));
-  const uint32_t r0 = mix(((t.first_block + (unsigned)block) * 64u + lane) * 0x9E3779B1u + h.key);
-  const uint32_t times[4] = {0x3C6EF373u, 0xA54FF53Bu, 0x510E527Fu, 0x9B05688Du};
+__device__ __forceinline__ void decode(uint32_t mc, uint32_t vc, float am, float av, float (&m)[4], float (&v)[4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    uint32_t r = r0 * times[i];
-    r ^= r >> 15;
-    const float um = ((r & 0xffffu) + 0.5f) * 0x1p-16f, uv = ((r >> 16) + 0.5f) * 0x1p-16f;
-    const float x = fabsf(m[i]);
-    float cm = 0.f, cv = 0.f;
-    if (am > 0.f) cm = copysignf(code_between(x, am, 127.f * sqrtf(x / am), 127.f, um, m_value), m[i]);
-    if (av > 0.f) {
-      cv = code_between(v[i], av, 255.f * sqrtf(sqrtf(v[i] / av)), 255.f, uv, v_value);
-      if (v[i] > 0.f) cv = fmaxf(cv, 1.f);
+    const float cm = (float)((int)(mc << (24 - 8 * i)) >> 24);
+    m[i] = copysignf(m_value(cm, am), cm);
+    v[i] = v_value((float)(vc >> (8 * i) & 255u), av);
+  }
+}
+
+// What a lane holds of a block.
+template <bool PARAM16, bool GRAD16, bool CODES>
+struct AdamwBlock {
+  typename Four<GRAD16>::Vec g;
+  f32x4_f32 w, m, v;
+  uint32_t mc, vc;
+  float am, av;
+
+  // left: how many of the lane's four values the tensor has (4 or more: all); FULL: all lanes' are there
+  template <bool FULL>
+  __device__ __forceinline__ void load(const AdamwTensor& t, long long block, long long at, long long left) {
+    const void* const weights = PARAM16 ? (const void*)t.master : t.param;
+    if (FULL) {
+      g = Four<GRAD16>::load(t.grad, at);
+      w = Four<false>::load(weights, at);
+    } else {
+      g = Four<GRAD16>::load_some(t.grad, at, left);
+      w = Four<false>::load_some(weights, at, left);
     }
-    if (at + i < t.n) {
-      static_cast<int8_t*>(t.m)[at + i] = (int8_t)cm;
-      static_cast<uint8_t*>(t.v)[at + i] = (uint8_t)cv;
+    if (CODES) {
+      mc = FULL ? load_codes(t.m, at) : load_codes_some(t.m, at, left);
+      vc = FULL ? load_codes(t.v, at) : load_codes_some(t.v, at, left);
+      am = t.m_scale[block];
+      av = t.v_scale[block];
+    } else {
+      m = FULL ? Four<false>::load(t.m, at) : Four<false>::load_some(t.m, at, left);
+      v = FULL ? Four<false>::load(t.v, at) : Four<false>::load_some(t.v, at, left);
     }
   }
-  if (lane == 0) {
-    t.m_scale[block] = am;
-    t.v_scale[block] = av;
+
+  template <bool FULL>
+  __device__ __forceinline__ void step(const AdamwTensor& t, const AdamwScalars& h, float gscale, float wd, long long block, long long at,
+                                       long long left, int lane) {
+    float g_[4], w_[4], m_[4], v_[4], root[4];
+    Four<GRAD16>::unpack(g, g_);
+    Four<false>::unpack(w, w_);
+    if (CODES) {
+      decode(mc, vc, am, av, m_, v_);
+    } else {
+      Four<false>::unpack(m, m_);
+      Four<false>::unpack(v, v_);
+    }
+    uint32_t big_m = 0, big_v = 0;
+    {
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float gr = g_[i] * gscale;
+        m_[i] = m_[i] * h.beta1 + gr * h.keep1;
+        v_[i] = v_[i] * h.beta2 + gr * h.keep2 * gr;
+        if (CODES) {
+          big_m = max(big_m, __float_as_uint(m_[i]) & 0x7fffffffu);
+          big_v = max(big_v, __float_as_uint(v_[i]) & 0x7fffffffu);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (CODES) {   // bound by arithmetic: the instructions for root and reciprocal, each within one unit in the last place
+        root[i] = __builtin_amdgcn_sqrtf(v_[i]);
+        w_[i] -= h.lr * (m_[i] * h.fix1 * __builtin_amdgcn_rcpf(fmaf(root[i], h.root2, h.eps)) + wd * w_[i]);
+      } else {
+        w_[i] -= h.lr * (m_[i] * h.fix1 / (sqrtf(v_[i] * h.fix2) + h.eps) + wd * w_[i]);
+      }
+    }
+    if (FULL) {
+      Four<false>::store(PARAM16 ? (void*)t.master : t.param, at, w_);
+      if (PARAM16) Four<true>::store(t.param, at, w_);
+      if (!CODES) {
+        Four<false>::store(t.m, at, m_);
+        Four<false>::store(t.v, at, v_);
+      }
+    } else {
+      Four<false>::store_some(PARAM16 ? (void*)t.master : t.param, at, left, w_);
+      if (PARAM16) Four<true>::store_some(t.param, at, left, w_);
+      if (!CODES) {
+        Four<false>::store_some(t.m, at, left, m_);
+        Four<false>::store_some(t.v, at, left, v_);
+      }
+    }
+    if (!CODES) return;
+    const float am_ = scale_of(wave_max(big_m)), av_ = scale_of(wave_max(big_v));
+    // the guesses: 127 sqrt(|m| / am), and 255 sqrt(root / sqrt(av)), as root is sqrt(v)
+    const float to_m = 1.f / am_, to_v = 255.f * 255.f * __builtin_amdgcn_rsqf(av_);
+    const uint32_t r0 = mix(((t.first_block + (unsigned)block) * 64u + lane) * 0x9E3779B1u + h.key);
+    const uint32_t times[4] = {0x3C6EF373u, 0xA54FF53Bu, 0x510E527Fu, 0x9B05688Du};
+    uint32_t mc_ = 0, vc_ = 0;
+    if (am_ > 0.f) {   // the same in all lanes
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t r = r0 * times[i];
+        r ^= r >> 15;
+        const float u = fmaf((float)(r & 0xffffu), 0x1p-16f, 0x1p-17f), x = fabsf(m_[i]);
+        const int c = (int)code_between(x, am_, 127.f * __builtin_amdgcn_sqrtf(x * to_m), 127.f, u, m_value);
+        mc_ |= ((uint32_t)(m_[i] < 0.f ? -c : c) & 255u) << (8 * i);
+      }
+    }
+    if (av_ > 0.f) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t r = r0 * times[i];
+        r ^= r >> 15;
+        const float u = fmaf((float)(r >> 16), 0x1p-16f, 0x1p-17f);
+        const float c = code_between(v_[i], av_, __builtin_amdgcn_sqrtf(root[i] * to_v), 255.f, u, v_value);
+        vc_ = __builtin_amdgcn_cvt_pk_u8_f32(v_[i] > 0.f ? fmaxf(c, 1.f) : 0.f, i, vc_);
+      }
+    }
+    if (FULL) {
+      store_codes(t.m, at, mc_);
+      store_codes(t.v, at, vc_);
+    } else {
+      store_codes_some(t.m, at, left, mc_);
+      store_codes_some(t.v, at, left, vc_);
+    }
+    if (lane == 0) {
+      t.m_scale[block] = am_;
+      t.v_scale[block] = av_;
+    }
+  }
+};
+
+constexpr int ADAMW_WAVES = ADAMW_THREADS / 64, ADAMW_ROUNDS = ADAMW_CHUNK / ADAMW_BLOCK / ADAMW_WAVES;
+
+// A wavefront's blocks of a chunk, all loads first.
+template <bool PARAM16, bool GRAD16, bool CODES>
+__device__ __forceinline__ void adamw_chunk(const AdamwTensor& t, const AdamwScalars& h, float gscale, long long first, int lane) {
+  const float wd = t.decay * h.wd;
+  if ((first + ADAMW_WAVES * (ADAMW_ROUNDS - 1) + 1) * ADAMW_BLOCK <= t.n) {
+    AdamwBlock<PARAM16, GRAD16, CODES> b[ADAMW_ROUNDS];
+#pragma unroll
+    for (int k = 0; k < ADAMW_ROUNDS; ++k) b[k].template load<true>(t, first + k * ADAMW_WAVES, (first + k * ADAMW_WAVES) * ADAMW_BLOCK + lane * 4, 4);
+#pragma unroll
+    for (int k = 0; k < ADAMW_ROUNDS; ++k)
+      b[k].template step<true>(t, h, gscale, wd, first + k * ADAMW_WAVES, (first + k * ADAMW_WAVES) * ADAMW_BLOCK + lane * 4, 4, lane);
+    return;
+  }
+  for (int k = 0; k < ADAMW_ROUNDS; ++k) {
+    const long long block = first + k * ADAMW_WAVES, at = block * ADAMW_BLOCK + lane * 4;
+    if (block * ADAMW_BLOCK >= t.n) return;
+    AdamwBlock<PARAM16, GRAD16, CODES> b;
+    b.template load<false>(t, block, at, t.n - at);
+    b.template step<false>(t, h, gscale, wd, block, at, t.n - at, lane);
   }
 }
 
@@ -188,21 +324,18 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwTensor*
                                                               const float* __restrict__ grad_scale) {
   const AdamwChunk c = chunks[blockIdx.x];
   const AdamwTensor t = tensors[c.tensor];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float gscale = grad_scale ? h.gscale * grad_scale[0] : h.gscale;
-  for (int k = wave; k < ADAMW_CHUNK / ADAMW_BLOCK; k += ADAMW_THREADS / 64) {
-    const long long block = (long long)c.at * (ADAMW_CHUNK / ADAMW_BLOCK) + k;
-    if (block * ADAMW_BLOCK >= t.n) return;
-    switch (t.kind) {
-      case 0: adamw_block<false, false, false>(t, h, gscale, block, lane); break;
-      case 1: adamw_block<true, false, false>(t, h, gscale, block, lane); break;
-      case 2: adamw_block<false, true, false>(t, h, gscale, block, lane); break;
-      case 3: adamw_block<true, true, false>(t, h, gscale, block, lane); break;
-      case 4: adamw_block<false, false, true>(t, h, gscale, block, lane); break;
-      case 5: adamw_block<true, false, true>(t, h, gscale, block, lane); break;
-      case 6: adamw_block<false, true, true>(t, h, gscale, block, lane); break;
-      default: adamw_block<true, true, true>(t, h, gscale, block, lane);
-    }
+  const long long first = (long long)c.at * (ADAMW_CHUNK / ADAMW_BLOCK) + wave;
+  switch (t.kind) {
+    case 0: adamw_chunk<false, false, false>(t, h, gscale, first, lane); break;
+    case 1: adamw_chunk<true, false, false>(t, h, gscale, first, lane); break;
+    case 2: adamw_chunk<false, true, false>(t, h, gscale, first, lane); break;
+    case 3: adamw_chunk<true, true, false>(t, h, gscale, first, lane); break;
+    case 4: adamw_chunk<false, false, true>(t, h, gscale, first, lane); break;
+    case 5: adamw_chunk<true, false, true>(t, h, gscale, first, lane); break;
+    case 6: adamw_chunk<false, true, true>(t, h, gscale, first, lane); break;
+    default: adamw_chunk<true, true, true>(t, h, gscale, first, lane);
   }
 }
 
@@ -211,28 +344,28 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_decode_kernel(const Adamw
                                                                      float* __restrict__ m_out, float* __restrict__ v_out) {
   const AdamwChunk c = chunks[blockIdx.x];
   const AdamwTensor t = tensors[c.tensor];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int k = wave; k < ADAMW_CHUNK / ADAMW_BLOCK; k += ADAMW_THREADS / 64) {
-    const long long block = (long long)c.at * (ADAMW_CHUNK / ADAMW_BLOCK) + k;
-    const long long at = block * ADAMW_BLOCK + lane * 4;
-    if (block * ADAMW_BLOCK >= t.n) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+  for (int k = 0; k < ADAMW_ROUNDS; ++k) {
+    const long long block = (long long)c.at * (ADAMW_CHUNK / ADAMW_BLOCK) + k * ADAMW_WAVES + wave;
+    const long long at = block * ADAMW_BLOCK + lane * 4, to = (long long)t.first_block * ADAMW_BLOCK + at, left = t.n - at;
+    if (left <= 0) return;
     float m[4], v[4];
     if (t.kind & 4) {
-      const float am = t.m_scale[block], av = t.v_scale[block];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float cm = at + i < t.n ? (float)static_cast<const int8_t*>(t.m)[at + i] : 0.f;
-        const float cv = at + i < t.n ? (float)static_cast<const uint8_t*>(t.v)[at + i] : 0.f;
-        m[i] = copysignf(m_value(cm, am), cm);
-        v[i] = v_value(cv, av);
-      }
+      const bool all = left >= 4;
+      decode(all ? load_codes(t.m, at) : load_codes_some(t.m, at, left), all ? load_codes(t.v, at) : load_codes_some(t.v, at, left),
+             t.m_scale[block], t.v_scale[block], m, v);
     } else {
-      load4<false>(t.m, at, t.n, m);
-      load4<false>(t.v, at, t.n, v);
+      Four<false>::unpack(Four<false>::load_some(t.m, at, left), m);
+      Four<false>::unpack(Four<false>::load_some(t.v, at, left), v);
     }
-    const long long to = (long long)t.first_block * ADAMW_BLOCK;
-    store4<false>(m_out + to, at, t.n, m);
-    store4<false>(v_out + to, at, t.n, v);
+    if (left >= 4) {
+      Four<false>::store(m_out, to, m);
+      Four<false>::store(v_out, to, v);
+    } else {
+      Four<false>::store_some(m_out, to, left, m);
+      Four<false>::store_some(v_out, to, left, v);
+    }
   }
 }
 
@@ -359,6 +492,7 @@ extern "C" int symi_adamw_step(const symi_ctx* ctx, const symi_adamw* opt, const
   h.eps = hp->eps; h.wd = hp->weight_decay; h.gscale = hp->grad_scale;
   h.fix1 = (float)(1.0 / (1.0 - pow((double)hp->beta1, hp->step)));
   h.fix2 = (float)(1.0 / (1.0 - pow((double)hp->beta2, hp->step)));
+  h.root2 = (float)sqrt(1.0 / (1.0 - pow((double)hp->beta2, hp->step)));
   h.key = mix(mix(seed) + (uint32_t)hp->step);
   hipStream_t st = as_stream(stream);
   SYMI_TIMED(ctx, K_ADAMW, st, (adamw_kernel<<<(unsigned)opt->chunks, ADAMW_THREADS, 0, st>>>(opt->tensors, opt->list, h, grad_scale)));
