@@ -101,15 +101,15 @@ struct Token {
   float gain, kl, slope;
   bool clipped;
 };
-__device__ __forceinline__ Token token_loss(const PolicyScalars& p, float logp, float old, bool has_ref, float ref, float A) {
+__device__ __forceinline__ Token token_loss(const PolicyScalars& p, double logp, float old, bool has_ref, float ref, float A) {
   Token k;
-  const float r = expf(logp - old);
+  const float r = expf((float)(logp - old));
   k.clipped = (A > 0.f && r > 1.f + p.clip_high) || (A < 0.f && r < 1.f - p.clip_low);
   k.gain = -A * (k.clipped ? (A > 0.f ? 1.f + p.clip_high : 1.f - p.clip_low) : r);
   k.slope = k.clipped ? 0.f : -A * r;
   k.kl = 0.f;
   if (has_ref) {
-    const float far = ref - logp, e = expm1f(far);
+    const float far = (float)(ref - logp), e = expm1f(far);
     // e^x - x - 1 loses all digits near 0, where it is x^2 / 2 + x^3 / 6 + ...
     k.kl = fabsf(far) < 0.125f ? far * far * (0.5f + far * (1.f / 6 + far * (1.f / 24 + far * (1.f / 120 + far * (1.f / 720))))) : e - far;
     k.slope -= p.kl_coef * e;
@@ -246,8 +246,12 @@ __device__ __forceinline__ Slope slope_of(const PolicyScalars& p, float w, float
 __device__ __forceinline__ float4 terms_of(const PolicyScalars& p, float w, const Token& k) {
   return float4{w * (k.gain + p.kl_coef * k.kl), w * k.gain, w * k.kl, k.clipped ? w : 0.f};
 }
-__device__ __forceinline__ float logp_of(const PolicyScalars& p, float za, float m, float s) {
-  return fmaf(za, p.c, -m) * 0.693147180559945309f - logf(s);
+// In 64 bits, as a ratio exp(logp - logp_old) has the absolute error of logp, and 32 bits leave 5e-7 to a logp of -10; the
+// logarithm is that of a number below 1 in 32 bits (off by 3e-8) and a multiple of ln 2.
+__device__ __forceinline__ double logp_of(const PolicyScalars& p, float za, float m, float s) {
+  int k;
+  const float f = frexpf(s, &k);
+  return (fma((double)za, (double)p.c, -(double)m) - k) * 0.693147180559945309 - (double)logf(f);
 }
 
 // A workgroup of THREADS takes a row.  What fits is read once and stays in registers from the logits to their gradient; of a
@@ -288,8 +292,8 @@ __global__ __launch_bounds__(THREADS) void policy_kernel(PolicyArgs g) {
   row.fetch(last, end);
   row.take(last, end, m, s, &chosen);
   join_threads<THREADS>(m, s);
-  const float lp = logp_of(g.p, chosen, m, s);
-  if (tid == 0) g.logp[t] = lp;
+  const double lp = logp_of(g.p, chosen, m, s);
+  if (tid == 0) g.logp[t] = (float)lp;
   if (!g.terms) return;
   const Token k = token_loss(g.p, lp, old, g.logp_ref != nullptr, ref, A);
   if (tid == 0) g.terms[t] = terms_of(g.p, w, k);
@@ -375,7 +379,7 @@ __global__ __launch_bounds__(SUM_SPLIT_THREADS) void policy_apply_kernel(PolicyA
     double sum[4] = {};
     for (int t = threadIdx.x; t < T; t += SUM_SPLIT_THREADS) {
       const float w = g.weight[t];
-      float lp = 0.f;
+      double lp = 0.;
       if (w != 0.f && (unsigned)g.action[t] < (unsigned)g.V) {
         join_waves<WAVES>(m, s, [&](int k) { return parts.ms[(long long)t * WAVES + k]; });
         lp = logp_of(g.p, parts.chosen[t], m, s);
@@ -383,7 +387,7 @@ __global__ __launch_bounds__(SUM_SPLIT_THREADS) void policy_apply_kernel(PolicyA
         const float4 x = terms_of(g.p, w, k);
         sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
       }
-      g.logp[t] = lp;
+      g.logp[t] = (float)lp;
     }
     add_terms<SUM_SPLIT_THREADS>(sum, stats);
     return;
@@ -406,7 +410,7 @@ __global__ __launch_bounds__(SUM_SPLIT_THREADS) void policy_apply_kernel(PolicyA
   }
   row.fetch(0, end);
   join_waves<WAVES>(m, s, [&](int k) { return parts.ms[t * WAVES + k]; });
-  const float lp = logp_of(g.p, parts.chosen[t], m, s);
+  const double lp = logp_of(g.p, parts.chosen[t], m, s);
   const Token k = token_loss(g.p, lp, g.logp_old[t], g.logp_ref != nullptr, g.logp_ref ? g.logp_ref[t] : 0.f, g.advantage[t]);
   const Slope d = slope_of(g.p, w, k.slope, m, s);
   for (int q0 = 0;;) {
