@@ -38,10 +38,17 @@ struct AdamwTensor {   // on the device
   float decay;
   int kind;               // bit 0: bf16 param, 1: bf16 gradient, 2: 8-bit states
 };
+// Work of a workgroup: ADAMW_CHUNK values (four blocks a wavefront), or, of what a tensor has behind its last whole chunk, one block
+// a wavefront: a small tensor or a ragged end is then as many workgroups and no chain of rounds.
 struct AdamwChunk {
   int tensor;
-  unsigned at;   // of the tensor's chunks
+  unsigned block;   // the first one; WHOLE: a whole chunk
 };
+constexpr unsigned WHOLE = 0x80000000u;
+// So few values in all that none of it is cut into whole chunks, as their rounds would leave units idle.  us, whole chunks : one
+// block a wavefront, 8-bit states: 0.2 million values 7.2 : 4.8, 1.6 million 12.7 : 9.6, 6.3 million 26.1 : 25.2, 12.5 million 40.8 :
+// 43.9, 20.9 million 72.9 : 91.9; 32-bit ones 4.4 : 3.9, 9.9 : 9.4, 27.3 : 28.0, 70.5 : 67.0.
+constexpr long long FINE_BELOW = 1LL << 23;
 
 struct AdamwScalars {
   float lr, beta1, keep1, beta2, keep2, eps, wd, gscale, fix1, fix2, root2;
@@ -299,9 +306,9 @@ constexpr int ADAMW_WAVES = ADAMW_THREADS / 64, ADAMW_ROUNDS = ADAMW_CHUNK / ADA
 
 // A wavefront's blocks of a chunk, all loads first.
 template <bool PARAM16, bool GRAD16, bool CODES>
-__device__ __forceinline__ void adamw_chunk(const AdamwTensor& t, const AdamwScalars& h, float gscale, long long first, int lane) {
+__device__ __forceinline__ void adamw_chunk(const AdamwTensor& t, const AdamwScalars& h, float gscale, bool whole, long long first, int lane) {
   const float wd = t.decay * h.wd;
-  if ((first + ADAMW_WAVES * (ADAMW_ROUNDS - 1) + 1) * ADAMW_BLOCK <= t.n) {
+  if (whole) {
     AdamwBlock<PARAM16, GRAD16, CODES> b[ADAMW_ROUNDS];
 #pragma unroll
     for (int k = 0; k < ADAMW_ROUNDS; ++k) b[k].template load<true>(t, first + k * ADAMW_WAVES, (first + k * ADAMW_WAVES) * ADAMW_BLOCK + lane * 4, 4);
@@ -310,12 +317,15 @@ __device__ __forceinline__ void adamw_chunk(const AdamwTensor& t, const AdamwSca
       b[k].template step<true>(t, h, gscale, wd, first + k * ADAMW_WAVES, (first + k * ADAMW_WAVES) * ADAMW_BLOCK + lane * 4, 4, lane);
     return;
   }
-  for (int k = 0; k < ADAMW_ROUNDS; ++k) {
-    const long long block = first + k * ADAMW_WAVES, at = block * ADAMW_BLOCK + lane * 4;
-    if (block * ADAMW_BLOCK >= t.n) return;
-    AdamwBlock<PARAM16, GRAD16, CODES> b;
-    b.template load<false>(t, block, at, t.n - at);
-    b.template step<false>(t, h, gscale, wd, block, at, t.n - at, lane);
+  const long long at = first * ADAMW_BLOCK + lane * 4;
+  if (first * ADAMW_BLOCK >= t.n) return;
+  AdamwBlock<PARAM16, GRAD16, CODES> b;
+  if ((first + 1) * ADAMW_BLOCK <= t.n) {
+    b.template load<true>(t, first, at, 4);
+    b.template step<true>(t, h, gscale, wd, first, at, 4, lane);
+  } else {
+    b.template load<false>(t, first, at, t.n - at);
+    b.template step<false>(t, h, gscale, wd, first, at, t.n - at, lane);
   }
 }
 
@@ -326,16 +336,17 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwTensor*
   const AdamwTensor t = tensors[c.tensor];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float gscale = grad_scale ? h.gscale * grad_scale[0] : h.gscale;
-  const long long first = (long long)c.at * (ADAMW_CHUNK / ADAMW_BLOCK) + wave;
+  const long long first = (c.block & ~WHOLE) + wave;
+  const bool whole = c.block & WHOLE;
   switch (t.kind) {
-    case 0: adamw_chunk<false, false, false>(t, h, gscale, first, lane); break;
-    case 1: adamw_chunk<true, false, false>(t, h, gscale, first, lane); break;
-    case 2: adamw_chunk<false, true, false>(t, h, gscale, first, lane); break;
-    case 3: adamw_chunk<true, true, false>(t, h, gscale, first, lane); break;
-    case 4: adamw_chunk<false, false, true>(t, h, gscale, first, lane); break;
-    case 5: adamw_chunk<true, false, true>(t, h, gscale, first, lane); break;
-    case 6: adamw_chunk<false, true, true>(t, h, gscale, first, lane); break;
-    default: adamw_chunk<true, true, true>(t, h, gscale, first, lane);
+    case 0: adamw_chunk<false, false, false>(t, h, gscale, whole, first, lane); break;
+    case 1: adamw_chunk<true, false, false>(t, h, gscale, whole, first, lane); break;
+    case 2: adamw_chunk<false, true, false>(t, h, gscale, whole, first, lane); break;
+    case 3: adamw_chunk<true, true, false>(t, h, gscale, whole, first, lane); break;
+    case 4: adamw_chunk<false, false, true>(t, h, gscale, whole, first, lane); break;
+    case 5: adamw_chunk<true, false, true>(t, h, gscale, whole, first, lane); break;
+    case 6: adamw_chunk<false, true, true>(t, h, gscale, whole, first, lane); break;
+    default: adamw_chunk<true, true, true>(t, h, gscale, whole, first, lane);
   }
 }
 
@@ -347,7 +358,8 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_decode_kernel(const Adamw
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
   for (int k = 0; k < ADAMW_ROUNDS; ++k) {
-    const long long block = (long long)c.at * (ADAMW_CHUNK / ADAMW_BLOCK) + k * ADAMW_WAVES + wave;
+    if (k && !(c.block & WHOLE)) return;
+    const long long block = (c.block & ~WHOLE) + k * ADAMW_WAVES + wave;
     const long long at = block * ADAMW_BLOCK + lane * 4, to = (long long)t.first_block * ADAMW_BLOCK + at, left = t.n - at;
     if (left <= 0) return;
     float m[4], v[4];
@@ -398,7 +410,9 @@ extern "C" int symi_adamw_create(const symi_adamw_tensor* tensors, int count, sy
   try {
     std::vector<AdamwTensor> list;
     std::vector<AdamwChunk> chunks;
-    long long blocks = 0;
+    long long blocks = 0, all = 0;
+    for (int i = 0; i < count; ++i) all += tensors[i].n > 0 && tensors[i].n < 1LL << 36 ? tensors[i].n : 0;
+    const bool fine = all < FINE_BELOW;
     for (int i = 0; i < count; ++i) {
       const symi_adamw_tensor& s = tensors[i];
       const auto bad = [&](bool cond, const char* msg) {
@@ -422,10 +436,12 @@ extern "C" int symi_adamw_create(const symi_adamw_tensor* tensors, int count, sy
       }
       list.push_back({s.param, s.master, s.grad, s.m, s.v, s.m_scale, s.v_scale, s.n, (unsigned)blocks, s.decay,
                       (s.param_dtype == SYMI_BF16) | (s.grad_dtype == SYMI_BF16) << 1 | (s.state_bits == 8) << 2});
-      for (long long c = 0; c * ADAMW_CHUNK < s.n; ++c) chunks.push_back({(int)list.size() - 1, (unsigned)c});
+      long long at = 0;
+      for (; !fine && at + ADAMW_CHUNK <= s.n; at += ADAMW_CHUNK) chunks.push_back({(int)list.size() - 1, (unsigned)(at / ADAMW_BLOCK) | WHOLE});
+      for (; at < s.n; at += ADAMW_WAVES * ADAMW_BLOCK) chunks.push_back({(int)list.size() - 1, (unsigned)(at / ADAMW_BLOCK)});
       blocks += mine;
       if (chunks.size() >= 1u << 24) {   // a workgroup each; the threads of a launch end at 2^32
-        set_error("%s: more than 2^24 - 1 chunks of %d values", who, ADAMW_CHUNK);
+        set_error("%s: more than 2^24 - 1 chunks of up to %d values", who, ADAMW_CHUNK);
         return SYMI_EUNSUPPORTED;
       }
     }
