@@ -32,30 +32,11 @@ template <bool BF16> struct Piece {
     return __builtin_bit_cast(Raw, ONCE ? __builtin_nontemporal_load(q) : *q);
   }
   static __device__ __forceinline__ void store(Elem* p, Raw r) { *reinterpret_cast<Vec*>(p) = __builtin_bit_cast(Vec, r); }
-  // the first n of its values, the others -inf
-  static __device__ __forceinline__ Raw load_some(const Elem* p, int n) {
-    uint32_t x[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (BF16) {
-        const uint32_t lo = 2 * i < n ? p[2 * i] : 0xff80u, hi = 2 * i + 1 < n ? p[2 * i + 1] : 0xff80u;
-        x[i] = lo | hi << 16;
-      } else {
-        x[i] = __float_as_uint(i < n ? p[i] : -INFINITY);
-      }
-    }
-    return Raw{x[0], x[1], x[2], x[3]};
+  static __device__ __forceinline__ float value(Elem x) {
+    if constexpr (BF16) return bf16_to_f32(x); else return x;
   }
-  static __device__ __forceinline__ void store_some(Elem* p, Raw r, int n) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (BF16) {
-        if (2 * i < n) p[2 * i] = (uint16_t)r[i];
-        if (2 * i + 1 < n) p[2 * i + 1] = (uint16_t)(r[i] >> 16);
-      } else if (i < n) {
-        p[i] = __uint_as_float(r[i]);
-      }
-    }
+  static __device__ __forceinline__ Elem element(float x) {
+    if constexpr (BF16) return f32_to_bf16(x); else return x;
   }
   static __device__ __forceinline__ void unpack(Raw r, float (&x)[N]) {
 #pragma unroll
@@ -134,76 +115,102 @@ struct Row {
   using P = Piece<BF16>;
   using Elem = typename P::Elem;
   static constexpr int N = P::N, STEP = NV * THREADS;
-  const Elem* z;
-  int V, whole, a, tid;   // whole: pieces that lie in the vocabulary; a: the chosen token; tid: of THREADS
-  float c;
+  // Pieces begin at multiples of 16 bytes, wherever the row does (8192 rows of 4493 bf16, seven in eight of them unaligned: 46 us
+  // with pieces that begin with the row, against 38 for rows of 4496).  The up to seven logits before the first piece
+  // and behind the last one are the edge, one of them each of the threads below 16.
+  const Elem* z;       // of the first piece
+  int end, q, j;       // pieces; the chosen token's piece and place in it (or no piece)
+  int V, head, tid, token;
+  float c, edge;
   typename P::Raw r[NV];
 
-  __device__ __forceinline__ Row(const PolicyArgs& g, long long t, int tid)
-      : z(static_cast<const Elem*>(g.logits) + t * g.ld), V(g.V), whole(g.V / N), a(g.action[t]), tid(tid), c(g.p.c) {}
-
-  // the pieces q0 + tid, q0 + THREADS + tid, ... below `end`
-  __device__ __forceinline__ void fetch(int q0, int end) {
+  __device__ __forceinline__ Row(const PolicyArgs& g, long long t, int token, int tid) : V(g.V), tid(tid), token(token), c(g.p.c) {
+    const Elem* const row = static_cast<const Elem*>(g.logits) + t * g.ld;
+    head = min(g.V, (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) % 16 / sizeof(Elem)));
+    end = (g.V - head) / N;
+    z = row + head;
+    const int tail = head + end * N;
+    q = token >= head && token < tail ? (token - head) / N : -1;
+    j = (token - head) % N;
+    edge = -INFINITY;
+  }
+  // the column of the thread's edge logit, or -1
+  __device__ __forceinline__ int edge_column() const {
+    if (tid < 8) return tid < head ? tid : -1;
+    const int at = head + end * N + tid - 8;
+    return tid < 16 && at < V ? at : -1;
+  }
+  // requested last, after the first pieces
+  __device__ __forceinline__ void fetch_edge() {
+    const int e = edge_column();
+    if (e >= 0) edge = P::value(z[e - head]);
+  }
+  __device__ __forceinline__ void take_edge(float& m, float& s, float* chosen) {
+    const int e = edge_column();
+    if (e < 0) return;
+    join(m, s, edge * c, 1.f);
+    if (e == token) *chosen = edge;
+  }
+  __device__ __forceinline__ void give_edge(Elem* dz, float u, float minus, float ref) {
+    const int e = edge_column();
+    if (e >= 0) dz[e] = P::element(minus * exp2_(fmaf(edge, c, -ref)) + (e == token ? u : 0.f));
+  }
+  // the pieces q0 + tid, q0 + THREADS + tid, ... below `stop`
+  __device__ __forceinline__ void fetch(int q0, int stop) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int q = q0 + i * THREADS + tid;
+      const int at = q0 + i * THREADS + tid;
       r[i] = P::none();
-      if (q < end) {
-        if (q < whole) r[i] = P::template load<ONCE>(z + (long long)q * N);
-        else r[i] = P::load_some(z + (long long)q * N, V - whole * N);
-      }
+      if (at < stop) r[i] = P::template load<ONCE>(z + (long long)at * N);
     }
   }
   // adds what is held to the thread's (m, s); the chosen token's logit goes to *chosen
-  __device__ __forceinline__ void take(int q0, int end, float& m, float& s, float* chosen) {
+  __device__ __forceinline__ void take(int q0, int stop, float& m, float& s, float* chosen) {
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      if (q0 + i * THREADS >= end) continue;
+      if (q0 + i * THREADS >= stop) continue;
       float x[N];
       P::unpack(r[i], x);
 #pragma unroll
-      for (int j = 0; j < N; ++j) top = fmaxf(top, x[j]);
-      if (q0 + i * THREADS + tid == a / N && a / N < end) {
+      for (int k = 0; k < N; ++k) top = fmaxf(top, x[k]);
+      if (q0 + i * THREADS + tid == q && q < stop) {
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (j == a % N) *chosen = x[j];
+        for (int k = 0; k < N; ++k)
+          if (k == j) *chosen = x[k];
       }
     }
     top *= c;
-    const float base = fmaxf(m, top), from = base == -INFINITY ? 0.f : base;   // nothing but -inf so far
-    s *= exp2_(m - from);
+    const float base = fmaxf(m, top), ref = base == -INFINITY ? 0.f : base;   // nothing but -inf so far
+    s *= exp2_(m - ref);
     m = base;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      if (q0 + i * THREADS >= end) continue;
+      if (q0 + i * THREADS >= stop) continue;
       float x[N];
       forget(r[i]);
       P::unpack(r[i], x);
 #pragma unroll
-      for (int j = 0; j < N; ++j) s += exp2_(fmaf(x[j], c, -from));
+      for (int k = 0; k < N; ++k) s += exp2_(fmaf(x[k], c, -ref));
     }
   }
-  // writes the gradient of what is held
-  __device__ __forceinline__ void give(int q0, int end, Elem* dz, float u, float minus, float from) {
+  // writes the gradient of what is held; dz: of the row's first logit
+  __device__ __forceinline__ void give(int q0, int stop, Elem* dz, float u, float minus, float ref) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int q = q0 + i * THREADS + tid;
-      if (q0 + i * THREADS >= end) continue;
+      const int at = q0 + i * THREADS + tid;
+      if (q0 + i * THREADS >= stop) continue;
       float x[N];
       forget(r[i]);
       P::unpack(r[i], x);
 #pragma unroll
-      for (int j = 0; j < N; ++j) x[j] = minus * exp2_(fmaf(x[j], c, -from));
-      if (q == a / N) {
+      for (int k = 0; k < N; ++k) x[k] = minus * exp2_(fmaf(x[k], c, -ref));
+      if (at == q) {
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (j == a % N) x[j] += u;
+        for (int k = 0; k < N; ++k)
+          if (k == j) x[k] += u;
       }
-      if (q < end) {
-        if (q < whole) P::store(dz + (long long)q * N, P::pack(x));
-        else P::store_some(dz + (long long)q * N, P::pack(x), V - whole * N);
-      }
+      if (at < stop) P::store(dz + head + (long long)at * N, P::pack(x));
     }
   }
 };
@@ -229,9 +236,15 @@ __device__ __forceinline__ void join_threads(float& m, float& s) {
   for (int k = 1; k < THREADS / 64; ++k) join(m, s, ms[k], ss[k]);
 }
 
-template <typename Elem>
-__device__ __forceinline__ void clear_row(Elem* dz, int from, int ld, int threads) {
-  for (int j = from + threadIdx.x; j < ld; j += threads) dz[j] = 0;
+// Zeros to p[0 .. n).
+template <bool BF16>
+__device__ __forceinline__ void clear(typename Piece<BF16>::Elem* p, int n, int tid, int threads) {
+  using P = Piece<BF16>;
+  const int head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) % 16 / sizeof(typename P::Elem)));
+  const int pieces = (n - head) / P::N, tail = head + pieces * P::N;
+  for (int j = tid; j < head; j += threads) p[j] = 0;
+  for (int q = tid; q < pieces; q += threads) P::store(p + head + (long long)q * P::N, typename P::Raw{0, 0, 0, 0});
+  for (int j = tail + tid; j < n; j += threads) p[j] = 0;
 }
 
 // The gradient of a logit is minus 2^(t - from), with u more for the chosen token.  2^24 moves from the factor into the
@@ -256,25 +269,23 @@ __device__ __forceinline__ double logp_of(const PolicyScalars& p, float za, floa
 
 // A workgroup of THREADS takes a row.  What fits is read once and stays in registers from the logits to their gradient; of a
 // longer row the last STEP pieces stay and the ones before them are read again.
+// Up to eight pieces a thread leave 64 registers: eight wavefronts a SIMD, two workgroups of 1024 a unit.
 template <bool BF16, bool GRAD, int THREADS, int NV>
-__global__ __launch_bounds__(THREADS) void policy_kernel(PolicyArgs g) {
+__global__ __launch_bounds__(THREADS, NV <= 8 ? 8 : 4) void policy_kernel(PolicyArgs g) {
   using R = Row<BF16, !GRAD, THREADS, NV>;
   __shared__ float chosen;
   const int tid = threadIdx.x;
   const long long t = blockIdx.x;
-  R row(g, t, tid);
+  const int token = g.action[t];
+  R row(g, t, token, tid);
   auto* const dz = static_cast<typename R::Elem*>(g.dlogits) + (GRAD ? t * g.ld : 0);
   const float w = g.weight ? g.weight[t] : 1.f;
-  if (w == 0.f || (unsigned)row.a >= (unsigned)g.V) {
+  if (w == 0.f || (unsigned)token >= (unsigned)g.V) {
     if (tid == 0) {
       g.logp[t] = 0.f;
       if (g.terms) g.terms[t] = float4{0.f, 0.f, 0.f, 0.f};
     }
-    if (GRAD) {
-      const typename R::P::Raw zero = {0, 0, 0, 0};
-      for (int q = tid; q < g.ld / R::N; q += THREADS) R::P::store(dz + (long long)q * R::N, zero);
-      clear_row(dz, g.ld / R::N * R::N, g.ld, THREADS);
-    }
+    if (GRAD) clear<BF16>(dz, g.ld, tid, THREADS);
     return;
   }
   float old = 0.f, ref = 0.f, A = 0.f;   // requested with the row
@@ -283,14 +294,16 @@ __global__ __launch_bounds__(THREADS) void policy_kernel(PolicyArgs g) {
     A = g.advantage[t];
     if (g.logp_ref) ref = g.logp_ref[t];
   }
-  const int end = (g.V + R::N - 1) / R::N, last = end > R::STEP ? end - R::STEP : 0;   // from `last` on pieces stay
+  const int end = row.end, last = end > R::STEP ? end - R::STEP : 0;   // from `last` on pieces stay
   float m = -INFINITY, s = 0.f;
   for (int q0 = 0; q0 < last; q0 += R::STEP) {
     row.fetch(q0, min(q0 + R::STEP, last));
     row.take(q0, min(q0 + R::STEP, last), m, s, &chosen);
   }
   row.fetch(last, end);
+  row.fetch_edge();
   row.take(last, end, m, s, &chosen);
+  row.take_edge(m, s, &chosen);
   join_threads<THREADS>(m, s);
   const double lp = logp_of(g.p, chosen, m, s);
   if (tid == 0) g.logp[t] = (float)lp;
@@ -300,17 +313,18 @@ __global__ __launch_bounds__(THREADS) void policy_kernel(PolicyArgs g) {
   if (!GRAD) return;
   const Slope d = slope_of(g.p, w, k.slope, m, s);
   row.give(last, end, dz, d.u, d.minus, d.from);
-  for (int q0 = 0; q0 < last; q0 += R::STEP) {
+  row.give_edge(dz, d.u, d.minus, d.from);
+  for (int q0 = (last - 1) / R::STEP * R::STEP; last && q0 >= 0; q0 -= R::STEP) {   // what was read last is the nearest
     row.fetch(q0, min(q0 + R::STEP, last));
     row.give(q0, min(q0 + R::STEP, last), dz, d.u, d.minus, d.from);
   }
-  clear_row(dz, g.V, g.ld, THREADS);
+  clear<BF16>(dz + g.V, g.ld - g.V, tid, THREADS);
 }
 
 // Few rows: every wavefront that policy_kernel would give a row is a workgroup of its own, in two launches.  The first
 // leaves each wavefront's (m, s) and the chosen logit; the second joins them, reads the logits again and writes their
 // gradient.  Which pieces a thread takes and how sums are joined is that of policy_kernel, so a row's bits do not
-// depend on the number of rows.  The first workgroup of the second launch takes the sums over the tokens.
+// depend on the number of rows (only on where it begins within 16 bytes).  The first workgroup of the second launch takes the sums over the tokens.
 constexpr int SUM_SPLIT_THREADS = 256;
 constexpr int PART_MAX = 16;         // wavefronts of a row
 constexpr int PART_ROWS_MAX = 256;   // rows of a batch that is split
@@ -326,16 +340,19 @@ __global__ __launch_bounds__(64) void policy_part_kernel(PolicyArgs g, Parts par
   constexpr int WAVES = THREADS / 64;
   const int wave = blockIdx.x % WAVES;
   const long long t = blockIdx.x / WAVES;
-  R row(g, t, wave * 64 + threadIdx.x);
-  if (g.weight[t] == 0.f || (unsigned)row.a >= (unsigned)g.V) return;
-  const int end = (g.V + R::N - 1) / R::N, last = end > R::STEP ? end - R::STEP : 0;
+  const int token = g.action[t];
+  R row(g, t, token, wave * 64 + threadIdx.x);
+  if (g.weight[t] == 0.f || (unsigned)token >= (unsigned)g.V) return;
+  const int end = row.end, last = end > R::STEP ? end - R::STEP : 0;
   float m = -INFINITY, s = 0.f;
   for (int q0 = 0; q0 < last; q0 += R::STEP) {
     row.fetch(q0, min(q0 + R::STEP, last));
     row.take(q0, min(q0 + R::STEP, last), m, s, parts.chosen + t);
   }
   row.fetch(last, end);
+  row.fetch_edge();
   row.take(last, end, m, s, parts.chosen + t);
+  row.take_edge(m, s, parts.chosen + t);
   join_wave(m, s);
   if (threadIdx.x == 0) parts.ms[t * WAVES + wave] = float2{m, s};
 }
@@ -395,24 +412,23 @@ __global__ __launch_bounds__(SUM_SPLIT_THREADS) void policy_apply_kernel(PolicyA
   if (threadIdx.x >= 64) return;   // the other workgroups are a wavefront
   const int wave = (blockIdx.x - 1) % WAVES;
   const long long t = (blockIdx.x - 1) / WAVES;
-  R row(g, t, wave * 64 + threadIdx.x);
+  const int token = g.action[t];
+  R row(g, t, token, wave * 64 + threadIdx.x);
   auto* const dz = static_cast<typename R::Elem*>(g.dlogits) + t * g.ld;
   const float w = g.weight[t];
-  const int end = (g.V + R::N - 1) / R::N;
-  if (wave == 0) clear_row(dz, g.V, g.ld, 64);
-  if (w == 0.f || (unsigned)row.a >= (unsigned)g.V) {
-    const typename R::P::Raw zero = {0, 0, 0, 0};
-    for (int q = row.tid; q < end; q += THREADS) {
-      if (q < row.whole) R::P::store(dz + (long long)q * R::N, zero);
-      else R::P::store_some(dz + (long long)q * R::N, zero, g.V - row.whole * R::N);
-    }
+  const int end = row.end;
+  if (w == 0.f || (unsigned)token >= (unsigned)g.V) {
+    clear<BF16>(dz, g.ld, row.tid, THREADS);
     return;
   }
+  if (wave == 0) clear<BF16>(dz + g.V, g.ld - g.V, row.tid, 64);
   row.fetch(0, end);
+  row.fetch_edge();
   join_waves<WAVES>(m, s, [&](int k) { return parts.ms[t * WAVES + k]; });
   const double lp = logp_of(g.p, parts.chosen[t], m, s);
   const Token k = token_loss(g.p, lp, g.logp_old[t], g.logp_ref != nullptr, g.logp_ref ? g.logp_ref[t] : 0.f, g.advantage[t]);
   const Slope d = slope_of(g.p, w, k.slope, m, s);
+  row.give_edge(dz, d.u, d.minus, d.from);
   for (int q0 = 0;;) {
     row.give(q0, end, dz, d.u, d.minus, d.from);
     if ((q0 += R::STEP) >= end) break;
@@ -458,24 +474,34 @@ static PolicyScalars scalars(const symi_policy* hp) {
   return {hp->clip_low, hp->clip_high, hp->kl_coef, hp->inv_temperature, hp->grad_scale, (float)(1.4426950408889634 * hp->inv_temperature)};
 }
 
+// The workgroup for a row with its gradient: f(THREADS, NV).  The smallest that holds the row comes first, with four to 16 pieces a
+// thread: us for 8192 rows in bf16, threads x pieces.  V = 3000: 64 x 8 31, 128 x 8 29, 256 x 4 34; 10001: 256 x 4 80, 256 x 8
+// 75, 512 x 4 85; 17010: 256 x 16 112, 512 x 8 113; 28000: 512 x 8 179, 512 x 12 176, 256 x 16 186; 45000: 512 x 12 285, 512 x 16
+// 274; 50001: 512 x 16 298, in two parts 10 % more.  Longer rows are read again in part, most of it from the memory-side cache,
+// and two workgroups a unit of 64 registers are faster than one of 128 that holds all (16384 of 131072, a quarter masked: 1567
+// against 1718).
+template <int X> using Int = std::integral_constant<int, X>;
+template <class F>
+static void by_length(int pieces, F f) {
+  if (pieces <= 64 * 4) f(Int<64>(), Int<4>());
+  else if (pieces <= 512) f(Int<128>(), Int<8>());
+  else if (pieces <= 256 * 4) f(Int<256>(), Int<4>());
+  else if (pieces <= 256 * 8) f(Int<256>(), Int<8>());
+  else if (pieces <= 3072) f(Int<512>(), Int<8>());
+  else if (pieces <= 512 * 9) f(Int<512>(), Int<12>());
+  else if (pieces <= 512 * 16) f(Int<512>(), Int<16>());
+  else f(Int<1024>(), Int<8>());
+}
+
 template <bool BF16>
 static void launch_rows(const symi_ctx* ctx, int kid, const PolicyArgs& g, hipStream_t st) {
   const int T = ctx->cfg.T, pieces = cdiv(g.V, Piece<BF16>::N);
 #define ROWS(GRAD, THREADS, NV) SYMI_TIMED(ctx, kid, st, (policy_kernel<BF16, GRAD, THREADS, NV><<<T, THREADS, 0, st>>>(g)))
-  // With the gradient: the smallest workgroup that holds the row, four pieces a thread first (bf16, 16384 rows of 2000: 64
-  // threads 41 us, 256 52, 1024 202; 8192 of 12000: 512 threads of four 84, 256 of eight 85), then up to 16 (8192 of
-  // 50001: 512 of 16 389, in two parts 413 - 450).  Longer rows are read again in part, most of it from the memory-side
-  // cache, and two workgroups a unit of 64 registers are faster than one of 128 that holds all (16384 of 131072, a quarter
-  // masked: 1567 against 1718).  Without it nothing has to stay: eight pieces of 256 threads at a time (8192 of 32000 81), on few
-  // rows 512 threads (300 of 131072: 21.7 against 25.5) or 1024 (16 of 128000: 10.3 against 11.0).
   if (g.dlogits) {
-    if (pieces <= 64 * 4) ROWS(true, 64, 4);
-    else if (pieces <= 256 * 4) ROWS(true, 256, 4);
-    else if (pieces <= 512 * 4) ROWS(true, 512, 4);
-    else if (pieces <= 512 * 8) ROWS(true, 512, 8);
-    else if (pieces <= 512 * 16) ROWS(true, 512, 16);
-    else ROWS(true, 1024, 8);
+    by_length(pieces, [&](auto threads, auto nv) { ROWS(true, decltype(threads)::value, decltype(nv)::value); });
   } else {
+    // Nothing has to stay: eight pieces of 256 threads at a time (8192 of 32000 in bf16 81 us), on few rows 512 threads (300 of
+    // 131072: 21.7 against 25.5) or 1024 (16 of 128000: 10.3 against 11.0).
     if (pieces <= 64 * 4) ROWS(false, 64, 4);
     else if (pieces <= 256 * 4) ROWS(false, 256, 4);
     else if (T <= ctx->cus / 4 && pieces > 8192) ROWS(false, 1024, 8);
@@ -490,24 +516,20 @@ static void launch_rows(const symi_ctx* ctx, int kid, const PolicyArgs& g, hipSt
 // 26.3 : 27.3; V = 50001: 1 row 13.2 : 11.4, 64 15.9 : 14.3, 128 16.8 : 17.8; V = 16000: 16 rows 8.7 : 6.8, 128 9.2 : 8.5, 256
 // 10.4 : 11.4; V = 4000: 16 rows 7.3 : 6.2, 256 7.6 : 6.9; fp32 V = 32003: 16 rows 11.9 : 11.5, 256 18.1 : 23.6.
 static bool wants_parts(const symi_ctx* ctx, int pieces) {
-  const int T = ctx->cfg.T, waves = pieces <= 64 * 4 ? 1 : pieces <= 256 * 4 ? 4 : pieces <= 512 * 16 ? 8 : 16;
-  return T >= 1 && T <= PART_ROWS_MAX && waves > 1 && T * waves <= 4 * ctx->cus;
+  int waves = 0;
+  by_length(pieces, [&](auto threads, auto) { waves = decltype(threads)::value / 64; });
+  return ctx->cfg.T >= 1 && ctx->cfg.T <= PART_ROWS_MAX && waves > 1 && ctx->cfg.T * waves <= 4 * ctx->cus;
 }
 template <bool BF16>
 static void launch_parts(const symi_ctx* ctx, const PolicyArgs& g, const Parts& parts, float* stats, hipStream_t st) {
-  const int T = ctx->cfg.T, pieces = cdiv(g.V, Piece<BF16>::N);
-#define PARTS(THREADS, NV)                                                                                                        \
-  do {                                                                                                                            \
-    SYMI_TIMED(ctx, K_POLICY, st, (policy_part_kernel<BF16, THREADS, NV><<<T * (THREADS / 64), 64, 0, st>>>(g, parts)));          \
-    SYMI_TIMED(ctx, K_POLICY_SUM, st, (policy_apply_kernel<BF16, THREADS, NV><<<T * (THREADS / 64) + 1, SUM_SPLIT_THREADS, 0, st>>>( \
-        g, parts, T, stats)));                                                                                                    \
-  } while (0)
-  if (pieces <= 256 * 4) PARTS(256, 4);
-  else if (pieces <= 512 * 4) PARTS(512, 4);
-  else if (pieces <= 512 * 8) PARTS(512, 8);
-  else if (pieces <= 512 * 16) PARTS(512, 16);
-  else PARTS(1024, 8);
-#undef PARTS
+  const int T = ctx->cfg.T;
+  by_length(cdiv(g.V, Piece<BF16>::N), [&](auto threads, auto nv) {
+    constexpr int THREADS = decltype(threads)::value, NV = decltype(nv)::value, WAVES = THREADS / 64;
+    if constexpr (WAVES > 1) {
+      SYMI_TIMED(ctx, K_POLICY, st, (policy_part_kernel<BF16, THREADS, NV><<<T * WAVES, 64, 0, st>>>(g, parts)));
+      SYMI_TIMED(ctx, K_POLICY_SUM, st, (policy_apply_kernel<BF16, THREADS, NV><<<T * WAVES + 1, SUM_SPLIT_THREADS, 0, st>>>(g, parts, T, stats)));
+    }
+  });
 }
 
 }  // namespace symi
