@@ -82,7 +82,7 @@ int symi_validate(const symi_cfg* cfg);
  * validated configuration of one MoE layer and optimizer partition (cfg->shard) together with
  * what the library needs to run it on the CURRENT device (queried once: compute units; created
  * once: the helper stream and events of the expert backward, only when the shape makes the two
- * gradient chains worth two streams).  Host function; with symi_adamw_create the only one that creates anything.
+ * gradient chains worth two streams).  Host function; the only one that creates anything on the device.
  *   flags: 0 or an OR of
  *     SYMI_CTX_NO_OVERLAP  every kernel of symi_expert_bwd* stays on the caller's stream
  *                          (default: the weight-gradient chain runs on the helper stream,
@@ -369,9 +369,10 @@ int symi_policy_loss(const symi_ctx* ctx, const symi_policy* hp, const void* log
  *   a hash of seed, hp->step and the element's place; the weight's update uses the values before
  *   rounding.  A block whose largest |value| is below 2^-126 is stored as zeros, one with a value that is not finite
  *   with the scale NaN (all of it reads as NaN).  Zeroed codes and scales are a fresh state.
- * The tensors' description is copied to the device by symi_adamw_create (host function, allocates
- * and waits); the memory it points to stays the caller's and has to stay in place until
- * symi_adamw_destroy.  No two tensors may overlap. */
+ * symi_adamw_create checks the tensors' description and copies what the step needs of it into `table`,
+ * symi_adamw_table_bytes(tensors, count) bytes of device memory (host function: the copy is ordered
+ * on `stream` and waited for, so it cannot be captured).  All memory stays the caller's; table and tensors have
+ * to stay in place while steps use them.  No two tensors may overlap. */
 typedef struct symi_adamw_tensor {
   void* param;         /* [n] in param_dtype, in/out */
   float* master;       /* [n] f32 in/out when param is bf16 (param = master rounded), else NULL */
@@ -386,8 +387,9 @@ typedef struct symi_adamw_tensor {
   int state_bits;      /* 32 or 8 */
 } symi_adamw_tensor;
 typedef struct symi_adamw symi_adamw;
-int symi_adamw_create(const symi_adamw_tensor* tensors, int count, symi_adamw** out);
-int symi_adamw_destroy(symi_adamw* opt);   /* NULL: no-op; the caller synchronises first */
+size_t symi_adamw_table_bytes(const symi_adamw_tensor* tensors, int count);   /* 0 if they are invalid */
+int symi_adamw_create(const symi_adamw_tensor* tensors, int count, void* table, symi_adamw** out, void* stream);
+int symi_adamw_destroy(symi_adamw* opt);   /* frees host memory only; NULL: no-op */
 /* One step.  grad_scale [1] f32 on the device (a clip factor, a loss scale) or NULL for 1. */
 int symi_adamw_step(const symi_ctx* ctx, const symi_adamw* opt, const symi_adam* hp,
                     const float* grad_scale, uint32_t seed, void* stream);

@@ -33,7 +33,7 @@ EXPORTS = [
     "symi_grad_source", "symi_collect_grads", "symi_rank_group", "symi_comm_cost",
     "symi_timing_reset", "symi_timing_read", "symi_kernel_count", "symi_kernel_name",
     "symi_embed_fwd", "symi_embed_workspace_bytes", "symi_embed_bwd", "symi_token_logp",
-    "symi_policy_workspace_bytes", "symi_policy_loss", "symi_adamw_create", "symi_adamw_destroy",
+    "symi_policy_workspace_bytes", "symi_policy_loss", "symi_adamw_table_bytes", "symi_adamw_create", "symi_adamw_destroy",
     "symi_adamw_step", "symi_adamw_values", "symi_adamw_decode",
 ]
 
@@ -120,15 +120,14 @@ class SymiAdamWTensor(ctypes.Structure):
 
 
 class SymiAdamW:
-    """Handle of a symi_adamw (symi_adamw_create); holds the tensors whose memory it describes."""
+    """Handle of a symi_adamw (symi_adamw_create); holds the table and the tensors whose memory it describes."""
 
-    def __init__(self, ptr, tensors, device):
-        self.ptr, self.tensors, self.device = ptr, tensors, device
+    def __init__(self, ptr, tensors, table):
+        self.ptr, self.tensors, self.table = ptr, tensors, table
 
     def __del__(self):
         try:
             if self.ptr:
-                torch.cuda.synchronize(self.device)   # a step in flight reads the description
                 symi_adamw_destroy(self)
         except Exception:
             pass
@@ -191,7 +190,8 @@ def lib():
             "symi_token_logp": ([ctx, ctypes.POINTER(SymiPolicy), vp, ci, ci, ip, fp, fp, vp], ci),
             "symi_policy_workspace_bytes": ([cfgp], ctypes.c_size_t),
             "symi_policy_loss": ([ctx, ctypes.POINTER(SymiPolicy), vp, ci, ci, ip, fp, fp, fp, fp, fp, fp, vp, vp, vp], ci),
-            "symi_adamw_create": ([ctypes.POINTER(SymiAdamWTensor), ci, ctypes.POINTER(ctypes.c_void_p)], ci),
+            "symi_adamw_table_bytes": ([ctypes.POINTER(SymiAdamWTensor), ci], ctypes.c_size_t),
+            "symi_adamw_create": ([ctypes.POINTER(SymiAdamWTensor), ci, vp, ctypes.POINTER(ctypes.c_void_p), vp], ci),
             "symi_adamw_destroy": ([vp], ci),
             "symi_adamw_step": ([ctx, vp, ctypes.POINTER(SymiAdam), fp, ctypes.c_uint32, vp], ci),
             "symi_adamw_values": ([vp], ctypes.c_longlong),
@@ -660,11 +660,16 @@ def _adamw_tensor(i, t):
 
 
 def symi_adamw_create(tensors):
+    """`tensors`: a list of dicts, see _adamw_tensor.  The table is allocated here, on the current device."""
     tensors = [dict(t) for t in tensors]
     entries = (SymiAdamWTensor * max(1, len(tensors)))(*[_adamw_tensor(i, t) for i, t in enumerate(tensors)])
-    out = ctypes.c_void_p()
-    _check(lib().symi_adamw_create(entries, len(tensors), ctypes.byref(out)), "symi_adamw_create")
-    return SymiAdamW(out, tensors, torch.cuda.current_device())
+    size = lib().symi_adamw_table_bytes(entries, len(tensors))
+    if size == 0:
+        raise SymiError(f"symi_adamw_create failed: {symi_last_error()}")
+    table, out = torch.empty(size, dtype=torch.uint8, device="cuda"), ctypes.c_void_p()
+    _check(lib().symi_adamw_create(entries, len(tensors), ctypes.c_void_p(table.data_ptr()), ctypes.byref(out), _stream()),
+           "symi_adamw_create")
+    return SymiAdamW(out, tensors, table)
 
 
 def symi_adamw_destroy(opt):

@@ -1,7 +1,7 @@
 // symi_adamw_*: AdamW over many tensors in one launch, states in 32 bits or in 8 bits with a scale for every 256 values.
 //
-// symi_adamw_create cuts the tensors into chunks and keeps the list on the device; a workgroup takes one chunk, so the
-// number of tensors costs nothing.  A block of 256 values is one wavefront, four values a lane.
+// symi_adamw_create cuts the tensors into chunks and writes the list into the caller's table; a workgroup takes one chunk,
+// so the number of tensors costs nothing.  A block of 256 values is one wavefront, four values a lane.
 //
 // 8-bit states: m = a sign(c) (c / 127)^2 and v = a (c / 255)^4 with a the largest |value| of the block.  Codes lie closer
 // where values are small: m reaches down to 6e-5 of a block's largest, v to 2e-10 (its root, which the update divides by,
@@ -385,10 +385,9 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_decode_kernel(const Adamw
 
 struct symi_adamw {
   uint32_t magic;
-  int device, count;
+  int device;
   long long chunks, values;
-  void* table;   // on the device: the tensors, then the chunks
-  const symi::AdamwTensor* tensors;
+  const symi::AdamwTensor* tensors;   // in the caller's table, the chunks behind them
   const symi::AdamwChunk* list;
 };
 
@@ -402,90 +401,120 @@ static int enter_adamw(const symi_ctx* ctx, const symi_adamw* opt, const char* w
   return SYMI_OK;
 }
 
-extern "C" int symi_adamw_create(const symi_adamw_tensor* tensors, int count, symi_adamw** out) {
+// Checks the tensors; sizes of the description, in elements of each kind.
+struct AdamwSizes {
+  long long tensors, chunks, blocks;
+  bool fine;
+  size_t list_at() const { return align_up((size_t)tensors * sizeof(AdamwTensor), 256); }
+  size_t bytes() const { return list_at() + (size_t)chunks * sizeof(AdamwChunk) + 256; }
+};
+static int check_tensors(const char* who, const symi_adamw_tensor* tensors, int count, AdamwSizes* out) {
+  SYMI_REQUIRE(count >= 0 && (tensors || count == 0), who, "count < 0 or no tensors");
+  AdamwSizes n = {0, 0, 0, false};
+  long long values = 0;
+  for (int i = 0; i < count; ++i) {
+    const symi_adamw_tensor& s = tensors[i];
+    const auto bad = [&](bool cond, const char* msg) {
+      if (cond) set_error("%s: tensor %d: %s", who, i, msg);
+      return cond;
+    };
+    if (bad(s.n < 0, "n < 0") || bad(s.state_bits != 32 && s.state_bits != 8, "state_bits must be 32 or 8") ||
+        bad(s.param_dtype != SYMI_F32 && s.param_dtype != SYMI_BF16, "param_dtype must be SYMI_F32 or SYMI_BF16") ||
+        bad(s.grad_dtype != SYMI_F32 && s.grad_dtype != SYMI_BF16, "grad_dtype must be SYMI_F32 or SYMI_BF16") ||
+        bad(!(s.decay >= 0.f), "decay must be >= 0") ||
+        bad(s.n && !(s.param && s.grad && s.m && s.v), "NULL pointer") ||
+        bad(s.n && (s.param_dtype == SYMI_BF16) != (s.master != nullptr), "a bf16 param needs its master, an fp32 one has none") ||
+        bad(s.n && ((s.state_bits == 8) != (s.m_scale != nullptr) || (s.state_bits == 8) != (s.v_scale != nullptr)),
+            "8-bit states need their scales, 32-bit ones have none"))
+      return SYMI_EINVAL;
+    if (s.n >> 36 || (n.blocks += (s.n + ADAMW_BLOCK - 1) / ADAMW_BLOCK) > 1LL << 28) {
+      set_error("%s: more than 2^28 blocks of 256 values", who);
+      return SYMI_EUNSUPPORTED;
+    }
+    values += s.n;
+  }
+  n.fine = values < FINE_BELOW;
+  for (int i = 0; i < count; ++i) {
+    const long long whole = n.fine ? 0 : tensors[i].n / ADAMW_CHUNK, rest = tensors[i].n - whole * ADAMW_CHUNK;
+    n.tensors += tensors[i].n > 0;
+    n.chunks += whole + (rest + ADAMW_WAVES * ADAMW_BLOCK - 1) / (ADAMW_WAVES * ADAMW_BLOCK);
+  }
+  if (n.chunks >= 1LL << 24) {   // a workgroup each; the threads of a launch end at 2^32
+    set_error("%s: more than 2^24 - 1 chunks of up to %d values", who, ADAMW_CHUNK);
+    return SYMI_EUNSUPPORTED;
+  }
+  *out = n;
+  return SYMI_OK;
+}
+
+extern "C" size_t symi_adamw_table_bytes(const symi_adamw_tensor* tensors, int count) {
+  AdamwSizes n;
+  return check_tensors("symi_adamw_table_bytes", tensors, count, &n) == SYMI_OK ? n.bytes() : 0;
+}
+
+extern "C" int symi_adamw_create(const symi_adamw_tensor* tensors, int count, void* table, symi_adamw** out, void* stream) {
   const char* const who = "symi_adamw_create";
   SYMI_REQUIRE(out, who, "out is NULL");
   *out = nullptr;
-  SYMI_REQUIRE(count >= 0 && (tensors || count == 0), who, "count < 0 or no tensors");
+  AdamwSizes n;
+  if (int rc = check_tensors(who, tensors, count, &n)) return rc;
+  SYMI_REQUIRE(table || n.chunks == 0, who, "table is NULL");
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess) {
+    (void)hipGetLastError();
+    set_error("%s: no usable HIP device is current", who);
+    return SYMI_EHIP;
+  }
+  char* const to = reinterpret_cast<char*>(align_up(reinterpret_cast<size_t>(table), 256));
+  std::vector<char> copy;
+  symi_adamw* opt = nullptr;
   try {
-    std::vector<AdamwTensor> list;
-    std::vector<AdamwChunk> chunks;
-    long long blocks = 0, all = 0;
-    for (int i = 0; i < count; ++i) all += tensors[i].n > 0 && tensors[i].n < 1LL << 36 ? tensors[i].n : 0;
-    const bool fine = all < FINE_BELOW;
-    for (int i = 0; i < count; ++i) {
-      const symi_adamw_tensor& s = tensors[i];
-      const auto bad = [&](bool cond, const char* msg) {
-        if (cond) set_error("%s: tensor %d: %s", who, i, msg);
-        return cond;
-      };
-      if (bad(s.n < 0, "n < 0") || bad(s.state_bits != 32 && s.state_bits != 8, "state_bits must be 32 or 8") ||
-          bad(s.param_dtype != SYMI_F32 && s.param_dtype != SYMI_BF16, "param_dtype must be SYMI_F32 or SYMI_BF16") ||
-          bad(s.grad_dtype != SYMI_F32 && s.grad_dtype != SYMI_BF16, "grad_dtype must be SYMI_F32 or SYMI_BF16") ||
-          bad(!(s.decay >= 0.f), "decay must be >= 0") ||
-          bad(s.n && !(s.param && s.grad && s.m && s.v), "NULL pointer") ||
-          bad(s.n && (s.param_dtype == SYMI_BF16) != (s.master != nullptr), "a bf16 param needs its master, an fp32 one has none") ||
-          bad(s.n && (s.state_bits == 8) != (s.m_scale != nullptr) , "8-bit states need their scales, 32-bit ones have none") ||
-          bad(s.n && (s.state_bits == 8) != (s.v_scale != nullptr), "8-bit states need their scales, 32-bit ones have none"))
-        return SYMI_EINVAL;
-      if (s.n == 0) continue;
-      const long long mine = s.n / ADAMW_BLOCK + (s.n % ADAMW_BLOCK != 0);
-      if (s.n >> 36 || blocks + mine > 1LL << 28) {
-        set_error("%s: more than 2^28 blocks of 256 values", who);
-        return SYMI_EUNSUPPORTED;
-      }
-      list.push_back({s.param, s.master, s.grad, s.m, s.v, s.m_scale, s.v_scale, s.n, (unsigned)blocks, s.decay,
-                      (s.param_dtype == SYMI_BF16) | (s.grad_dtype == SYMI_BF16) << 1 | (s.state_bits == 8) << 2});
-      long long at = 0;
-      for (; !fine && at + ADAMW_CHUNK <= s.n; at += ADAMW_CHUNK) chunks.push_back({(int)list.size() - 1, (unsigned)(at / ADAMW_BLOCK) | WHOLE});
-      for (; at < s.n; at += ADAMW_WAVES * ADAMW_BLOCK) chunks.push_back({(int)list.size() - 1, (unsigned)(at / ADAMW_BLOCK)});
-      blocks += mine;
-      if (chunks.size() >= 1u << 24) {   // a workgroup each; the threads of a launch end at 2^32
-        set_error("%s: more than 2^24 - 1 chunks of up to %d values", who, ADAMW_CHUNK);
-        return SYMI_EUNSUPPORTED;
-      }
-    }
-    int dev = -1;
-    if (hipGetDevice(&dev) != hipSuccess) {
-      (void)hipGetLastError();
-      set_error("%s: no usable HIP device is current", who);
-      return SYMI_EHIP;
-    }
-    symi_adamw* const opt = new symi_adamw();
-    opt->device = dev;
-    opt->count = count;
-    opt->chunks = (long long)chunks.size();
-    opt->values = blocks * ADAMW_BLOCK;
-    opt->table = nullptr;
-    const size_t bytes1 = align_up(list.size() * sizeof(AdamwTensor), 256), bytes2 = chunks.size() * sizeof(AdamwChunk);
-    if (bytes2) {
-      hipError_t e = hipMalloc(&opt->table, bytes1 + bytes2);
-      if (e == hipSuccess) e = hipMemcpy(opt->table, list.data(), list.size() * sizeof(AdamwTensor), hipMemcpyHostToDevice);
-      if (e == hipSuccess) e = hipMemcpy(static_cast<char*>(opt->table) + bytes1, chunks.data(), bytes2, hipMemcpyHostToDevice);
-      if (e != hipSuccess) {
-        set_error("%s: %s", who, hipGetErrorString(e));
-        (void)hipGetLastError();
-        if (opt->table) (void)hipFree(opt->table);
-        delete opt;
-        return SYMI_EHIP;
-      }
-    }
-    opt->tensors = static_cast<const AdamwTensor*>(opt->table);
-    opt->list = reinterpret_cast<const AdamwChunk*>(static_cast<char*>(opt->table) + bytes1);
-    opt->magic = ADAMW_MAGIC;
-    *out = opt;
-    return SYMI_OK;
-  } catch (const std::bad_alloc&) {
+    copy.resize(n.list_at() + (size_t)n.chunks * sizeof(AdamwChunk));
+    opt = new symi_adamw();
+  } catch (const std::exception&) {
     set_error("%s: out of host memory", who);
     return SYMI_EHIP;
   }
+  AdamwTensor* t = reinterpret_cast<AdamwTensor*>(copy.data());
+  AdamwChunk* c = reinterpret_cast<AdamwChunk*>(copy.data() + n.list_at());
+  unsigned block = 0;
+  int index = 0;
+  for (int i = 0; i < count; ++i) {
+    const symi_adamw_tensor& s = tensors[i];
+    if (s.n == 0) continue;
+    *t++ = {s.param, s.master, s.grad, s.m, s.v, s.m_scale, s.v_scale, s.n, block, s.decay,
+            (s.param_dtype == SYMI_BF16) | (s.grad_dtype == SYMI_BF16) << 1 | (s.state_bits == 8) << 2};
+    long long at = 0;
+    for (; !n.fine && at + ADAMW_CHUNK <= s.n; at += ADAMW_CHUNK) *c++ = {index, (unsigned)(at / ADAMW_BLOCK) | WHOLE};
+    for (; at < s.n; at += ADAMW_WAVES * ADAMW_BLOCK) *c++ = {index, (unsigned)(at / ADAMW_BLOCK)};
+    block += (unsigned)((s.n + ADAMW_BLOCK - 1) / ADAMW_BLOCK);
+    ++index;
+  }
+  opt->device = dev;
+  opt->chunks = n.chunks;
+  opt->values = n.blocks * ADAMW_BLOCK;
+  opt->tensors = reinterpret_cast<const AdamwTensor*>(to);
+  opt->list = reinterpret_cast<const AdamwChunk*>(to + n.list_at());
+  if (n.chunks) {
+    hipStream_t st = as_stream(stream);
+    hipError_t e = hipMemcpyAsync(to, copy.data(), copy.size(), hipMemcpyHostToDevice, st);
+    if (e == hipSuccess) e = hipStreamSynchronize(st);
+    if (e != hipSuccess) {
+      set_error("%s: %s", who, hipGetErrorString(e));
+      (void)hipGetLastError();
+      delete opt;
+      return SYMI_EHIP;
+    }
+  }
+  opt->magic = ADAMW_MAGIC;
+  *out = opt;
+  return SYMI_OK;
 }
 
 extern "C" int symi_adamw_destroy(symi_adamw* opt) {
   if (!opt) return SYMI_OK;
   SYMI_REQUIRE(opt->magic == ADAMW_MAGIC, "symi_adamw_destroy", "not a live one of symi_adamw_create");
   opt->magic = 0;
-  if (opt->table) (void)hipFree(opt->table);
   delete opt;
   return SYMI_OK;
 }

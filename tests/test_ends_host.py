@@ -29,9 +29,13 @@ def test_descriptions_are_checked_before_any_device_is_needed():
 
     def create(count=1, **kw):
         t = (SymiAdamWTensor * 1)(SymiAdamWTensor(**{**ok, **kw}))
-        return L.symi_adamw_create(t, count, ctypes.byref(out))
+        size = L.symi_adamw_table_bytes(t, count)
+        rc = L.symi_adamw_create(t, count, 256, ctypes.byref(out), None)
+        assert (size > 0) == (rc not in (-1, -2))
+        return rc
 
-    assert L.symi_adamw_create(None, 1, ctypes.byref(out)) == -1 and L.symi_adamw_create(None, 0, None) == -1
+    assert L.symi_adamw_create(None, 1, None, ctypes.byref(out), None) == -1 and L.symi_adamw_create(None, 0, None, None, None) == -1
+    assert L.symi_adamw_create((SymiAdamWTensor * 1)(SymiAdamWTensor(**ok)), 1, None, ctypes.byref(out), None) == -1   # no table
     for kw in (dict(n=-1), dict(state_bits=16), dict(param_dtype=2), dict(grad_dtype=-1), dict(decay=-1.0), dict(decay=float("nan")),
                dict(param=None), dict(grad=None), dict(m=None), dict(v=None), dict(param_dtype=1), dict(master=8), dict(state_bits=8),
                dict(state_bits=8, m_scale=8), dict(m_scale=8), dict(v_scale=8), dict(count=-1)):
