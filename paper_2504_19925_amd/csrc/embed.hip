@@ -135,7 +135,12 @@ __global__ __launch_bounds__(WAVES * 64) void embed_sort_kernel(const int32_t* _
       own += __popcll(mask);
     }
   }
-  for (int k = lane; k < min(own, keep); k += 64) atomicAdd(&mine[kept[wave][k] & 1023u], 1);
+  for (int k = 0; k < min(own, keep); k += 64) {   // the first one's equals at once: a frequent row's would wait for each other
+    const bool there = k + lane < min(own, keep);
+    const uint32_t r = kept[wave][min(k + lane, SORT_KEEP - 1)] & 1023u, first = (uint32_t)__builtin_amdgcn_readfirstlane((int)r);
+    const unsigned long long same = __ballot(there && r == first);
+    if (there && (r != first || lane == 0)) atomicAdd(&mine[r], lane == 0 ? (int)__popcll(same) : 1);
+  }
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) less += __shfl_xor(less, m, 64);
   if (lane == 0) wave_less[wave] = less;
@@ -204,9 +209,13 @@ __global__ __launch_bounds__(WAVES * 64) void embed_sort_kernel(const int32_t* _
 }
 
 // Sums: the sorted tokens are cut into chunks of C, whatever their rows, so that a row that half the batch chose is as much
-// parallel work as any other.  A wavefront takes 64 pieces of the rows of a chunk.  A run of at most 2 C tokens of one row is all of
-// it the work of the chunk in which it begins.  Of a longer one every chunk sums its share and leaves it in `partial`
-// [chunks, 2, d]: in slot 1 where the run begins, in slot 0 of the chunks after it; embed_join adds them up in order.
+// parallel work as any other.  A wavefront takes 64 pieces of the rows of a chunk: all tokens of the runs (equal rows) that begin in
+// it.  Only a run of more than 2 C tokens across a multiple of SHARE is split, at those multiples: its parts go to `partial`
+// [blocks of SHARE, 2, d], in slot 1 where the run begins, in slot 0 of the blocks after it, and embed_join adds them up in order.
+// Sums and joins, us, with 16 : 32 : 64 tokens a share: 42750 tokens of d = 48 17 : 21 : 32, 19626 of 408, a third of them one row, 18 : 24 :
+// 36, 8192 of 1024 19 : 24 : 36, 65536 of 1024, a quarter one row, 74 : 83 : 131, 65536 of 4096 348 : 347 : 375.
+constexpr int SHARE = 16;   // a multiple of every C
+__device__ __forceinline__ bool is_split(int2 run, int C) { return run.y - run.x > 2 * C && run.x / SHARE != (run.y - 1) / SHARE; }
 constexpr int SUM_ROWS = 8;   // rows that a wavefront has in flight
 
 __device__ __forceinline__ void put_row(float* to, const float* x, float scale) {
@@ -258,20 +267,28 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(
   if (unit >= units || begin >= end) return;
   const int c = ((unit % parts) * 64 + lane) * N;
   const bool live = c < d;
-  int head = 0, tail = 0;   // tokens of long runs that began before / that go on behind
+  // places below head_end are a share of a run that began before, those from tail_begin on one of a run that goes on behind
+  int head_end = lo, tail_begin = 0x7fffffff;
   {
     const int2 a = span[__builtin_amdgcn_readlane(row, 0)], z = span[__builtin_amdgcn_readlane(row, end - 1 - lo)];
-    if (z.y > end) {
-      if (z.y - z.x <= 2 * C) end = z.y;
-      else tail = end - max(z.x, begin);
+    if (z.x >= lo && z.y > end) {
+      if (is_split(z, C)) {
+        end = (z.x / SHARE + 1) * SHARE;
+        tail_begin = z.x;
+      } else {
+        end = z.y;
+      }
     }
-    if (a.x < begin) {
-      if (a.y - a.x <= 2 * C) begin = a.y;
-      else head = min(a.y, lo + C) - begin;
+    if (a.x < lo) {
+      if (lo % SHARE == 0 && is_split(a, C)) {
+        head_end = min(a.y, lo + SHARE);
+        end = max(end, head_end);
+      } else {
+        begin = a.y;
+      }
     }
-    if (head && tail == end - begin) tail = 0;   // nothing but the middle of one run
+    if (begin >= end) return;
   }
-  const int first_own = begin + head, last_own = end - tail;
   float sum[N] = {};
   for (int w0 = lo; w0 < end; w0 += 64) {   // lane i holds place w0 + i
     const int n = min(64, end - w0);
@@ -291,7 +308,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(
         const int i = i0 + u;
         if (i >= n) continue;
         if (live) x[u] = P::load(dX, (long long)__builtin_amdgcn_readlane(token, i) * d + c);
-        if (ADD && live && (ends >> i & 1) && w0 + i >= first_own && w0 + i < last_own)
+        if (ADD && live && (ends >> i & 1) && w0 + i >= head_end && w0 + i < tail_begin)
 #pragma unroll
           for (int h = 0; h < N / 4; ++h)
             old[u][h] = *reinterpret_cast<const f32x4_f32*>(dTable + (long long)__builtin_amdgcn_readlane(row, i) * d + c + 4 * h);
@@ -305,7 +322,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(
 #pragma unroll
         for (int j = 0; j < N; ++j) sum[j] += y[j];
         if (!(ends >> i & 1)) continue;
-        if (live && w0 + i >= first_own && w0 + i < last_own) {
+        if (live && w0 + i >= head_end && w0 + i < tail_begin) {
           float* const to = dTable + (long long)__builtin_amdgcn_readlane(row, i) * d + c;
 #pragma unroll
           for (int h = 0; h < N / 4; ++h) {
@@ -313,7 +330,8 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(
             else put_row(to + 4 * h, sum + 4 * h, scale);
           }
         } else if (live) {
-          float* const to = partial + ((long long)chunk * 2 + (w0 + i >= first_own)) * d + c;
+          const bool tail = w0 + i >= head_end;
+          float* const to = partial + ((long long)((tail ? tail_begin : lo) / SHARE) * 2 + tail) * d + c;
 #pragma unroll
           for (int h = 0; h < N / 4; ++h) put_row(to + 4 * h, sum + 4 * h, 1.f);
         }
@@ -324,8 +342,8 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(
   }
 }
 
-// A workgroup: 256 columns of the long runs that begin in one of JOIN_CHUNKS chunks.  The workgroups behind those fill rows.
-constexpr int JOIN_WAVES = 8, JOIN_ROWS = 8, JOIN_CHUNKS = 16;
+// A workgroup: 256 columns of the split runs that begin in one of JOIN_BLOCKS blocks.  The workgroups behind those fill rows.
+constexpr int JOIN_WAVES = 8, JOIN_ROWS = 8, JOIN_BLOCKS = 8;
 template <bool ADD>
 __global__ __launch_bounds__(JOIN_WAVES * 64) void embed_join_kernel(const int2* __restrict__ span, const int32_t* __restrict__ rows_of,
                                                                      const int32_t* __restrict__ total_of, const float* __restrict__ partial,
@@ -341,25 +359,25 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void embed_join_kernel(const int2*
   const int block = (int)(group / columns), column = (int)(group % columns);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int total = *total_of;
-  // the last run of a chunk
-  const long long hi = ((long long)block * JOIN_CHUNKS + lane + 1) * C;
+  // the run across the end of a block
+  const long long hi = ((long long)block * JOIN_BLOCKS + lane + 1) * SHARE;
   const int row_of = rows_of[min(hi, (long long)size) - 1];   // beyond the total: anything
-  const bool there = lane < JOIN_CHUNKS && hi < total;
+  const bool there = lane < JOIN_BLOCKS && hi < total;
   const int2 s = there ? span[row_of] : int2{0, 0};
-  unsigned long long todo = __ballot(there && s.y > hi && s.x >= hi - C && s.y - s.x > 2 * C);
+  unsigned long long todo = __ballot(there && s.y > hi && s.x >= hi - SHARE && is_split(s, C));
   const int c = (column * 64 + lane) * 4;
   const bool live = c < d;
   for (; todo; todo &= todo - 1) {
     const int i = (int)__builtin_ctzll(todo), row = __builtin_amdgcn_readlane(row_of, i), stop = __builtin_amdgcn_readlane(s.y, i);
-    const int chunk = block * JOIN_CHUNKS + i;
-    const int count = (stop - 1) / C - chunk + 1;   // shares: slot 1 of this chunk, slot 0 of the next ones
+    const int first = block * JOIN_BLOCKS + i;
+    const int count = (stop - 1) / SHARE - first + 1;   // shares: slot 1 of this block, slot 0 of the next ones
     const int each = (count + JOIN_WAVES - 1) / JOIN_WAVES, begin = wave * each, end = min(begin + each, count);
     float4 sum = {0.f, 0.f, 0.f, 0.f};
     for (int k0 = begin; k0 < end && live; k0 += JOIN_ROWS) {
       float4 x[JOIN_ROWS];
 #pragma unroll
       for (int u = 0; u < JOIN_ROWS; ++u)
-        if (k0 + u < end) x[u] = *reinterpret_cast<const float4*>(partial + ((long long)(chunk + k0 + u) * 2 + (k0 + u == 0)) * d + c);
+        if (k0 + u < end) x[u] = *reinterpret_cast<const float4*>(partial + ((long long)(first + k0 + u) * 2 + (k0 + u == 0)) * d + c);
 #pragma unroll
       for (int u = 0; u < JOIN_ROWS; ++u)
         if (k0 + u < end) { sum.x += x[u].x; sum.y += x[u].y; sum.z += x[u].z; sum.w += x[u].w; }
@@ -478,11 +496,10 @@ __global__ __launch_bounds__(WAVES * 64) void embed_few_kernel(const int32_t* __
   }
 }
 
-// Tokens of a chunk: many chunks keep the chip busy, but every chunk of a long run leaves a row in fp32, and one workgroup
-// adds up what a run left.
+// Tokens of a chunk: few while the chip has room for their wavefronts, more where the look-ups in front of the sums would count.
 static int embed_chunk(const symi_cfg* c, int parts) {
   int C = 4;
-  while (C < 64 && ((long long)c->T * parts > 16384LL * C || c->T > 2048 * C)) C *= 2;
+  while (C < SHARE && (long long)c->T * parts > 16384LL * C) C *= 2;
   return C;
 }
 
@@ -501,7 +518,7 @@ static EmbedWs embed_ws(const symi_cfg* c, int V) {
   L.parts = cdiv(c->d, 64 * (c->dtype == SYMI_BF16 ? 8 : 4));
   L.chunk = embed_chunk(c, L.parts);
   L.chunks = cdiv(c->T, L.chunk);
-  L.partial = take((size_t)L.chunks * 2 * c->d * sizeof(float));
+  L.partial = take(((size_t)c->T / SHARE + 1) * 2 * c->d * sizeof(float));
   L.total = off + 256;
   return L;
 }
@@ -607,7 +624,7 @@ extern "C" int symi_embed_bwd(const symi_ctx* ctx, const int32_t* tokens, const 
   else SUM(false, false);
 #undef SUM
   {
-    const int joins = cdiv(L.chunks, JOIN_CHUNKS), columns = cdiv(cfg->d, 256);
+    const int joins = cdiv(cfg->T, SHARE * JOIN_BLOCKS), columns = cdiv(cfg->d, 256);
     const dim3 grid = grid_of((long long)joins * columns + fills(pieces - fill_sum));
 #define JOIN(ADD)                                                                                         \
   SYMI_TIMED(ctx, K_EMBED_JOIN, st, (embed_join_kernel<ADD><<<grid, JOIN_WAVES * 64, 0, st>>>(            \
