@@ -210,12 +210,19 @@ __global__ __launch_bounds__(WAVES * 64) void embed_sort_kernel(const int32_t* _
 
 // Sums: the sorted tokens are cut into chunks of C, whatever their rows, so that a row that half the batch chose is as much
 // parallel work as any other.  A wavefront takes 64 pieces of the rows of a chunk: all tokens of the runs (equal rows) that begin in
-// it.  Only a run of more than 2 C tokens across a multiple of SHARE is split, at those multiples: its parts go to `partial`
-// [blocks of SHARE, 2, d], in slot 1 where the run begins, in slot 0 of the blocks after it, and embed_join adds them up in order.
+// it.  Only a run of more than 2 C tokens across a multiple of its share is split, at those multiples: its parts go to `partial`
+// [blocks of SHARE, 2, d], by the block in which they begin: in slot 1 where the run begins, else in slot 0.  embed_join
+// adds them up in order.
 // Sums and joins, us, with 16 : 32 : 64 tokens a share: 42750 tokens of d = 48 17 : 21 : 32, 19626 of 408, a third of them one row, 18 : 24 :
 // 36, 8192 of 1024 19 : 24 : 36, 65536 of 1024, a quarter one row, 74 : 83 : 131, 65536 of 4096 348 : 347 : 375.
-constexpr int SHARE = 16;   // a multiple of every C
-__device__ __forceinline__ bool is_split(int2 run, int C) { return run.y - run.x > 2 * C && run.x / SHARE != (run.y - 1) / SHARE; }
+constexpr int SHARE = 16;          // a multiple of every C
+constexpr int SHARES_MAX = 1024;   // of a run, as one workgroup adds them up: longer runs have larger shares
+__device__ __forceinline__ int share_of(int2 run) {
+  int S = SHARE;
+  while (run.y - run.x > SHARES_MAX * S) S *= 2;
+  return S;
+}
+__device__ __forceinline__ bool is_split(int2 run, int C, int S) { return run.y - run.x > 2 * C && run.x / S != (run.y - 1) / S; }
 constexpr int SUM_ROWS = 8;   // rows that a wavefront has in flight
 
 __device__ __forceinline__ void put_row(float* to, const float* x, float scale) {
@@ -272,16 +279,18 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(
   {
     const int2 a = span[__builtin_amdgcn_readlane(row, 0)], z = span[__builtin_amdgcn_readlane(row, end - 1 - lo)];
     if (z.x >= lo && z.y > end) {
-      if (is_split(z, C)) {
-        end = (z.x / SHARE + 1) * SHARE;
+      const int S = share_of(z);
+      if (is_split(z, C, S)) {
+        end = (z.x / S + 1) * S;
         tail_begin = z.x;
       } else {
         end = z.y;
       }
     }
     if (a.x < lo) {
-      if (lo % SHARE == 0 && is_split(a, C)) {
-        head_end = min(a.y, lo + SHARE);
+      const int S = share_of(a);
+      if (lo % S == 0 && is_split(a, C, S)) {
+        head_end = min(a.y, lo + S);
         end = max(end, head_end);
       } else {
         begin = a.y;
@@ -364,20 +373,22 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void embed_join_kernel(const int2*
   const int row_of = rows_of[min(hi, (long long)size) - 1];   // beyond the total: anything
   const bool there = lane < JOIN_BLOCKS && hi < total;
   const int2 s = there ? span[row_of] : int2{0, 0};
-  unsigned long long todo = __ballot(there && s.y > hi && s.x >= hi - SHARE && is_split(s, C));
+  unsigned long long todo = __ballot(there && s.y > hi && s.x >= hi - SHARE && is_split(s, C, share_of(s)));
   const int c = (column * 64 + lane) * 4;
   const bool live = c < d;
   for (; todo; todo &= todo - 1) {
     const int i = (int)__builtin_ctzll(todo), row = __builtin_amdgcn_readlane(row_of, i), stop = __builtin_amdgcn_readlane(s.y, i);
-    const int first = block * JOIN_BLOCKS + i;
-    const int count = (stop - 1) / SHARE - first + 1;   // shares: slot 1 of this block, slot 0 of the next ones
+    // shares: slot 1 of this block, slot 0 of the blocks at the multiples of S behind it
+    const int start = __builtin_amdgcn_readlane(s.x, i), S = share_of(int2{start, stop});
+    const int count = (stop - 1) / S - start / S + 1;
+    const auto block_of = [&](int k) { return (k == 0 ? start : (start / S + k) * S) / SHARE; };
     const int each = (count + JOIN_WAVES - 1) / JOIN_WAVES, begin = wave * each, end = min(begin + each, count);
     float4 sum = {0.f, 0.f, 0.f, 0.f};
     for (int k0 = begin; k0 < end && live; k0 += JOIN_ROWS) {
       float4 x[JOIN_ROWS];
 #pragma unroll
       for (int u = 0; u < JOIN_ROWS; ++u)
-        if (k0 + u < end) x[u] = *reinterpret_cast<const float4*>(partial + ((long long)(first + k0 + u) * 2 + (k0 + u == 0)) * d + c);
+        if (k0 + u < end) x[u] = *reinterpret_cast<const float4*>(partial + ((long long)block_of(k0 + u) * 2 + (k0 + u == 0)) * d + c);
 #pragma unroll
       for (int u = 0; u < JOIN_ROWS; ++u)
         if (k0 + u < end) { sum.x += x[u].x; sum.y += x[u].y; sum.z += x[u].z; sum.w += x[u].w; }
