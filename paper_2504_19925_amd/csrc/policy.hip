@@ -477,9 +477,9 @@ static PolicyScalars scalars(const symi_policy* hp) {
 // The workgroup for a row with its gradient: f(THREADS, NV).  The smallest that holds the row comes first, with four to 16 pieces a
 // thread: us for 8192 rows in bf16, threads x pieces.  V = 3000: 64 x 8 31, 128 x 8 29, 256 x 4 34; 10001: 256 x 4 80, 256 x 8
 // 75, 512 x 4 85; 17010: 256 x 16 112, 512 x 8 113; 28000: 512 x 8 179, 512 x 12 176, 256 x 16 186; 45000: 512 x 12 285, 512 x 16
-// 274; 50001: 512 x 16 298, in two parts 10 % more.  Longer rows are read again in part, most of it from the memory-side cache,
-// and two workgroups a unit of 64 registers are faster than one of 128 that holds all (16384 of 131072, a quarter masked: 1567
-// against 1718).
+// 274; 50001: 512 x 16 298, in two parts 10 % more.  Longer rows are read again in part, most of it from the memory-side cache: 4096
+// of 100000 with eight pieces of 1024 threads 337, with 16 351; 16384 of 131072, a quarter masked, 1508 and 1444; 2048 of
+// 200000 in fp32 889 and 782.
 template <int X> using Int = std::integral_constant<int, X>;
 template <class F>
 static void by_length(int pieces, F f) {
@@ -490,7 +490,8 @@ static void by_length(int pieces, F f) {
   else if (pieces <= 3072) f(Int<512>(), Int<8>());
   else if (pieces <= 512 * 9) f(Int<512>(), Int<12>());
   else if (pieces <= 512 * 16) f(Int<512>(), Int<16>());
-  else f(Int<1024>(), Int<8>());
+  else if (pieces <= 12800) f(Int<1024>(), Int<8>());
+  else f(Int<1024>(), Int<16>());
 }
 
 template <bool BF16>
