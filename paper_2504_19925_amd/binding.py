@@ -201,12 +201,15 @@ def lib():
             fn = getattr(L, name)
             fn.argtypes = args
             fn.restype = res
-        _marshal.update(_load_marshal(L))
+        for name, fast in _load_marshal(L).items():
+            (_marshal_ends if name in ENDS else _marshal)[name] = fast
         _LIB = L
     return _LIB
 
 
-_marshal = {}   # name -> function of _marshal.so, filled when libsymi.so is loaded
+_marshal = {}   # name -> function of _marshal.so, filled when libsymi.so is loaded: the layer's calls
+_marshal_ends = {}   # and those of the ends of the step
+ENDS = ("symi_embed_fwd", "symi_embed_bwd", "symi_token_logp", "symi_policy_loss", "symi_adamw_step", "symi_adamw_decode")
 
 
 def _load_marshal(L):
@@ -239,6 +242,23 @@ def _device_call(slow):
         if rc:
             _check(rc, name)
 
+    return call
+
+
+def _ends_call(slow):
+    """The same for the ends of the step; the ctypes path is `call.through_ctypes`."""
+    name = slow.__name__
+
+    def call(*args, **kw):
+        fast = None if kw else _marshal_ends.get(name)
+        rc = fast(*args) if fast else None
+        if rc is None:
+            return slow(*args, **kw)
+        if rc:
+            _check(rc, name)
+
+    call.__name__ = call.__qualname__ = name
+    call.__doc__, call.through_ctypes = slow.__doc__, slow
     return call
 
 
@@ -593,14 +613,14 @@ def symi_policy_workspace_bytes(cfg):
     return lib().symi_policy_workspace_bytes(ctypes.byref(_cfg_of(cfg)))
 
 
-@_device_call
+@_ends_call
 def symi_embed_fwd(ctx, tokens, table, V, scale, X):
     dt = ctx.torch_dtype
     _check(lib().symi_embed_fwd(ctx.ptr, _dev(tokens, I32, "tokens", ctx.T), _dev(table, dt, "table", int(V) * ctx.d),
                                 int(V), float(scale), _dev(X, dt, "X", ctx.T * ctx.d), _stream()), "symi_embed_fwd")
 
 
-@_device_call
+@_ends_call
 def symi_embed_bwd(ctx, tokens, dX, V, scale, accumulate, dTable, ws):
     _check(lib().symi_embed_bwd(
         ctx.ptr, _dev(tokens, I32, "tokens", ctx.T), _dev(dX, ctx.torch_dtype, "dX", ctx.T * ctx.d), int(V), float(scale),
@@ -612,7 +632,7 @@ def _rows(t, hp, name, ctx, ld):
     return _dev(t, hp.torch_dtype, name, ctx.T * int(ld))
 
 
-@_device_call
+@_ends_call
 def symi_token_logp(ctx, hp, logits, V, ld, action, weight, logp):
     _check(lib().symi_token_logp(
         ctx.ptr, ctypes.byref(hp), _rows(logits, hp, "logits", ctx, ld), int(V), int(ld), _dev(action, I32, "action", ctx.T),
@@ -620,7 +640,7 @@ def symi_token_logp(ctx, hp, logits, V, ld, action, weight, logp):
         "symi_token_logp")
 
 
-@_device_call
+@_ends_call
 def symi_policy_loss(ctx, hp, logits, V, ld, action, logp_old, logp_ref, advantage, weight, logp, stats, dlogits, ws):
     _check(lib().symi_policy_loss(
         ctx.ptr, ctypes.byref(hp), _rows(logits, hp, "logits", ctx, ld), int(V), int(ld), _dev(action, I32, "action", ctx.T),
@@ -682,14 +702,14 @@ def symi_adamw_values(opt):
     return lib().symi_adamw_values(opt.ptr)
 
 
-@_device_call
+@_ends_call
 def symi_adamw_step(ctx, opt, hp, grad_scale, seed):
     _check(lib().symi_adamw_step(ctx.ptr, opt.ptr, ctypes.byref(hp),
                                  None if grad_scale is None else _dev(grad_scale, F32, "grad_scale", 1),
                                  int(seed) & 0xffffffff, _stream()), "symi_adamw_step")
 
 
-@_device_call
+@_ends_call
 def symi_adamw_decode(ctx, opt, m, v):
     n = symi_adamw_values(opt)
     _check(lib().symi_adamw_decode(ctx.ptr, opt.ptr, _dev(m, F32, "m", n), _dev(v, F32, "v", n), _stream()),

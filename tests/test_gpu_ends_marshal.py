@@ -1,0 +1,84 @@
+"""The argument checks of the ends of the step, in C++ and in Python: every tensor of every call at exactly the size it needs,
+refused one element shorter or of another type, with the same words on both paths; options that may be left out; integers
+and numbers of other kinds through the Python path."""
+import numpy as np
+import pytest
+import torch
+
+import harness as Hn
+import paper_2504_19925_amd as symi
+from paper_2504_19925_amd import binding
+
+pytestmark = pytest.mark.gpu
+OTHER = {torch.float32: torch.int32, torch.int32: torch.float32, torch.bfloat16: torch.float16, torch.uint8: torch.int8}
+
+
+def arguments(dtype):
+    T, d, V, ld = 37, 24, 19, 23
+    ctx = symi.symi_create(symi.SymiCfg.make(T, 1, 1, d, 8, 1, 1, 0, dtype))
+    new = lambda *n, dtype=ctx.torch_dtype: torch.zeros(*n, dtype=dtype, device="cuda")   # noqa: E731
+    f32, i32 = torch.float32, torch.int32
+    bytes_ = lambda n: new(n, dtype=torch.uint8)   # noqa: E731
+    other = "bf16" if dtype == "f32" else "f32"      # the logits' type is their own
+    hp = symi.SymiPolicy.make(kl_coef=0.1, dtype=other)
+    z = lambda: new(T, ld, dtype=hp.torch_dtype)   # noqa: E731
+    opt = symi.symi_adamw_create([dict(param=new(300, dtype=f32), grad=new(300, dtype=f32), m=new(300, dtype=f32), v=new(300, dtype=f32))])
+    calls = {
+        "symi_embed_fwd": [new(T, dtype=i32), new(V, d), V, 1.5, new(T, d)],
+        "symi_embed_bwd": [new(T, dtype=i32), new(T, d), V, 1.5, 0, new(V, d, dtype=f32), bytes_(symi.symi_embed_workspace_bytes(ctx, V))],
+        "symi_token_logp": [hp, z(), V, ld, new(T, dtype=i32), new(T, dtype=f32), new(T, dtype=f32)],
+        "symi_policy_loss": [hp, z(), V, ld, new(T, dtype=i32), *(new(T, dtype=f32) for _ in range(5)), new(4, dtype=f32), z(),
+                             bytes_(symi.symi_policy_workspace_bytes(ctx))],
+        "symi_adamw_step": [opt, Hn.make_adam()[0], new(1, dtype=f32), 2 ** 32 - 1],
+        "symi_adamw_decode": [opt, new(512, dtype=f32), new(512, dtype=f32)],
+    }
+    return {n: [ctx, *a] for n, a in calls.items()}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_exact_sizes_and_types(dtype):
+    calls = arguments(dtype)
+    assert set(calls) == set(binding.ENDS) == set(binding._marshal_ends)
+    for name, args in calls.items():
+        fast, call = binding._marshal_ends[name], getattr(symi, name)
+        assert fast(*args) == 0, name
+        call.through_ctypes(*args)
+        for i, t in enumerate(args):
+            if not isinstance(t, torch.Tensor):
+                continue
+            for bad in (t.view(-1)[:-1], t.view(OTHER[t.dtype])):
+                wrong = args[:i] + [bad] + args[i + 1:]
+                assert fast(*wrong) is None, (name, i)
+                said = []
+                for f in (call, call.through_ctypes):
+                    with pytest.raises(symi.SymiError, match="needs at least|expected dtype") as e:
+                        f(*wrong)
+                    said.append(str(e.value))
+                assert said[0] == said[1], name
+        assert fast(*args[:-1]) is None
+        with pytest.raises(TypeError):
+            call(*args[:-1])
+    torch.cuda.synchronize()
+
+
+def test_what_may_be_left_out_and_numbers_of_other_kinds():
+    calls = arguments("f32")
+    for name, i in (("symi_token_logp", 6), ("symi_policy_loss", 12), ("symi_adamw_step", 3)):
+        args = list(calls[name])
+        args[i] = None
+        assert binding._marshal_ends[name](*args) == 0
+        getattr(symi, name).through_ctypes(*args)
+    args = list(calls["symi_policy_loss"])
+    args[7], args[1] = None, symi.SymiPolicy.make(kl_coef=0.0, dtype="bf16")          # no reference: no KL term
+    assert binding._marshal_ends["symi_policy_loss"](*args) == 0
+    args = list(calls["symi_embed_fwd"])
+    args[3], args[4] = np.int64(19), 2                                               # not the plain types: the Python path takes them
+    assert binding._marshal_ends["symi_embed_fwd"](*args) is None
+    symi.symi_embed_fwd(*args)
+    symi.symi_embed_fwd(args[0], tokens=args[1], table=args[2], V=19, scale=2.0, X=args[5])
+    gone = calls["symi_adamw_step"][1]
+    symi.symi_adamw_destroy(gone)
+    for name in ("symi_adamw_step", "symi_adamw_decode"):
+        with pytest.raises(symi.SymiError):
+            getattr(symi, name)(*calls[name])
+    torch.cuda.synchronize()
