@@ -324,7 +324,8 @@ int symi_embed_bwd(const symi_ctx* ctx, const int32_t* tokens, const void* dX, i
  *   pg    = -min(r A, min(max(r, 1 - clip_low), 1 + clip_high) A)
  *   kl    = exp(logp_ref - logp) - (logp_ref - logp) - 1
  *   loss  = sum over tokens of w (pg + kl_coef kl)
- * The caller's weights carry mask and mean: 0 for prompts and padding, 1 / count for a mean. */
+ * The caller's weights carry mask and mean: 0 for prompts and padding, 1 / count for a mean.  A token without an
+ * advantage (A = 0) has pg = 0 whatever its ratio; with kl_coef = 0 the KL is reported and nothing else. */
 typedef struct symi_policy {
   float clip_low, clip_high;  /* >= 0, clip_low <= 1 */
   float kl_coef;              /* >= 0; 0 without logp_ref */

@@ -86,14 +86,14 @@ __device__ __forceinline__ Token token_loss(const PolicyScalars& p, double logp,
   Token k;
   const float r = expf((float)(logp - old));
   k.clipped = (A > 0.f && r > 1.f + p.clip_high) || (A < 0.f && r < 1.f - p.clip_low);
-  k.gain = -A * (k.clipped ? (A > 0.f ? 1.f + p.clip_high : 1.f - p.clip_low) : r);
-  k.slope = k.clipped ? 0.f : -A * r;
+  k.gain = A == 0.f ? 0.f : -A * (k.clipped ? (A > 0.f ? 1.f + p.clip_high : 1.f - p.clip_low) : r);   // also where r is infinite
+  k.slope = k.clipped || A == 0.f ? 0.f : -A * r;
   k.kl = 0.f;
   if (has_ref) {
     const float far = (float)(ref - logp), e = expm1f(far);
     // e^x - x - 1 loses all digits near 0, where it is x^2 / 2 + x^3 / 6 + ...
     k.kl = fabsf(far) < 0.125f ? far * far * (0.5f + far * (1.f / 6 + far * (1.f / 24 + far * (1.f / 120 + far * (1.f / 720))))) : e - far;
-    k.slope -= p.kl_coef * e;
+    if (p.kl_coef > 0.f) k.slope -= p.kl_coef * e;   // a KL that is only looked at may be infinite
   }
   return k;
 }
@@ -257,7 +257,7 @@ __device__ __forceinline__ Slope slope_of(const PolicyScalars& p, float w, float
   return {u, -u / s * 0x1p-24f, m - 24.f};
 }
 __device__ __forceinline__ float4 terms_of(const PolicyScalars& p, float w, const Token& k) {
-  return float4{w * (k.gain + p.kl_coef * k.kl), w * k.gain, w * k.kl, k.clipped ? w : 0.f};
+  return float4{w * (p.kl_coef > 0.f ? k.gain + p.kl_coef * k.kl : k.gain), w * k.gain, w * k.kl, k.clipped ? w : 0.f};
 }
 // In 64 bits, as a ratio exp(logp - logp_old) has the absolute error of logp, and 32 bits leave 5e-7 to a logp of -10; the
 // logarithm is that of a number below 1 in 32 bits (off by 3e-8) and a multiple of ln 2.

@@ -82,3 +82,26 @@ def test_what_may_be_left_out_and_numbers_of_other_kinds():
         with pytest.raises(symi.SymiError):
             getattr(symi, name)(*calls[name])
     torch.cuda.synchronize()
+
+
+def test_a_timing_context_books_every_kernel():
+    T, d, V = 3000, 64, 500
+    ctx = symi.symi_create(symi.SymiCfg.make(T, 1, 1, d, 8, 1, 1, 0, "f32"), symi.CTX_TIMING)
+    new = lambda *n, dtype=torch.float32: torch.zeros(*n, dtype=dtype, device="cuda")   # noqa: E731
+    tokens, table, X = torch.arange(T, device="cuda", dtype=torch.int32) % V, new(V, d), new(T, d)
+    ws = new(max(symi.symi_embed_workspace_bytes(ctx, V), symi.symi_policy_workspace_bytes(ctx)), dtype=torch.uint8)
+    hp, z, one = symi.SymiPolicy.make(dtype="f32"), new(T, V), new(T) + 1
+    opt = symi.symi_adamw_create([dict(param=new(9), grad=new(9), m=new(9), v=new(9))])
+    for call, kernels in (
+            (lambda: symi.symi_embed_fwd(ctx, tokens, table, V, 1.0, X), {"embed_fwd"}),
+            (lambda: symi.symi_embed_bwd(ctx, tokens, X, V, 1.0, 0, table, ws), {"embed_sort", "embed_sum", "embed_join"}),
+            (lambda: symi.symi_token_logp(ctx, hp, z, V, V, tokens, None, one), {"token_logp"}),
+            (lambda: symi.symi_policy_loss(ctx, hp, z, V, V, tokens, one, None, one, one, new(T), new(4), z, ws), {"policy_loss", "policy_sum"}),
+            (lambda: symi.symi_adamw_step(ctx, opt, Hn.make_adam()[0], None, 0), {"adamw"}),
+            (lambda: symi.symi_adamw_decode(ctx, opt, new(256), new(256)), {"adamw_decode"})):
+        symi.symi_timing_reset(ctx)
+        call()
+        torch.cuda.synchronize()
+        seen = {symi.symi_kernel_name(k): symi.symi_timing_read(ctx, k) for k in range(symi.symi_kernel_count())}
+        assert {k for k, (_, n) in seen.items() if n} == kernels
+        assert all(n == 1 and ms > 0 for ms, n in seen.values() if n)

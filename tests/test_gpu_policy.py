@@ -203,6 +203,25 @@ def test_kl_near_zero_and_far():
         assert abs(float(stats[2]) - want) <= tol, (one, float(stats[2]), want)
 
 
+def test_terms_without_a_say_may_be_infinite():
+    """A KL that is only looked at (coefficient 0) and a ratio without an advantage: neither makes the loss or the gradient infinite."""
+    T, V = 3, 40
+    ctx = context(T)
+    b = batch(T, V, V, "f32", 9)
+    b["weight"].fill_(1.0)
+    b["ref"][0] = 300.0                       # exp(300 - logp) is infinite
+    b["old"][1], b["advantage"][1] = -400.0, 0.0
+    hp = symi.SymiPolicy.make(LOW, HIGH, 0.0, dtype="f32")
+    logp, stats, dz = call(ctx, hp, b, V)
+    assert stats[2].isinf() and stats[[0, 1, 3]].isfinite().all() and dz.isfinite().all()
+    assert not dz[1].any()
+    rest = {k: v.clone() for k, v in b.items()}
+    rest["ref"][0], rest["old"][1] = 0.0, 0.0
+    want = oracle(rest, V, hp)
+    assert np.abs(Hn.npf(stats)[:2] - want["stats"][:2]).max() <= 1e-4 * np.abs(want["terms"]).sum()
+    assert np.abs(Hn.npf(dz) - want["dlogits"]).max() <= 1e-4
+
+
 def test_gradient_against_differences():
     """Directional derivatives: (loss(z + h D) - loss(z - h D)) / 2 h of the binary64 loss = <dlogits, D>, for the kernel's
     gradient of fp32 logits (whose errors are below 1e-4 of the summands' sizes); h^2 / 6 of the third derivative is below 1e-7."""
