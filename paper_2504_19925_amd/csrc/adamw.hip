@@ -63,9 +63,9 @@ __host__ __device__ inline uint32_t mix(uint32_t x) {
   return x ^ (x >> 16);
 }
 
-__device__ __forceinline__ float m_value(float c, float a) {
+__device__ __forceinline__ float m_value(float c, float a) {   // of a code with its sign
 #pragma clang fp contract(off)
-  return c * c * M_UNIT * a;
+  return c * fabsf(c) * M_UNIT * a;
 }
 __device__ __forceinline__ float v_value(float c, float a) {
 #pragma clang fp contract(off)
@@ -176,7 +176,7 @@ __device__ __forceinline__ void decode(uint32_t mc, uint32_t vc, float am, float
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float cm = (float)((int)(mc << (24 - 8 * i)) >> 24);
-    m[i] = copysignf(m_value(cm, am), cm);
+    m[i] = m_value(cm, am);
     v[i] = v_value((float)(vc >> (8 * i) & 255u), av);
   }
 }
@@ -233,7 +233,7 @@ struct AdamwBlock {
         v_[i] = v_[i] * h.beta2 + gr * h.keep2 * gr;
         if (CODES) {
           big_m = max(big_m, __float_as_uint(m_[i]) & 0x7fffffffu);
-          big_v = max(big_v, __float_as_uint(v_[i]) & 0x7fffffffu);
+          big_v = max(big_v, __float_as_uint(v_[i]));   // never below 0; a NaN of any sign is on top
         }
       }
     }
@@ -264,26 +264,31 @@ struct AdamwBlock {
     if (!CODES) return;
     const float am_ = scale_of(wave_max(big_m)), av_ = scale_of(wave_max(big_v));
     // the guesses: 127 sqrt(|m| / am), and 255 sqrt(root / sqrt(av)), as root is sqrt(v)
-    const float to_m = 1.f / am_, to_v = 255.f * 255.f * __builtin_amdgcn_rsqf(av_);
+    const float to_m = am_ < 0x1p125f ? __builtin_amdgcn_rcpf(am_) : 1.f / am_;   // the instruction makes 0 of a denormal result
+    const float to_v = 255.f * 255.f * __builtin_amdgcn_rsqf(av_);
     const uint32_t r0 = mix(((t.first_block + (unsigned)block) * 64u + lane) * 0x9E3779B1u + h.key);
     const uint32_t times[4] = {0x3C6EF373u, 0xA54FF53Bu, 0x510E527Fu, 0x9B05688Du};
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      r[i] = r0 * times[i];
+      r[i] ^= r[i] >> 15;
+    }
     uint32_t mc_ = 0, vc_ = 0;
     if (am_ > 0.f) {   // the same in all lanes
+      uint32_t c[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        uint32_t r = r0 * times[i];
-        r ^= r >> 15;
-        const float u = fmaf((float)(r & 0xffffu), 0x1p-16f, 0x1p-17f), x = fabsf(m_[i]);
-        const int c = (int)code_between(x, am_, 127.f * __builtin_amdgcn_sqrtf(x * to_m), 127.f, u, m_value);
-        mc_ |= ((uint32_t)(m_[i] < 0.f ? -c : c) & 255u) << (8 * i);
+        const float u = fmaf((float)(r[i] & 0xffffu), 0x1p-16f, 0x1p-17f), x = fabsf(m_[i]);
+        c[i] = (uint32_t)(int)copysignf(code_between(x, am_, 127.f * __builtin_amdgcn_sqrtf(x * to_m), 127.f, u, m_value), m_[i]);
       }
+      // the lowest byte of each
+      mc_ = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[3], c[2], 0x0c0c0400u), __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400u), 0x05040100u);
     }
     if (av_ > 0.f) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        uint32_t r = r0 * times[i];
-        r ^= r >> 15;
-        const float u = fmaf((float)(r >> 16), 0x1p-16f, 0x1p-17f);
+        const float u = fmaf((float)(r[i] >> 16), 0x1p-16f, 0x1p-17f);
         const float c = code_between(v_[i], av_, __builtin_amdgcn_sqrtf(root[i] * to_v), 255.f, u, v_value);
         vc_ = __builtin_amdgcn_cvt_pk_u8_f32(v_[i] > 0.f ? fmaxf(c, 1.f) : 0.f, i, vc_);
       }
