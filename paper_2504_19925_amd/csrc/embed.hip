@@ -3,8 +3,8 @@
 //
 // The gradient needs the tokens of a row together and in an order that is the same on every run.  One launch sorts: the
 // rows of the table are dealt out to workgroups like cards (the most frequent tokens are neighbours in many vocabularies),
-// and each workgroup reads all tokens twice: it counts the ones of the workgroups before it, where its part of the sorted order
-// begins, and its own by row and wavefront, then gives every token its place.  Counts are integer sums and places come from
+// and each workgroup reads all tokens: it counts the ones of the workgroups before it, where its part of the sorted order
+// begins, keeps its own ones in LDS and counts them by row and wavefront, then gives every one its place.  Counts are integer sums and places come from
 // ballots, so nothing depends on the order of the additions in LDS.
 #include <algorithm>
 #include <type_traits>
@@ -51,7 +51,8 @@ template <bool BF16> struct Piece {
   }
 };
 
-// 2^lg lanes share a token's row and walk it in pieces, R rows at a time.
+// 2^lg lanes share a token's row and walk it in pieces, R rows at a time.  Bound by memory: 65536 rows of d = 4096 in bf16, 5 %
+// padding, from a table of 131072 rows: 148 us, 0.34 GB fetched and 0.54 written (5.9 TB/s).
 template <bool BF16, int R>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_fwd_kernel(const int32_t* __restrict__ tokens,
                                                                   const void* __restrict__ table, void* __restrict__ X,
@@ -83,6 +84,8 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_fwd_kernel(const int32_t*
 
 // Workgroup b of 2^lg: the rows v with v mod 2^lg = b.  span [V]: where each row's tokens begin and end in `order`, which lists
 // the tokens (their places in the batch) row by row, in the order of the wavefronts; rows_of: the rows of the same list; total: its length.
+// Bound by the instructions that look at a token, in every workgroup: 65536 tokens 21 us (vector units busy 58 %), 8192 7 us,
+// most of it the latency of the launch and of three dependent loads.
 constexpr int SORT_KEEP = 1408;       // own tokens that a wavefront keeps from the first reading; with more it reads again
 constexpr int SORT_KEEP_T = 1 << 22;  // in batches of at most this many: place in the batch and place among the own rows in 32 bits
 template <int WAVES, int U>
@@ -253,6 +256,8 @@ __device__ __forceinline__ void fill_rows(const int2* __restrict__ span, long lo
   }
 }
 
+// Bound by memory: 65536 tokens of d = 4096 in bf16 and a table of 65536 rows in 300 us, 0.55 GB fetched and 0.98 written
+// (5.1 TB/s); 8192 of d = 1024, added to the table, 12 us, three loads one after another and the store.
 template <bool BF16, bool ADD>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(
     const void* __restrict__ dX, const int2* __restrict__ span, const int32_t* __restrict__ order,
@@ -351,7 +356,9 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(
   }
 }
 
-// A workgroup: 256 columns of the split runs that begin in one of JOIN_BLOCKS blocks.  The workgroups behind those fill rows.
+// A workgroup: 256 columns of the split runs that begin in one of JOIN_BLOCKS blocks.  The workgroups behind those fill rows: one in front of
+// each join's instead, or one for many joins', took as long or 2 us more.  Bound by latency, four loads one after another (8192 tokens of
+// d = 1024 8 us); the 65536 of d = 4096 above 48 us, 0.04 GB fetched and 0.13 written.
 constexpr int JOIN_WAVES = 8, JOIN_ROWS = 8, JOIN_BLOCKS = 8;
 template <bool ADD>
 __global__ __launch_bounds__(JOIN_WAVES * 64) void embed_join_kernel(const int2* __restrict__ span, const int32_t* __restrict__ rows_of,
@@ -412,7 +419,8 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void embed_join_kernel(const int2*
 
 // Small batches, in one launch without a sort: a workgroup takes 64 pieces of one token's row.  It reads all tokens and does
 // the work of the row if its token is the first of it: every wavefront sums the row's tokens of its part of the batch.  The
-// workgroups behind those look which of their rows of the table the batch has and write zeros to the others.
+// workgroups behind those look which of their rows of the table the batch has and write zeros to the others.  Bound by latency:
+// 1024 tokens of d = 128 in fp32 and 8000 rows (4.6 MB) 5.2 us.
 constexpr int FEW_MAX = 2048;   // tokens
 template <bool BF16, bool ADD, int WAVES, int STEPS>
 __global__ __launch_bounds__(WAVES * 64) void embed_few_kernel(const int32_t* __restrict__ tokens, const void* __restrict__ dX, int T,
