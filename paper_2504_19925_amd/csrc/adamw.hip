@@ -332,8 +332,8 @@ __device__ __forceinline__ void adamw_chunk(const AdamwTensor& t, const AdamwSca
 }
 
 // Bound by memory with 32-bit states: 202 million values, bf16 weights with masters, 1131 us, 3.24 GB fetched and 2.83 written (5.4 TB/s).  With
-// 8-bit ones by memory and vector instructions alike: 539 million 1540 to 1590 us, 5.46 and 3.26 GB (5.6 TB/s), units busy 95 %; 26 million
-// with bf16 gradients 77 us.  Five wavefronts a SIMD instead of four: 2 % less with bf16 gradients, 4 % more with fp32 ones.
+// 8-bit ones by memory and vector instructions alike: 539 million 1540 to 1590 us, 5.46 and 3.26 GB (5.6 TB/s), units busy all the time;
+// 26 million with bf16 gradients 77 us.  Five wavefronts a SIMD instead of four: 2 % less with bf16 gradients, 4 % more with fp32 ones.
 __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwTensor* __restrict__ tensors,
                                                               const AdamwChunk* __restrict__ chunks, AdamwScalars h,
                                                               const float* __restrict__ grad_scale) {
@@ -355,7 +355,7 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwTensor*
   }
 }
 
-// A chunk is `parts` workgroups: two of two rounds each where there are whole chunks (539 million values 968 -> 908 us, 5.9 TB/s,
+// A chunk is `parts` workgroups: two of two rounds each where there are whole chunks (539 million values 968 -> 908 us, 6.0 TB/s,
 // 26 million 54.8 -> 51.0; four of one round 918 and 52.2), else one of one (6.3 million 11.6 us, 16.8 beside idle ones).
 constexpr int DECODE_ROUNDS = 2;
 __global__ __launch_bounds__(ADAMW_THREADS) void adamw_decode_kernel(const AdamwTensor* __restrict__ tensors,
