@@ -356,40 +356,47 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(
   }
 }
 
-// A workgroup: 256 columns of the split runs that begin in one of JOIN_BLOCKS blocks.  The workgroups behind those fill rows: one in front of
-// each join's instead, or one for many joins', took as long or 2 us more.  Bound by latency, four loads one after another (8192 tokens of
-// d = 1024 8 us); the 65536 of d = 4096 above 48 us, 0.04 GB fetched and 0.13 written.
-constexpr int JOIN_WAVES = 8, JOIN_ROWS = 8, JOIN_BLOCKS = 8;
+// Runs of more than JOIN_LONG shares: a workgroup takes 256 columns of those that begin in one of LONG_BLOCKS blocks, its wavefronts
+// a part of the shares each.  The others: a wavefront takes 256 columns of those that begin in one of JOIN_BLOCKS blocks.  The workgroups
+// behind those fill rows (between them instead they took as long).  Bound by latency, four loads one after another.  Joins of 8192
+// tokens of d = 1024, 65536 of 4096 and 30000 of 2048 in fp32, 300 rows, all in workgroups of eight blocks : so, us: 9.1 : 8.0,
+// 31 : 20, 16 : 9.6; with JOIN_BLOCKS 8 8.9, 21, 9.7, with 1 8, 25, 11.8.
+constexpr int JOIN_WAVES = 8, JOIN_ROWS = 8, JOIN_BLOCKS = 4, JOIN_LONG = 16, LONG_BLOCKS = 64;
 template <bool ADD>
 __global__ __launch_bounds__(JOIN_WAVES * 64) void embed_join_kernel(const int2* __restrict__ span, const int32_t* __restrict__ rows_of,
                                                                      const int32_t* __restrict__ total_of, const float* __restrict__ partial,
-                                                                     int size, int d, int C, int joins, int columns, long long fill_from,
-                                                                     long long fill_to, float scale,
+                                                                     int size, int d, int C, int long_groups, int join_groups, int columns,
+                                                                     long long fill_from, long long fill_to, float scale,
                                                                      float* __restrict__ dTable) {
   __shared__ float4 share[JOIN_WAVES][64];
   const long long group = (long long)blockIdx.y * gridDim.x + blockIdx.x;
-  if (group >= (long long)joins * columns) {
-    fill_rows<JOIN_WAVES * 64>(span, fill_from + (group - (long long)joins * columns) * FILL_PIECES, fill_to, d, dTable);
+  if (group >= join_groups) {
+    fill_rows<JOIN_WAVES * 64>(span, fill_from + (group - join_groups) * FILL_PIECES, fill_to, d, dTable);
     return;
   }
-  const int block = (int)(group / columns), column = (int)(group % columns);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool is_long = group < long_groups;
+  const int unit = is_long ? (int)group : ((int)group - long_groups) * JOIN_WAVES + wave;
+  const int blocks = is_long ? LONG_BLOCKS : JOIN_BLOCKS, column = unit % columns;
   const int total = *total_of;
   // the run across the end of a block
-  const long long hi = ((long long)block * JOIN_BLOCKS + lane + 1) * SHARE;
+  const long long hi = ((long long)(unit / columns) * blocks + lane + 1) * SHARE;
   const int row_of = rows_of[min(hi, (long long)size) - 1];   // beyond the total: anything
-  const bool there = lane < JOIN_BLOCKS && hi < total;
+  const bool there = lane < blocks && hi < total;
   const int2 s = there ? span[row_of] : int2{0, 0};
-  unsigned long long todo = __ballot(there && s.y > hi && s.x >= hi - SHARE && is_split(s, C, share_of(s)));
+  const int S_of = share_of(s), count_of = (s.y - 1) / S_of - s.x / S_of + 1;
+  unsigned long long todo = __ballot(there && s.y > hi && s.x >= hi - SHARE && is_split(s, C, S_of) && (count_of > JOIN_LONG) == is_long);
   const int c = (column * 64 + lane) * 4;
   const bool live = c < d;
   for (; todo; todo &= todo - 1) {
-    const int i = (int)__builtin_ctzll(todo), row = __builtin_amdgcn_readlane(row_of, i), stop = __builtin_amdgcn_readlane(s.y, i);
+    const int i = (int)__builtin_ctzll(todo), row = __builtin_amdgcn_readlane(row_of, i);
     // shares: slot 1 of this block, slot 0 of the blocks at the multiples of S behind it
-    const int start = __builtin_amdgcn_readlane(s.x, i), S = share_of(int2{start, stop});
-    const int count = (stop - 1) / S - start / S + 1;
+    const int start = __builtin_amdgcn_readlane(s.x, i), S = __builtin_amdgcn_readlane(S_of, i), count = __builtin_amdgcn_readlane(count_of, i);
     const auto block_of = [&](int k) { return (k == 0 ? start : (start / S + k) * S) / SHARE; };
-    const int each = (count + JOIN_WAVES - 1) / JOIN_WAVES, begin = wave * each, end = min(begin + each, count);
+    const int each = is_long ? (count + JOIN_WAVES - 1) / JOIN_WAVES : count, begin = is_long ? wave * each : 0, end = min(begin + each, count);
+    float* const to = dTable + (long long)row * d + c;
+    f32x4_f32 old = {0.f, 0.f, 0.f, 0.f};
+    if (ADD && live && begin == 0) old = *reinterpret_cast<const f32x4_f32*>(to);
     float4 sum = {0.f, 0.f, 0.f, 0.f};
     for (int k0 = begin; k0 < end && live; k0 += JOIN_ROWS) {
       float4 x[JOIN_ROWS];
@@ -400,20 +407,21 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void embed_join_kernel(const int2*
       for (int u = 0; u < JOIN_ROWS; ++u)
         if (k0 + u < end) { sum.x += x[u].x; sum.y += x[u].y; sum.z += x[u].z; sum.w += x[u].w; }
     }
-    share[wave][lane] = sum;
-    __syncthreads();
-    if (wave == 0 && live) {
-      float y[4] = {sum.x, sum.y, sum.z, sum.w};
+    float y[4] = {sum.x, sum.y, sum.z, sum.w};
+    if (is_long) {
+      share[wave][lane] = sum;
+      __syncthreads();
 #pragma unroll
       for (int w = 1; w < JOIN_WAVES; ++w) {
         const float4 o = share[w][lane];
         y[0] += o.x; y[1] += o.y; y[2] += o.z; y[3] += o.w;
       }
-      float* const to = dTable + (long long)row * d + c;
-      if (ADD) put_row(to, y, scale, *reinterpret_cast<const f32x4_f32*>(to));
+      __syncthreads();
+    }
+    if (live && begin == 0) {
+      if (ADD) put_row(to, y, scale, old);
       else put_row(to, y, scale);
     }
-    __syncthreads();
   }
 }
 
@@ -643,11 +651,12 @@ extern "C" int symi_embed_bwd(const symi_ctx* ctx, const int32_t* tokens, const 
   else SUM(false, false);
 #undef SUM
   {
-    const int joins = cdiv(cfg->T, SHARE * JOIN_BLOCKS), columns = cdiv(cfg->d, 256);
-    const dim3 grid = grid_of((long long)joins * columns + fills(pieces - fill_sum));
+    const int columns = cdiv(cfg->d, 256), long_groups = cdiv(cfg->T, SHARE * LONG_BLOCKS) * columns;
+    const int join_groups = long_groups + cdiv((long long)cdiv(cfg->T, SHARE * JOIN_BLOCKS) * columns, JOIN_WAVES);
+    const dim3 grid = grid_of(join_groups + fills(pieces - fill_sum));
 #define JOIN(ADD)                                                                                         \
   SYMI_TIMED(ctx, K_EMBED_JOIN, st, (embed_join_kernel<ADD><<<grid, JOIN_WAVES * 64, 0, st>>>(            \
-      span, ints(L.rows_of), ints(L.count), partial, cfg->T, cfg->d, L.chunk, joins, columns, fill_sum, pieces, scale, dTable)))
+      span, ints(L.rows_of), ints(L.count), partial, cfg->T, cfg->d, L.chunk, long_groups, join_groups, columns, fill_sum, pieces, scale, dTable)))
     if (accumulate) JOIN(true);
     else JOIN(false);
 #undef JOIN
