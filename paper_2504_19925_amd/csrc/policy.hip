@@ -492,7 +492,7 @@ static void by_length(int pieces, F f) {
   else if (pieces <= 512) f(Int<128>(), Int<8>());
   else if (pieces <= 256 * 4) f(Int<256>(), Int<4>());
   else if (pieces <= 256 * 8) f(Int<256>(), Int<8>());
-  else if (pieces <= 3072) f(Int<512>(), Int<8>());
+  else if (pieces <= 3000) f(Int<512>(), Int<8>());
   else if (pieces <= 512 * 9) f(Int<512>(), Int<12>());
   else if (pieces <= 512 * 16) f(Int<512>(), Int<16>());
   else if (pieces <= 12800) f(Int<1024>(), Int<8>());

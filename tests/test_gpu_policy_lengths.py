@@ -8,8 +8,8 @@ import paper_2504_19925_amd as symi
 from tests.test_gpu_policy import HIGH, KL, LOW, batch, call, check, context
 
 pytestmark = pytest.mark.gpu
-PIECES = [63, 64, 255, 256, 257, 511, 512, 513, 1023, 1024, 1025, 2047, 2048, 2049, 3071, 3072, 3073, 4607, 4608, 4609, 8191, 8192, 8193,
-          16383, 16384, 16385, 24577]
+PIECES = [63, 64, 255, 256, 257, 511, 512, 513, 1023, 1024, 1025, 2047, 2048, 2049, 2999, 3000, 3001, 4607, 4608, 4609, 8191, 8192, 8193,
+          12800, 12801, 16383, 16384, 16385, 24577]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
