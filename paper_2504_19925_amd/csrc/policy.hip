@@ -109,6 +109,21 @@ struct PolicyArgs {
   PolicyScalars p;
 };
 
+// The gradient of a logit is minus 2^(t - m), with u more for the chosen token.  The power is taken as the square of its root:
+// 2^(t - m) itself would become 0 below 2^-126, where the gradient in single precision need not be 0, and an exponent that is
+// moved up instead (m less a constant) loses the last bits of those near 0, which are most of the sum.  Halves are exact.
+struct Slope {
+  float u, minus, half_c, half_m;
+  __device__ __forceinline__ float of(float x) const {
+    const float root = exp2_(fmaf(x, half_c, -half_m));
+    return minus * root * root;
+  }
+};
+__device__ __forceinline__ Slope slope_of(const PolicyScalars& p, float w, float slope, float m, float s) {
+  const float u = p.scale * p.inv_temp * w * slope;
+  return {u, -u / s, 0.5f * p.c, 0.5f * m};
+}
+
 // What a workgroup does with a row of logits, every thread NV pieces of it at a time.
 template <bool BF16, bool ONCE, int THREADS, int NV>
 struct Row {
@@ -151,9 +166,9 @@ struct Row {
     join(m, s, edge * c, 1.f);
     if (e == token) *chosen = edge;
   }
-  __device__ __forceinline__ void give_edge(Elem* dz, float u, float minus, float ref) {
+  __device__ __forceinline__ void give_edge(Elem* dz, const Slope& d) {
     const int e = edge_column();
-    if (e >= 0) dz[e] = P::element(minus * exp2_(fmaf(edge, c, -ref)) + (e == token ? u : 0.f));
+    if (e >= 0) dz[e] = P::element(d.of(edge) + (e == token ? d.u : 0.f));
   }
   // the pieces q0 + tid, q0 + THREADS + tid, ... below `stop`
   __device__ __forceinline__ void fetch(int q0, int stop) {
@@ -195,7 +210,7 @@ struct Row {
     }
   }
   // writes the gradient of what is held; dz: of the row's first logit
-  __device__ __forceinline__ void give(int q0, int stop, Elem* dz, float u, float minus, float ref) {
+  __device__ __forceinline__ void give(int q0, int stop, Elem* dz, const Slope& d) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int at = q0 + i * THREADS + tid;
@@ -204,11 +219,11 @@ struct Row {
       forget(r[i]);
       P::unpack(r[i], x);
 #pragma unroll
-      for (int k = 0; k < N; ++k) x[k] = minus * exp2_(fmaf(x[k], c, -ref));
+      for (int k = 0; k < N; ++k) x[k] = d.of(x[k]);
       if (at == q) {
 #pragma unroll
         for (int k = 0; k < N; ++k)
-          if (k == j) x[k] += u;
+          if (k == j) x[k] += d.u;
       }
       if (at < stop) P::store(dz + head + (long long)at * N, P::pack(x));
     }
@@ -247,15 +262,6 @@ __device__ __forceinline__ void clear(typename Piece<BF16>::Elem* p, int n, int 
   for (int j = tail + tid; j < n; j += threads) p[j] = 0;
 }
 
-// The gradient of a logit is minus 2^(t - from), with u more for the chosen token.  2^24 moves from the factor into the
-// exponent: the power is then no denormal number, which would become 0, where the gradient in single precision is not 0.
-struct Slope {
-  float u, minus, from;
-};
-__device__ __forceinline__ Slope slope_of(const PolicyScalars& p, float w, float slope, float m, float s) {
-  const float u = p.scale * p.inv_temp * w * slope;
-  return {u, -u / s * 0x1p-24f, m - 24.f};
-}
 __device__ __forceinline__ float4 terms_of(const PolicyScalars& p, float w, const Token& k) {
   return float4{w * (p.kl_coef > 0.f ? k.gain + p.kl_coef * k.kl : k.gain), w * k.gain, w * k.kl, k.clipped ? w : 0.f};
 }
@@ -315,11 +321,11 @@ __global__ __launch_bounds__(THREADS, NV <= 8 ? 8 : 4) void policy_kernel(Policy
   if (tid == 0) g.terms[t] = terms_of(g.p, w, k);
   if (!GRAD) return;
   const Slope d = slope_of(g.p, w, k.slope, m, s);
-  row.give(last, end, dz, d.u, d.minus, d.from);
-  row.give_edge(dz, d.u, d.minus, d.from);
+  row.give(last, end, dz, d);
+  row.give_edge(dz, d);
   for (int q0 = (last - 1) / R::STEP * R::STEP; last && q0 >= 0; q0 -= R::STEP) {   // what was read last is the nearest
     row.fetch(q0, min(q0 + R::STEP, last));
-    row.give(q0, min(q0 + R::STEP, last), dz, d.u, d.minus, d.from);
+    row.give(q0, min(q0 + R::STEP, last), dz, d);
   }
   clear<BF16>(dz + g.V, g.ld - g.V, tid, THREADS);
 }
@@ -432,9 +438,9 @@ __global__ __launch_bounds__(SUM_SPLIT_THREADS) void policy_apply_kernel(PolicyA
   const double lp = logp_of(g.p, parts.chosen[t], m, s);
   const Token k = token_loss(g.p, lp, g.logp_old[t], g.logp_ref != nullptr, g.logp_ref ? g.logp_ref[t] : 0.f, g.advantage[t]);
   const Slope d = slope_of(g.p, w, k.slope, m, s);
-  row.give_edge(dz, d.u, d.minus, d.from);
+  row.give_edge(dz, d);
   for (int q0 = 0;;) {
-    row.give(q0, end, dz, d.u, d.minus, d.from);
+    row.give(q0, end, dz, d);
     if ((q0 += R::STEP) >= end) break;
     row.fetch(q0, end);
   }
