@@ -1,8 +1,8 @@
 // symi_token_logp / symi_policy_loss: log probabilities of the chosen tokens, the clipped policy loss with a KL term, and
 // the gradient of the logits.
 //
-// Per row of logits, in base 2 with c = log2(e) / temperature: t_j = c z_j, m = max t_j, s = sum 2^(t_j - m),
-//   logp = ln 2 (t_a - m) - ln s,   dlogits_j = u ([j = a] - 2^(t_j - m) / s),   u = grad_scale w / temperature dL/dlogp.
+// Per row of logits, in base 2 with c = log2(e) / temperature: m = max z_j, s = sum 2^(c (z_j - m)),
+//   logp = ln 2 c (z_a - m) - ln s,   dlogits_j = u ([j = a] - 2^(c (z_j - m)) / s),   u = grad_scale w / temperature dL/dlogp.
 // The weights are the caller's, so u needs nothing from other rows: one workgroup takes a row from its logits to
 // their gradient.  Statistics and sums are fp32; the four sums over the rows are taken in 64 bits by one workgroup, in order.
 #include <math.h>
@@ -69,11 +69,22 @@ __device__ __forceinline__ void forget(Raw& r) { asm volatile("" : "+v"(r)); }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }   // below 2^-126: 0
 
-// (m, s) of a set of t: m its largest value, s the sum of 2^(t - m).
-__device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
+// c (x - ref) in one operation, as c x - by with by = c ref rounded, where what the rounding makes of the power can be put right afterwards: by
+// `rest`, 2^(by - c ref) to first order (the second is below 2^-25).  Elsewhere, among masks of -1e10 or -1e30, c x - by may be anything.
+struct Exponent {
+  float by, rest;
+  bool near;
+};
+__device__ __forceinline__ Exponent exponent_of(float ref, float c) {
+  const float by = ref * c;
+  return {by, fmaf(fmaf(ref, c, -by), -0.693147181f, 1.f), fabsf(by) < 4096.f};
+}
+
+// (m, s) of a set of logits: m the largest, s the sum of 2^(c (z - m)).
+__device__ __forceinline__ void join(float& m, float& s, float m2, float s2, float c) {
   const float top = fmaxf(m, m2);
-  const float ref = top == -INFINITY ? 0.f : top;   // nothing but -inf so far: 2^(-inf - 0) = 0
-  s = s * exp2_(m - ref) + s2 * exp2_(m2 - ref);
+  const float ref = top == -INFINITY ? 0.f : top;   // nothing but -inf so far: 2^(c (-inf - 0)) = 0
+  s = s * exp2_((m - ref) * c) + s2 * exp2_((m2 - ref) * c);
   m = top;
 }
 
@@ -109,19 +120,20 @@ struct PolicyArgs {
   PolicyScalars p;
 };
 
-// The gradient of a logit is minus 2^(t - m), with u more for the chosen token.  The power is taken as the square of its root:
-// 2^(t - m) itself would become 0 below 2^-126, where the gradient in single precision need not be 0, and an exponent that is
+// The gradient of a logit is minus 2^(c (z - m)), with u more for the chosen token.  The power is taken as the square of its root:
+// 2^(c (z - m)) itself would become 0 below 2^-126, where the gradient in single precision need not be 0, and an exponent that is
 // moved up instead (m less a constant) loses the last bits of those near 0, which are most of the sum.  Halves are exact.
 struct Slope {
-  float u, minus, half_c, half_m;
-  __device__ __forceinline__ float of(float x) const {
-    const float root = exp2_(fmaf(x, half_c, -half_m));
-    return minus * root * root;
-  }
+  float u, minus, half_c, half_by, m;   // near: fma(z, half_c, -half_by) is the root's exponent
+  bool near;
+  __device__ __forceinline__ float of(float root) const { return minus * root * root; }
+  __device__ __forceinline__ float of_near(float x) const { return of(exp2_(fmaf(x, half_c, -half_by))); }
+  __device__ __forceinline__ float of_far(float x) const { return of(exp2_((x - m) * half_c)); }
 };
 __device__ __forceinline__ Slope slope_of(const PolicyScalars& p, float w, float slope, float m, float s) {
   const float u = p.scale * p.inv_temp * w * slope;
-  return {u, -u / s, 0.5f * p.c, 0.5f * m};
+  const Exponent e = exponent_of(m, p.c);
+  return {u, -u / s * (e.near ? e.rest : 1.f), 0.5f * p.c, 0.5f * e.by, m, e.near};
 }
 
 // What a workgroup does with a row of logits, every thread NV pieces of it at a time.
@@ -163,12 +175,12 @@ struct Row {
   __device__ __forceinline__ void take_edge(float& m, float& s, float* chosen) {
     const int e = edge_column();
     if (e < 0) return;
-    join(m, s, edge * c, 1.f);
+    join(m, s, edge, 1.f, c);
     if (e == token) *chosen = edge;
   }
   __device__ __forceinline__ void give_edge(Elem* dz, const Slope& d) {
     const int e = edge_column();
-    if (e >= 0) dz[e] = P::element(d.of(edge) + (e == token ? d.u : 0.f));
+    if (e >= 0) dz[e] = P::element((d.near ? d.of_near(edge) : d.of_far(edge)) + (e == token ? d.u : 0.f));
   }
   // the pieces q0 + tid, q0 + THREADS + tid, ... below `stop`
   __device__ __forceinline__ void fetch(int q0, int stop) {
@@ -195,10 +207,11 @@ struct Row {
           if (k == j) *chosen = x[k];
       }
     }
-    top *= c;
     const float base = fmaxf(m, top), ref = base == -INFINITY ? 0.f : base;   // nothing but -inf so far
-    s *= exp2_(m - ref);
+    s *= exp2_((m - ref) * c);
     m = base;
+    const Exponent e = exponent_of(ref, c);
+    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if (q0 + i * THREADS >= stop) continue;
@@ -206,11 +219,43 @@ struct Row {
       forget(r[i]);
       P::unpack(r[i], x);
 #pragma unroll
-      for (int k = 0; k < N; ++k) s += exp2_(fmaf(x[k], c, -ref));
+      for (int k = 0; k < N; ++k) sum += exp2_(fmaf(x[k], c, -e.by));
     }
+    sum *= e.rest;
+    if (__builtin_expect(__ballot(!e.near) != 0, 0)) {   // anew; what is held stays as it is
+      float far = 0.f;
+#pragma unroll 1
+      for (int at = q0 + tid; at < min(stop, q0 + STEP); at += THREADS) {
+        float x[N];
+        P::unpack(P::template load<ONCE>(z + (long long)at * N), x);
+#pragma unroll
+        for (int k = 0; k < N; ++k) far += exp2_((x[k] - ref) * c);
+      }
+      if (!e.near) sum = far;
+    }
+    s += sum;
+  }
+  __device__ __forceinline__ void give_piece(int at, float (&x)[N], Elem* dz, const Slope& d) {
+    if (at == q) {
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (k == j) x[k] += d.u;
+    }
+    P::store(dz + head + (long long)at * N, P::pack(x));
   }
   // writes the gradient of what is held; dz: of the row's first logit
   __device__ __forceinline__ void give(int q0, int stop, Elem* dz, const Slope& d) {
+    if (__builtin_expect(!d.near, 0)) {
+#pragma unroll 1
+      for (int at = q0 + tid; at < min(stop, q0 + STEP); at += THREADS) {
+        float x[N];
+        P::unpack(P::template load<ONCE>(z + (long long)at * N), x);
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = d.of_far(x[k]);
+        give_piece(at, x, dz, d);
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int at = q0 + i * THREADS + tid;
@@ -219,26 +264,21 @@ struct Row {
       forget(r[i]);
       P::unpack(r[i], x);
 #pragma unroll
-      for (int k = 0; k < N; ++k) x[k] = d.of(x[k]);
-      if (at == q) {
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-          if (k == j) x[k] += d.u;
-      }
-      if (at < stop) P::store(dz + head + (long long)at * N, P::pack(x));
+      for (int k = 0; k < N; ++k) x[k] = d.of_near(x[k]);
+      if (at < stop) give_piece(at, x, dz, d);
     }
   }
 };
 
-__device__ __forceinline__ void join_wave(float& m, float& s) {
+__device__ __forceinline__ void join_wave(float& m, float& s, float c) {
 #pragma unroll
-  for (int k = 32; k >= 1; k >>= 1) join(m, s, __shfl_xor(m, k, 64), __shfl_xor(s, k, 64));
+  for (int k = 32; k >= 1; k >>= 1) join(m, s, __shfl_xor(m, k, 64), __shfl_xor(s, k, 64), c);
 }
 // (m, s) of a workgroup, in every thread.
 template <int THREADS>
-__device__ __forceinline__ void join_threads(float& m, float& s) {
+__device__ __forceinline__ void join_threads(float& m, float& s, float c) {
   __shared__ float ms[THREADS / 64], ss[THREADS / 64];
-  join_wave(m, s);
+  join_wave(m, s, c);
   if (THREADS > 64 && (threadIdx.x & 63) == 0) {
     ms[threadIdx.x >> 6] = m;
     ss[threadIdx.x >> 6] = s;
@@ -248,7 +288,7 @@ __device__ __forceinline__ void join_threads(float& m, float& s) {
   m = ms[0];
   s = ss[0];
 #pragma unroll
-  for (int k = 1; k < THREADS / 64; ++k) join(m, s, ms[k], ss[k]);
+  for (int k = 1; k < THREADS / 64; ++k) join(m, s, ms[k], ss[k], c);
 }
 
 // Zeros to p[0 .. n).
@@ -266,11 +306,15 @@ __device__ __forceinline__ float4 terms_of(const PolicyScalars& p, float w, cons
   return float4{w * (p.kl_coef > 0.f ? k.gain + p.kl_coef * k.kl : k.gain), w * k.gain, w * k.kl, k.clipped ? w : 0.f};
 }
 // In 64 bits, as a ratio exp(logp - logp_old) has the absolute error of logp, and 32 bits leave 5e-7 to a logp of -10; the
-// logarithm is that of a number below 1 in 32 bits (off by 3e-8) and a multiple of ln 2.
+// logarithm is that of a number near 1 in 32 bits (off by 3e-8) and a multiple of ln 2.
 __device__ __forceinline__ double logp_of(const PolicyScalars& p, float za, float m, float s) {
   int k;
-  const float f = frexpf(s, &k);
-  return (fma((double)za, (double)p.c, -(double)m) - k) * 0.693147180559945309 - (double)logf(f);
+  float f = frexpf(s, &k);
+  if (f < 0.70710678f) {   // nearer to 1: the logarithm of 1 is 0
+    f *= 2.f;
+    k -= 1;
+  }
+  return (((double)za - (double)m) * (double)p.c - k) * 0.693147180559945309 - (double)logf(f);
 }
 
 // A workgroup of THREADS takes a row.  What fits is read once and stays in registers from the logits to their gradient; of a
@@ -313,7 +357,7 @@ __global__ __launch_bounds__(THREADS, NV <= 8 ? 8 : 4) void policy_kernel(Policy
   row.fetch_edge();
   row.take(last, end, m, s, &chosen);
   row.take_edge(m, s, &chosen);
-  join_threads<THREADS>(m, s);
+  join_threads<THREADS>(m, s, g.p.c);
   const double lp = logp_of(g.p, chosen, m, s);
   if (tid == 0) g.logp[t] = (float)lp;
   if (!g.terms) return;
@@ -363,7 +407,7 @@ __global__ __launch_bounds__(64) void policy_part_kernel(PolicyArgs g, Parts par
   row.fetch_edge();
   row.take(last, end, m, s, parts.chosen + t);
   row.take_edge(m, s, parts.chosen + t);
-  join_wave(m, s);
+  join_wave(m, s, g.p.c);
   if (threadIdx.x == 0) parts.ms[t * WAVES + wave] = float2{m, s};
 }
 
@@ -386,14 +430,14 @@ __device__ __forceinline__ void add_terms(double (&sum)[4], float* __restrict__ 
 
 // m and s of a row: those of its wavefronts, joined in order.
 template <int WAVES, class Load>
-__device__ __forceinline__ void join_waves(float& m, float& s, Load load) {
+__device__ __forceinline__ void join_waves(float& m, float& s, float c, Load load) {
   float2 x = load(0);
   m = x.x;
   s = x.y;
 #pragma unroll
   for (int k = 1; k < WAVES; ++k) {
     x = load(k);
-    join(m, s, x.x, x.y);
+    join(m, s, x.x, x.y, c);
   }
 }
 
@@ -408,7 +452,7 @@ __global__ __launch_bounds__(SUM_SPLIT_THREADS) void policy_apply_kernel(PolicyA
       const float w = g.weight[t];
       double lp = 0.;
       if (w != 0.f && (unsigned)g.action[t] < (unsigned)g.V) {
-        join_waves<WAVES>(m, s, [&](int k) { return parts.ms[(long long)t * WAVES + k]; });
+        join_waves<WAVES>(m, s, g.p.c, [&](int k) { return parts.ms[(long long)t * WAVES + k]; });
         lp = logp_of(g.p, parts.chosen[t], m, s);
         const Token k = token_loss(g.p, lp, g.logp_old[t], g.logp_ref != nullptr, g.logp_ref ? g.logp_ref[t] : 0.f, g.advantage[t]);
         const float4 x = terms_of(g.p, w, k);
@@ -434,7 +478,7 @@ __global__ __launch_bounds__(SUM_SPLIT_THREADS) void policy_apply_kernel(PolicyA
   if (wave == 0) clear<BF16>(dz + g.V, g.ld - g.V, row.tid, 64);
   row.fetch(0, end);
   row.fetch_edge();
-  join_waves<WAVES>(m, s, [&](int k) { return parts.ms[t * WAVES + k]; });
+  join_waves<WAVES>(m, s, g.p.c, [&](int k) { return parts.ms[t * WAVES + k]; });
   const double lp = logp_of(g.p, parts.chosen[t], m, s);
   const Token k = token_loss(g.p, lp, g.logp_old[t], g.logp_ref != nullptr, g.logp_ref ? g.logp_ref[t] : 0.f, g.advantage[t]);
   const Slope d = slope_of(g.p, w, k.slope, m, s);
@@ -482,7 +526,7 @@ static PolicyWs policy_ws(const symi_cfg* c) {
 }
 
 static PolicyScalars scalars(const symi_policy* hp) {
-  return {hp->clip_low, hp->clip_high, hp->kl_coef, hp->inv_temperature, hp->grad_scale, (float)(1.4426950408889634 * hp->inv_temperature)};
+  return {hp->clip_low, hp->clip_high, hp->kl_coef, hp->inv_temperature, hp->grad_scale, (float)std::min(1.4426950408889634 * hp->inv_temperature, 3.4028234663852886e38)};
 }
 
 // The workgroup for a row with its gradient: f(THREADS, NV).  The smallest that holds the row comes first, with four to 16 pieces a
