@@ -120,10 +120,23 @@ class SymiAdamWTensor(ctypes.Structure):
 
 
 class SymiAdamW:
-    """Handle of a symi_adamw (symi_adamw_create); holds the table and the tensors whose memory it describes."""
+    """Handle of a symi_adamw (symi_adamw_create); holds the table and the tensors whose memory it describes.
+
+    It may be dropped while steps are queued, on whatever streams: the allocator keeps the memory until they are done.  A
+    captured step is not seen again when its graph is replayed, so the handle has to outlive the graph."""
 
     def __init__(self, ptr, tensors, table):
         self.ptr, self.tensors, self.table = ptr, tensors, table
+        self.stream, self.streams = None, set()   # the last call's stream; all of them
+
+    def use_on(self, stream):
+        """Tells the allocator, once for each stream, that work on it uses the memory."""
+        at = stream.cuda_stream
+        if at not in self.streams:
+            for x in [self.table] + [x for t in self.tensors for x in t.values() if isinstance(x, torch.Tensor)]:
+                x.record_stream(stream)
+            self.streams.add(at)
+        self.stream = at
 
     def __del__(self):
         try:
@@ -689,7 +702,9 @@ def symi_adamw_create(tensors):
     table, out = torch.empty(size, dtype=torch.uint8, device="cuda"), ctypes.c_void_p()
     _check(lib().symi_adamw_create(entries, len(tensors), ctypes.c_void_p(table.data_ptr()), ctypes.byref(out), _stream()),
            "symi_adamw_create")
-    return SymiAdamW(out, tensors, table)
+    opt = SymiAdamW(out, tensors, table)
+    opt.use_on(torch.cuda.current_stream())
+    return opt
 
 
 def symi_adamw_destroy(opt):
@@ -704,6 +719,7 @@ def symi_adamw_values(opt):
 
 @_ends_call
 def symi_adamw_step(ctx, opt, hp, grad_scale, seed):
+    opt.use_on(torch.cuda.current_stream())
     _check(lib().symi_adamw_step(ctx.ptr, opt.ptr, ctypes.byref(hp),
                                  None if grad_scale is None else _dev(grad_scale, F32, "grad_scale", 1),
                                  int(seed) & 0xffffffff, _stream()), "symi_adamw_step")
@@ -711,6 +727,7 @@ def symi_adamw_step(ctx, opt, hp, grad_scale, seed):
 
 @_ends_call
 def symi_adamw_decode(ctx, opt, m, v):
+    opt.use_on(torch.cuda.current_stream())
     n = symi_adamw_values(opt)
     _check(lib().symi_adamw_decode(ctx.ptr, opt.ptr, _dev(m, F32, "m", n), _dev(v, F32, "v", n), _stream()),
            "symi_adamw_decode")

@@ -40,7 +40,7 @@ PyTypeObject* g_ctx_type = nullptr;    // binding.SymiCtx
 PyTypeObject* g_adam_type = nullptr;   // binding.SymiAdam
 PyTypeObject* g_policy_type = nullptr; // binding.SymiPolicy
 PyTypeObject* g_adamw_type = nullptr;  // binding.SymiAdamW
-PyObject *g_ptr = nullptr, *g_cfg = nullptr;   // interned attribute names
+PyObject *g_ptr = nullptr, *g_cfg = nullptr, *g_stream = nullptr;   // interned attribute names
 
 // one argument of a C call: converts to the type of the parameter it is passed for
 struct Val {
@@ -138,6 +138,7 @@ class Call {
     ok = ok && p && p != Py_None && read_ctypes(p, v.p) && v.p;
     Py_XDECREF(p);
     if (!ok) PyErr_Clear();
+    ok = ok && on_its_stream(a_[i]);
     return v;
   }
   template <class Fn, size_t N>
@@ -147,6 +148,14 @@ class Call {
   }
 
  private:
+  // whether the handle's last call was on the current stream; else binding.py notes the new one first
+  static bool on_its_stream(PyObject* opt) {
+    PyObject* s = PyObject_GetAttr(opt, g_stream);
+    const bool is = s && PyLong_Check(s) && PyLong_AsVoidPtr(s) == static_cast<void*>(c10::hip::getCurrentHIPStream().stream());
+    Py_XDECREF(s);
+    if (PyErr_Occurred()) PyErr_Clear();
+    return is;
+  }
   Val tensor(int i, at::ScalarType type, long long n) {
     Val v;
     if (!ok) return v;
@@ -394,6 +403,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};
 PyMODINIT_FUNC PyInit__marshal() {
   g_ptr = PyUnicode_InternFromString("ptr");
   g_cfg = PyUnicode_InternFromString("cfg");
-  if (!g_ptr || !g_cfg) return nullptr;
+  g_stream = PyUnicode_InternFromString("stream");
+  if (!g_ptr || !g_cfg || !g_stream) return nullptr;
   return PyModule_Create(&module);
 }
