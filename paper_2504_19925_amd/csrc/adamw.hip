@@ -12,6 +12,7 @@
 // which code is taken does not depend on how the compiler fuses them.
 #include <math.h>
 
+#include <algorithm>
 #include <new>
 #include <type_traits>
 #include <vector>
@@ -359,10 +360,12 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwTensor*
 // 26 million 54.8 -> 51.0; four of one round 918 and 52.2), else one of one (6.3 million 11.6 us, 16.8 beside idle ones).
 constexpr int DECODE_ROUNDS = 2;
 __global__ __launch_bounds__(ADAMW_THREADS) void adamw_decode_kernel(const AdamwTensor* __restrict__ tensors,
-                                                                     const AdamwChunk* __restrict__ chunks, int parts,
+                                                                     const AdamwChunk* __restrict__ chunks, int parts, unsigned groups,
                                                                      float* __restrict__ m_out, float* __restrict__ v_out) {
-  const AdamwChunk c = chunks[blockIdx.x / (unsigned)parts];
-  const unsigned part = blockIdx.x % (unsigned)parts;
+  const unsigned group = blockIdx.y * gridDim.x + blockIdx.x;
+  if (group >= groups) return;
+  const AdamwChunk c = chunks[group / (unsigned)parts];
+  const unsigned part = group % (unsigned)parts;
   if (part && !(c.block & WHOLE)) return;
   const AdamwTensor t = tensors[c.tensor];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -564,7 +567,10 @@ extern "C" int symi_adamw_decode(const symi_ctx* ctx, const symi_adamw* opt, flo
   SYMI_REQUIRE(m && v, who, "NULL pointer");
   hipStream_t st = as_stream(stream);
   const int parts = opt->fine ? 1 : ADAMW_ROUNDS / DECODE_ROUNDS;
-  SYMI_TIMED(ctx, K_ADAMW_DECODE, st, (adamw_decode_kernel<<<(unsigned)opt->chunks * parts, ADAMW_THREADS, 0, st>>>(opt->tensors, opt->list, parts, m, v)));
+  // two dimensions beyond 2^20 workgroups: the threads of one end at 2^32, which two workgroups a chunk can reach
+  const unsigned groups = (unsigned)opt->chunks * parts, across = std::min(groups, 1u << 20);
+  SYMI_TIMED(ctx, K_ADAMW_DECODE, st, (adamw_decode_kernel<<<dim3(across, (groups + across - 1) / across), ADAMW_THREADS, 0, st>>>(
+      opt->tensors, opt->list, parts, groups, m, v)));
   SYMI_LAUNCH_CHECK(who);
   return SYMI_OK;
 }
