@@ -26,6 +26,7 @@ constexpr int ADAMW_BLOCK = 256;     // values that share a scale
 constexpr int ADAMW_THREADS = 256;
 constexpr int ADAMW_CHUNK = 4096;    // values of one workgroup
 constexpr float SMALLEST = 1.17549435e-38f;
+constexpr int POSITIVE_DENORMAL = 1 << 7;   // class of a number
 constexpr float M_UNIT = (float)(1.0 / (127 * 127)), V_UNIT = (float)(1.0 / (255 * 255));
 
 struct AdamwTensor {   // on the device
@@ -238,13 +239,24 @@ struct AdamwBlock {
         }
       }
     }
+    // Codes are bound by arithmetic: the instructions for root and reciprocal, each within one unit in the last place.  They take denormal
+    // numbers for 0 (v of gradients below 1e-17 is one, and a denormal eps): there, as with 32-bit states, the functions.
+    bool denormal = CODES && h.eps < SMALLEST;
+    if (CODES) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (CODES) {   // bound by arithmetic: the instructions for root and reciprocal, each within one unit in the last place
+      for (int i = 0; i < 4; ++i) {
         root[i] = __builtin_amdgcn_sqrtf(v_[i]);
-        w_[i] -= h.lr * (m_[i] * h.fix1 * __builtin_amdgcn_rcpf(fmaf(root[i], h.root2, h.eps)) + wd * w_[i]);
-      } else {
+        denormal |= __builtin_amdgcn_classf(v_[i], POSITIVE_DENORMAL);
+      }
+    }
+    if (CODES && __builtin_expect(__ballot(denormal) == 0, 1)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w_[i] -= h.lr * (m_[i] * h.fix1 * __builtin_amdgcn_rcpf(fmaf(root[i], h.root2, h.eps)) + wd * w_[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
         w_[i] -= h.lr * (m_[i] * h.fix1 / (sqrtf(v_[i] * h.fix2) + h.eps) + wd * w_[i]);
+        if (CODES) root[i] = sqrtf(v_[i]);
       }
     }
     if (FULL) {
