@@ -567,14 +567,17 @@ static void launch_rows(const symi_ctx* ctx, int kid, const PolicyArgs& g, hipSt
 #undef ROWS
 }
 
-// Whether a row's wavefronts are workgroups of their own: while all of them together are at most four for each
-// compute unit.  us with the gradient, one workgroup a row : split.  bf16 V = 131072: 16 rows 22.0 : 14.2, 64 23.8 : 20.4, 128
-// 26.3 : 27.3; V = 50001: 1 row 13.2 : 11.4, 64 15.9 : 14.3, 128 16.8 : 17.8; V = 16000: 16 rows 8.7 : 6.8, 128 9.2 : 8.5, 256
-// 10.4 : 11.4; V = 4000: 16 rows 7.3 : 6.2, 256 7.6 : 6.9; fp32 V = 32003: 16 rows 11.9 : 11.5, 256 18.1 : 23.6.
+// Whether a row's wavefronts are workgroups of their own: while all of them together are at most four for each compute unit and, of rows of
+// up to eight wavefronts, a wavefront's pieces of all rows at most 2^16, as every logit is read twice.  us with the gradient, one workgroup a
+// row : split.  bf16 V = 131072: 16 rows 22.4 : 12.9, 64 25.2 : 20.6, 128 27.5 : 28.9; 65000: 64 rows 17.3 : 15.8, 96 18.0 : 18.4; 50001: 1 row
+// 13.3 : 11.1, 64 14.9 : 13.4, 96 15.9 : 15.8, 128 17.1 : 17.5; 32000: 128 rows 13.3 : 12.8, 192 14.5 : 15.6; 16000: 16 rows 10.1 : 8.6, 128
+// 10.7 : 9.9, 192 11.0 : 11.3, 256 11.8 : 12.6; 4000: 16 rows 9.0 : 7.3, 256 9.2 : 7.9; fp32 V = 32003: 16 rows 11.9 : 11.1, 64 13.7 : 14.0, 96
+// 14.4 : 15.9; 25000: 64 rows 12.3 : 11.8, 96 13.1 : 13.8; 8000: 128 rows 9.7 : 8.9, 256 11.1 : 11.8.
 static bool wants_parts(const symi_ctx* ctx, int pieces) {
   int waves = 0;
   by_length(pieces, [&](auto threads, auto) { waves = decltype(threads)::value / 64; });
-  return ctx->cfg.T >= 1 && ctx->cfg.T <= PART_ROWS_MAX && waves > 1 && ctx->cfg.T * waves <= 4 * ctx->cus;
+  const int T = ctx->cfg.T;
+  return T >= 1 && T <= PART_ROWS_MAX && waves > 1 && T * waves <= 4 * ctx->cus && (waves == PART_MAX || (long long)T * pieces <= waves * 65536LL);
 }
 template <bool BF16>
 static void launch_parts(const symi_ctx* ctx, const PolicyArgs& g, const Parts& parts, float* stats, hipStream_t st) {
