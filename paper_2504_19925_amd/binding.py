@@ -128,15 +128,21 @@ class SymiAdamW:
     def __init__(self, ptr, tensors, table):
         self.ptr, self.tensors, self.table = ptr, tensors, table
         self.stream, self.streams = None, set()   # the last call's stream; all of them
+        self._used = []
 
     def use_on(self, stream):
-        """Tells the allocator, once for each stream, that work on it uses the memory."""
-        at = stream.cuda_stream
-        if at not in self.streams:
+        """Notes that work on `stream` uses the memory."""
+        self.stream = stream.cuda_stream
+        if self.stream not in self.streams:
+            self.streams.add(self.stream)
+            self._used.append(stream)
+
+    def release(self):
+        """Tells the allocator about the streams: it keeps the memory, once nobody holds it, until their work so far is done."""
+        used, self._used = self._used, []
+        for stream in used:
             for x in [self.table] + [x for t in self.tensors for x in t.values() if isinstance(x, torch.Tensor)]:
                 x.record_stream(stream)
-            self.streams.add(at)
-        self.stream = at
 
     def __del__(self):
         try:
@@ -709,6 +715,7 @@ def symi_adamw_create(tensors):
 
 def symi_adamw_destroy(opt):
     ptr, opt.ptr = opt.ptr, None
+    opt.release()
     if ptr:
         _check(lib().symi_adamw_destroy(ptr), "symi_adamw_destroy")
 
