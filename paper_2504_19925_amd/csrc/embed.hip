@@ -607,8 +607,9 @@ extern "C" int symi_embed_bwd(const symi_ctx* ctx, const int32_t* tokens, const 
   // workgroups over two dimensions: the threads of one end at 2^32
   const auto grid_of = [](long long groups) { return dim3((unsigned)std::min(groups, 1LL << 20), (unsigned)((groups + (1LL << 20) - 1) >> 20)); };
   // us on rows of d = 128 (one part), 1024 (two) and 4096 (eight), sorted : not.  512 tokens of d = 1024: 13 : 4; 1024 tokens 14 : 5.5,
-  // 15 : 7.3, 19 : 24; 2048: 15 : 7.3, 17 : 12.5, 24 : 44; 3000: 16 : 11, 19 : 23, 28 : 77; 4096: 15.5 : 14.5, 19 : 30, 33 : 105.  All
-  // 2048 tokens the same: 20 : 35.
+  // 15 : 7.3, 19 : 24; 2048: 15 : 7.3, 17 : 12.5, 24 : 44; 3000: 16 : 11, 19 : 23, 28 : 77; 4096: 15.5 : 14.5, 19 : 30, 33 : 105.  With one
+  // part the line would lie at 4000 tokens; it is where embed_few_kernel's eight wavefronts of 4 x 64 tokens end.  All 2048 tokens the same:
+  // 20 : 35; what the tokens are is not known here.
   if (cfg->T <= 64 || (cfg->T <= FEW_MAX && (long long)cfg->T * L.parts <= 4096)) {
     const long long groups = (long long)cfg->T * L.parts + (accumulate ? 0 : ((long long)V * (cfg->d / 4) + 1023) / 1024);
     if (groups == 0) return SYMI_OK;

@@ -4,7 +4,8 @@
 // Per row of logits, in base 2 with c = log2(e) / temperature: m = max z_j, s = sum 2^(c (z_j - m)),
 //   logp = ln 2 c (z_a - m) - ln s,   dlogits_j = u ([j = a] - 2^(c (z_j - m)) / s),   u = grad_scale w / temperature dL/dlogp.
 // The weights are the caller's, so u needs nothing from other rows: one workgroup takes a row from its logits to
-// their gradient.  Statistics and sums are fp32; the four sums over the rows are taken in 64 bits by one workgroup, in order.
+// their gradient.  A row's statistics are fp32.  logp, and the differences that the ratio and the KL are exponentials of, are taken in 64
+// bits from there; ratio, KL and a token's terms are fp32 again, and the four sums over the rows 64 bits, by one workgroup, in order.
 #include <math.h>
 
 #include <algorithm>
@@ -320,9 +321,9 @@ __device__ __forceinline__ double logp_of(const PolicyScalars& p, float za, floa
 // A workgroup of THREADS takes a row.  What fits is read once and stays in registers from the logits to their gradient; of a
 // longer row the last STEP pieces stay and the ones before them are read again.
 // Up to eight pieces a thread leave 64 registers: eight wavefronts a SIMD, two workgroups of 1024 a unit.
-// Bound by memory on many rows: with the gradient 16384 of 131072 in bf16, a quarter masked, 1427 us, 3.2 GB fetched and 4.3 written
-// (5.3 TB/s, vector units busy 57 %); without it 8192 of 50001, 40 % masked, 84 us, 0.51 GB (6.1 TB/s, busy 90 %).  777 rows of 32003 in
-// fp32, a fifth masked, 41 us at 4.3 TB/s: 622 rows on places for 512 workgroups.  16 rows of 128000: 11 us, the exponentials of 16 units.
+// Bound by memory on many rows: with the gradient 16384 of 131072 in bf16, a quarter masked, 1444 us, 3.2 GB fetched and 4.3 written
+// (5.2 TB/s, vector units busy 61 %); without it 8192 of 50001, 40 % masked, 84 us, 0.51 GB (6.0 TB/s, busy 91 %).  777 rows of 32003 in
+// fp32, a fifth masked, 42 us at 4.3 TB/s: 622 rows on places for 512 workgroups.  16 rows of 128000: 11 us, the exponentials of 16 units.
 template <bool BF16, bool GRAD, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS, NV <= 8 ? 8 : 4) void policy_kernel(PolicyArgs g) {
   using R = Row<BF16, !GRAD, THREADS, NV>;
@@ -376,8 +377,8 @@ __global__ __launch_bounds__(THREADS, NV <= 8 ? 8 : 4) void policy_kernel(Policy
 
 // Few rows: every wavefront that policy_kernel would give a row is a workgroup of its own, in two launches.  The first
 // leaves each wavefront's (m, s) and the chosen logit; the second joins them, reads the logits again and writes their
-// gradient.  Which pieces a thread takes and how sums are joined is that of policy_kernel, so a row's bits do not
-// depend on the number of rows (only on where it begins within 16 bytes).  The first workgroup of the second launch takes the sums over the tokens.
+// gradient.  Which pieces a thread takes and how sums are joined is that of policy_kernel with a gradient, so a row's bits do not
+// depend on the number of rows (only on where it begins within 16 bytes); without a gradient they do, see launch_rows.  The first workgroup of the second launch takes the sums over the tokens.
 // Bound by latency, as the second reading comes from the caches; measured at wants_parts.
 constexpr int SUM_SPLIT_THREADS = 256;
 constexpr int PART_MAX = 16;         // wavefronts of a row
@@ -530,11 +531,11 @@ static PolicyScalars scalars(const symi_policy* hp) {
 }
 
 // The workgroup for a row with its gradient: f(THREADS, NV).  The smallest that holds the row comes first, with four to 16 pieces a
-// thread: us for 8192 rows in bf16, threads x pieces.  V = 3000: 64 x 8 31, 128 x 8 29, 256 x 4 34; 10001: 256 x 4 80, 256 x 8
-// 75, 512 x 4 85; 17010: 256 x 16 112, 512 x 8 113; 28000: 512 x 8 179, 512 x 12 176, 256 x 16 186; 45000: 512 x 12 285, 512 x 16
-// 274; 50001: 512 x 16 298, in two parts 10 % more.  Longer rows are read again in part, most of it from the memory-side cache: 4096
-// of 100000 with eight pieces of 1024 threads 337, with 16 351; 16384 of 131072, a quarter masked, 1508 and 1444; 2048 of
-// 200000 in fp32 889 and 782.
+// thread: us for 8192 rows in bf16, threads x pieces, sums included.  V = 3000: 64 x 8 29, 128 x 8 30, 256 x 4 36; 10001: 256 x 4 74, 256 x 8
+// 70, 512 x 4 81; 17010: 256 x 16 110, 512 x 8 112; 28000: 512 x 8 185, 512 x 12 172, 256 x 16 188; 45000: 512 x 12 286, 512 x 16
+// 271; 50001: 512 x 16 300, 512 x 12 317.  Longer rows are read again in part, most of it from the memory-side cache: 4096
+// of 100000 with eight pieces of 1024 threads 338, with 16 363; 16384 of 131072, a quarter masked, 1495 and 1451; 2048 of
+// 200000 in fp32 880 and 776.
 template <int X> using Int = std::integral_constant<int, X>;
 template <class F>
 static void by_length(int pieces, F f) {
@@ -556,8 +557,8 @@ static void launch_rows(const symi_ctx* ctx, int kid, const PolicyArgs& g, hipSt
   if (g.dlogits) {
     by_length(pieces, [&](auto threads, auto nv) { ROWS(true, decltype(threads)::value, decltype(nv)::value); });
   } else {
-    // Nothing has to stay: eight pieces of 256 threads at a time (8192 of 32000 in bf16 81 us), on few rows 512 threads (300 of
-    // 131072: 21.7 against 25.5) or 1024 (16 of 128000: 10.3 against 11.0).
+    // Nothing has to stay: eight pieces of 256 threads at a time (8192 of 32000 in bf16 82 us, 512 x 4 84), on few rows 512 threads (300 of
+    // 131072: 20.7 against 22.9) or 1024 (16 of 128000: 11.9 against 13.8).  So a row's last bits depend on the batch here.
     if (pieces <= 64 * 4) ROWS(false, 64, 4);
     else if (pieces <= 256 * 4) ROWS(false, 256, 4);
     else if (T <= ctx->cus / 4 && pieces > 8192) ROWS(false, 1024, 8);
