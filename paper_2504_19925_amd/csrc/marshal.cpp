@@ -149,12 +149,21 @@ class Call {
 
  private:
   // whether the handle's last call was on the current stream; else binding.py notes the new one first
-  static bool on_its_stream(PyObject* opt) {
+  bool on_its_stream(PyObject* opt) {
     PyObject* s = PyObject_GetAttr(opt, g_stream);
-    const bool is = s && PyLong_Check(s) && PyLong_AsVoidPtr(s) == static_cast<void*>(c10::hip::getCurrentHIPStream().stream());
+    bool is = false;
+    try {
+      is = s && PyLong_CheckExact(s) && PyLong_AsVoidPtr(s) == stream();
+    } catch (...) {   // no current stream: the slow path says so
+    }
     Py_XDECREF(s);
-    if (PyErr_Occurred()) PyErr_Clear();
+    if (!is) PyErr_Clear();
     return is;
+  }
+  void* stream() {
+    if (!has_stream_) stream_ = c10::hip::getCurrentHIPStream().stream();
+    has_stream_ = true;
+    return stream_;
   }
   Val tensor(int i, at::ScalarType type, long long n) {
     Val v;
@@ -174,9 +183,9 @@ class Call {
   PyObject* run(Fn fn, const Val (&v)[N], std::index_sequence<I...>) {
     int rc = 0;
     try {
-      void* const stream = c10::hip::getCurrentHIPStream().stream();
+      void* const on = stream();
       Py_BEGIN_ALLOW_THREADS
-      rc = fn(ctx_, v[I]..., stream);
+      rc = fn(ctx_, v[I]..., on);
       Py_END_ALLOW_THREADS
     } catch (const std::exception& e) {
       PyErr_SetString(PyExc_RuntimeError, e.what());
@@ -188,6 +197,8 @@ class Call {
   symi_ctx* ctx_ = nullptr;
   symi_adam hp_;
   symi_policy pp_;
+  void* stream_ = nullptr;
+  bool has_stream_ = false;
 };
 
 #define DEF(name) PyObject* py_##name(PyObject*, PyObject* const* a, Py_ssize_t n)
