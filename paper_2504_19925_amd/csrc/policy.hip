@@ -569,16 +569,18 @@ static void launch_rows(const symi_ctx* ctx, int kid, const PolicyArgs& g, hipSt
 }
 
 // Whether a row's wavefronts are workgroups of their own: while all of them together are at most four for each compute unit and, of rows of
-// up to eight wavefronts, a wavefront's pieces of all rows at most 2^16, as every logit is read twice.  us with the gradient, one workgroup a
+// up to eight wavefronts, a wavefront's pieces of all rows at most 80000 (58000 of fp32 rows of eight), as every logit is read twice.  us with the gradient, one workgroup a
 // row : split.  bf16 V = 131072: 16 rows 22.4 : 12.9, 64 25.2 : 20.6, 128 27.5 : 28.9; 65000: 64 rows 17.3 : 15.8, 96 18.0 : 18.4; 50001: 1 row
-// 13.3 : 11.1, 64 14.9 : 13.4, 96 15.9 : 15.8, 128 17.1 : 17.5; 32000: 128 rows 13.3 : 12.8, 192 14.5 : 15.6; 16000: 16 rows 10.1 : 8.6, 128
-// 10.7 : 9.9, 192 11.0 : 11.3, 256 11.8 : 12.6; 4000: 16 rows 9.0 : 7.3, 256 9.2 : 7.9; fp32 V = 32003: 16 rows 11.9 : 11.1, 64 13.7 : 14.0, 96
-// 14.4 : 15.9; 25000: 64 rows 12.3 : 11.8, 96 13.1 : 13.8; 8000: 128 rows 9.7 : 8.9, 256 11.1 : 11.8.
-static bool wants_parts(const symi_ctx* ctx, int pieces) {
+// 13.3 : 11.1, 64 14.9 : 13.4, 96 15.9 : 15.8, 128 17.1 : 17.5; 32000: 128 rows 13.3 : 12.8, 192 14.5 : 15.6; 16000: 16 rows 10.1 : 8.6, 160
+// 10.9 : 10.4, 192 11.0 : 11.3, 256 11.8 : 12.6; 12000: 192 rows 10.3 : 9.8, 256 10.5 : 10.6; 4000: 16 rows 9.0 : 7.3, 256 9.2 : 7.9; fp32 V = 32003:
+// 16 rows 11.9 : 11.1, 64 13.7 : 14.0, 96 14.4 : 15.9; 25000: 64 rows 12.3 : 11.8, 96 13.1 : 13.8; 16000: 96 rows 11.0 : 10.4, 128 11.5 : 11.7;
+// 8000: 160 rows 10.1 : 9.8, 256 11.1 : 11.8.
+static bool wants_parts(const symi_ctx* ctx, int pieces, bool bf16) {
   int waves = 0;
   by_length(pieces, [&](auto threads, auto) { waves = decltype(threads)::value / 64; });
   const int T = ctx->cfg.T;
-  return T >= 1 && T <= PART_ROWS_MAX && waves > 1 && T * waves <= 4 * ctx->cus && (waves == PART_MAX || (long long)T * pieces <= waves * 65536LL);
+  const long long each = waves == 8 && !bf16 ? 58000 : 80000;
+  return T >= 1 && T <= PART_ROWS_MAX && waves > 1 && T * waves <= 4 * ctx->cus && (waves == PART_MAX || (long long)T * pieces <= waves * each);
 }
 template <bool BF16>
 static void launch_parts(const symi_ctx* ctx, const PolicyArgs& g, const Parts& parts, float* stats, hipStream_t st) {
@@ -630,7 +632,7 @@ extern "C" int symi_policy_loss(const symi_ctx* ctx, const symi_policy* hp, cons
   char* const w = reinterpret_cast<char*>(align_up(reinterpret_cast<size_t>(ws), 256));
   const PolicyArgs g = {logits, V, ld, action, logp_old, logp_ref, advantage, weight, logp, reinterpret_cast<float4*>(w + L.terms), dlogits, scalars(hp)};
   const bool bf16 = hp->logits_dtype == SYMI_BF16;
-  if (dlogits && wants_parts(ctx, cdiv(V, bf16 ? 8 : 4))) {
+  if (dlogits && wants_parts(ctx, cdiv(V, bf16 ? 8 : 4), bf16)) {
     const Parts parts = {reinterpret_cast<float2*>(w + L.ms), reinterpret_cast<float*>(w + L.chosen)};
     if (bf16) launch_parts<true>(ctx, g, parts, stats, st);
     else launch_parts<false>(ctx, g, parts, stats, st);
