@@ -71,14 +71,14 @@ __device__ __forceinline__ void forget(Raw& r) { asm volatile("" : "+v"(r)); }
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }   // below 2^-126: 0
 
 // c (x - ref) in one operation, as c x - by with by = c ref rounded, where what the rounding makes of the power can be put right afterwards: by
-// `rest`, 2^(by - c ref) to first order (the second is below 2^-25).  Elsewhere, among masks of -1e10 or -1e30, c x - by may be anything.
+// `rest`, 2^(by - c ref) to second order (the third is below 2^-25).  Elsewhere, among masks of -1e10 or -1e30, c x - by may be anything.
 struct Exponent {
   float by, rest;
   bool near;
 };
 __device__ __forceinline__ Exponent exponent_of(float ref, float c) {
-  const float by = ref * c;
-  return {by, fmaf(fmaf(ref, c, -by), -0.693147181f, 1.f), fabsf(by) < 4096.f};
+  const float by = ref * c, y = fmaf(ref, c, -by) * -0.693147181f;
+  return {by, fmaf(y, fmaf(y, 0.5f, 1.f), 1.f), fabsf(by) < 0x1p18f};
 }
 
 // (m, s) of a set of logits: m the largest, s the sum of 2^(c (z - m)).

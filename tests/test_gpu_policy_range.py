@@ -114,3 +114,32 @@ def test_the_largest_inverse_temperature(dtype):
     b = dict(z=z, action=torch.full((T,), 77, dtype=torch.int32, device="cuda"), old=f(0.0), ref=None, advantage=f(0.0), weight=f(1.0))
     logp, stats, dz = call(context(T), hp, b, V)
     assert not logp.any() and not stats.any() and not dz.any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tau", [0.1, 0.003, 3e-4, 1.1e-4, 1e-5])
+def test_low_temperatures(tau, dtype):
+    """Exponents of the largest logit from some hundred to some million: on both sides of where they are taken in one operation."""
+    T, dt = 40, torch.bfloat16 if dtype == "bf16" else torch.float32
+    for V, rows in ((300, T), (20000, T), (20000, 300)):
+        g = torch.Generator(device="cuda").manual_seed(V)
+        top = torch.linspace(-40, 40, rows, device="cuda")[:, None]
+        z = top - torch.rand(rows, V, generator=g, device="cuda") * 40 * tau      # as near as the temperature lets them count
+        z = z.to(dt)
+        hp = symi.SymiPolicy.make(0.5, 0.5, 0.0, tau, 1.0, dtype)
+        d = (z.double() - z.double().amax(1, keepdim=True)) * hp.inv_temperature
+        a = torch.randint(0, V, (rows, 1), generator=g, device="cuda")
+        lp = torch.log_softmax(d, 1).gather(1, a)[:, 0]
+        f = lambda x: torch.full((rows,), x, device="cuda")   # noqa: E731
+        b = dict(z=z, action=a[:, 0].to(torch.int32), old=lp.float(), ref=None, advantage=f(1.0), weight=f(1.0))
+        Z = torch.where(d > -110, -d, 0.0).amax(1)
+        e = U32 * (6 * Z + V / 64 + 24 + 3 * lp.abs())
+        logp, stats, dz = call(context(rows), hp, b, V)
+        assert ((logp.double() - lp).abs() <= e).all()
+        ratio = torch.exp(lp - b["old"].double())
+        rel = 2 * e + U32 * (16 + 4 * lp.abs())
+        p, u = torch.softmax(d, 1), -hp.inv_temperature * ratio[:, None]
+        want = (-u * p).scatter_add_(1, a, u)
+        part = p.scatter_add(1, a, torch.ones_like(u))
+        bound = u.abs() * 2 * rel[:, None] * part + (U16 if dtype == "bf16" else U32) * 1.01 * want.abs() + 1e-38
+        assert ((dz.double() - want).abs() <= bound).all()
