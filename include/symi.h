@@ -15,6 +15,9 @@
  *              the ends of the step around the MoE layers: symi_embed_fwd / symi_embed_bwd,
  *              symi_policy_loss / symi_token_logp, symi_adamw_step for every tensor that
  *              is no expert's;
+ *              the way into the experts: symi_norm_fwd / symi_norm_bwd in front of a layer,
+ *              symi_route_scored instead of symi_route, symi_expert_fwd8 instead of
+ *              symi_expert_fwd;
  *              host helpers for the multi-rank plan at the end of this file
  *
  * Conventions
@@ -411,6 +414,97 @@ int symi_adamw_step(const symi_ctx* ctx, const symi_adamw* opt, const symi_adam*
  * from element 256 * (sum of ceil(n_j / 256) over j < i) on; what lies between is not written. */
 long long symi_adamw_values(const symi_adamw* opt);
 int symi_adamw_decode(const symi_ctx* ctx, const symi_adamw* opt, float* m, float* v, void* stream);
+
+/* ---- the way of a batch into the experts: the norm in front of a layer, routing by scores with a bias and groups,
+ * and the experts' products in 8 bits.  T, E, k, d, f, S_tot, dtype and renorm are those of the context.  Buffers may start at any
+ * element unless a call says so; an output may overlap nothing else of the call unless it says so. */
+
+/* Layer norm (center = 1) or RMS norm (center = 0) of rows, behind a residual sum where there is one:
+ *   R = X + residual, rounded to the activation dtype (residual NULL: R = X, and the argument R is NULL);
+ *   mean = sum R / d (center = 0: 0),  rstd = 1 / sqrt(sum (R - mean)^2 / d + eps),  Y = (R - mean) rstd w + b.
+ *   X, residual, R, Y [T,d] in the activation dtype; w, b [d] f32 or NULL (1 and 0).  R may be X or residual.
+ *   mean, rstd [T] f32 out, each NULL if it is not wanted (the backward pass needs them).  eps >= 0; with eps = 0 a row without any
+ *   variation is NaN.  Statistics are fp32, the variance a sum of squares of differences.  A row's results do not depend on the batch. */
+int symi_norm_fwd(const symi_ctx* ctx, int center, float eps, const void* X, const void* residual, const float* w,
+                  const float* b, void* R, void* Y, float* mean, float* rstd, void* stream);
+
+/* Its gradients, with xh = (R - mean) rstd and g = dY w:
+ *   dX = rstd (g - [center] sum g / d - xh sum(g xh) / d) + dR,  dw = sum over the rows of dY xh,  db = sum of dY.
+ *   dX is the gradient of X and of residual; dR [T,d] the one that R gets from elsewhere, or NULL.  dX may be dY or dR.
+ *   R: symi_norm_fwd's (X where there was no residual); mean is not read with center = 0.
+ *   w NULL: 1.  dw, db [d] f32 out, each NULL if it is not wanted; the sums over the rows are taken in an order that
+ *   only T and d decide (same bits on every run); T = 0 gives zeros.
+ *   ws: symi_norm_workspace_bytes(cfg) bytes of scratch, under the rules of symi_workspace_bytes (0 if cfg is invalid). */
+size_t symi_norm_workspace_bytes(const symi_cfg* cfg);
+int symi_norm_bwd(const symi_ctx* ctx, int center, const void* dY, const void* R, const float* mean, const float* rstd,
+                  const float* w, const void* dR, void* dX, float* dw, float* db, void* ws, void* stream);
+
+/* Routing by scores.  For a token with logits z over the E classes:
+ *   s   = softmax(z) or 1 / (1 + exp(-z)),  c = s + bias
+ *   groups of E / groups consecutive classes: a group counts as the sum of the group_top largest c of its unmasked classes (as many as
+ *         there are; none: as -inf); the top_groups best groups stay
+ *   idx = the k classes with the largest c in them, best first
+ *   gate = scale s (renorm: scale s / sum of the k)
+ * The bias takes part in the choice only.  c and the groups' sums are compared as binary64 evaluates them, equal ones go to the lower
+ * index; without a bias classes are compared by their logits, which is the same order.  A class whose logit is -inf is masked: it is
+ * never chosen for its score.  Where fewer than k classes are left, the lowest of the others fill up, with gate 0: idx always
+ * holds k different classes, and a row that is masked altogether has gates 0.  A row with a NaN logit, or in a softmax one of +inf, has
+ * NaN for all its gates and any k classes; a bias of NaN or -inf masks its class.  Renormalised gates are quotients of scores taken relative to
+ * the largest of the k, so that they keep their digits where the scores underflow. */
+typedef struct symi_score {
+  int score;       /* SYMI_SOFTMAX or SYMI_SIGMOID */
+  int groups;      /* 1 <= groups <= 64, a divisor of E; 1: no groups */
+  int top_groups;  /* 1 <= top_groups <= groups, top_groups E / groups >= k */
+  int group_top;   /* 1 or 2, at most E / groups */
+  float scale;     /* > 0: the gates are multiplied by it */
+} symi_score;
+enum { SYMI_SOFTMAX = 0, SYMI_SIGMOID = 1 };
+/* logits [T,E] f32, bias [E] f32 or NULL; idx [T,k] i32, gate [T,k] f32 and hist [E] i32 out as symi_route's: symi_dispatch and
+ * symi_combine take them. */
+int symi_route_scored(const symi_ctx* ctx, const symi_score* hp, const float* logits, const float* bias, int32_t* idx,
+                      float* gate, int32_t* hist, void* stream);
+/* dlogits [T,E] f32 out from dgate [T,k] f32; idx, gate: symi_route_scored's.  The choice has no gradient; a class that only
+ * filled up (gate 0) has none either. */
+int symi_route_scored_bwd(const symi_ctx* ctx, const symi_score* hp, const float* logits, const int32_t* idx,
+                          const float* gate, const float* dgate, float* dlogits, void* stream);
+/* The step that balances the classes without a loss: bias[e] += rate sign(sum of hist / E - hist[e]), the comparison in integers.
+ * hist [E] i32 (symi_route_scored's, or its sum over ranks), bias [E] f32 in/out. */
+int symi_route_bias(const symi_ctx* ctx, const int32_t* hist, float rate, float* bias, void* stream);
+
+/* Values in 8 bits.  128 consecutive values of a row (block = 1: activations), or of 128 consecutive rows (block = 128: weights),
+ * share a power of two; the last blocks of a row and of a group of rows hold what is left:
+ *   x = q 2^(s - 127),  q in e4m3 (4 bits of precision, finite up to 448, no infinities),
+ *   s the smallest byte with which the block's largest |x| is at most 448 2^(s - 127), 0 where that is 0
+ * q is x 2^(127 - s) rounded to nearest, ties to even; powers of two add no rounding of their own, and the matrix instruction multiplies by them
+ * itself.  A value that is not finite is stored as NaN, and the others of its block as if it were not there.
+ *   X [groups,rows,n] in the activation dtype, n a multiple of 8, at most 2^22;
+ *   q [groups,rows,symi_pitch8(n)] bytes, 16-byte aligned: n rounded up to whole blocks, zeros behind n;
+ *   s [groups,ceil(rows / block),symi_scale_pitch8(n)] bytes, 4-byte aligned: the blocks of n rounded up to whole fours, zeros behind. */
+int symi_pitch8(int n);         /* host functions; SYMI_EINVAL for n that the calls refuse */
+int symi_scale_pitch8(int n);
+int symi_quant8(const symi_ctx* ctx, const void* X, int groups, int rows, int n, int block, void* q, void* s, void* stream);
+/* The values that q and s stand for, rounded to the activation dtype (in bf16 that rounds only below 2^-126 and above its largest value). */
+int symi_dequant8(const symi_ctx* ctx, const void* q, const void* s, int groups, int rows, int n, int block, void* X, void* stream);
+
+/* Products of 8-bit values over replica slots: for the rows [slot_offsets[p], slot_offsets[p+1]) of slot p
+ *   Y[row, j] = sum over i < n of A[row, i] W[p, j, i]
+ *   summed in fp32; in a bf16 context by the 8-bit matrix instruction, which drops of every 8 neighbouring products what is below 2^-13 of
+ *   the largest (some 1.5e-5 of a result, a hundredth of its rounding), in an fp32 context at half that rate without such a loss.
+ *   Aq, As: [T k, n] with block = 1;  Wq, Ws: [S_tot, R, n] with block = 128;  slot_offsets [S_tot+1] as symi_dispatch's, up to T k;
+ *   Y [T k, R] out in the activation dtype; rows outside the slots are not written.  R a multiple of 8, at most 2^22.
+ *   ws: symi_workspace8_bytes(cfg) bytes of scratch, under the rules of symi_workspace_bytes (0 if cfg is invalid). */
+size_t symi_workspace8_bytes(const symi_cfg* cfg);
+int symi_product8(const symi_ctx* ctx, const void* Aq, const void* As, const int32_t* slot_offsets, const void* Wq,
+                  const void* Ws, int R, int n, void* Y, void* ws, void* stream);
+
+/* symi_expert_fwd in 8 bits, for bf16 contexts (fp32: SYMI_EUNSUPPORTED): Xp and the hidden units are rounded to 8 bits (block = 1) on their
+ * way into the products, u, v and h are fp32 until they are stored.
+ *   W1q, W1s: [S_tot, 2f, d], W2q, W2s: [S_tot, d, f] with block = 128 (symi_quant8 of W1_slots, W2_slots).
+ *   UV, H: as symi_expert_fwd's (H: h rounded to bf16), for symi_expert_bwd, which takes the roundings to 8 bits as having gradient 1; NULL,
+ *   both, where there is no backward pass.  symi_dequant8 gives the weights that the products saw.
+ *   Rows behind slot_offsets[S_tot] are neither read nor written. */
+int symi_expert_fwd8(const symi_ctx* ctx, const void* Xp, const int32_t* slot_offsets, const void* W1q, const void* W1s,
+                     const void* W2q, const void* W2s, void* UV, void* H, void* Yp, void* ws, void* stream);
 
 /* ---- host helpers for the multi-rank part of the method (no GPU work; all pointers HOST).
  * Slot q of a placement lives on rank q / s, s = S_tot / N (S_tot must divide by N). */

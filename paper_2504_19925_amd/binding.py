@@ -35,6 +35,8 @@ EXPORTS = [
     "symi_embed_fwd", "symi_embed_workspace_bytes", "symi_embed_bwd", "symi_token_logp",
     "symi_policy_workspace_bytes", "symi_policy_loss", "symi_adamw_table_bytes", "symi_adamw_create", "symi_adamw_destroy",
     "symi_adamw_step", "symi_adamw_values", "symi_adamw_decode",
+    "symi_norm_fwd", "symi_norm_workspace_bytes", "symi_norm_bwd", "symi_route_scored", "symi_route_scored_bwd", "symi_route_bias",
+    "symi_pitch8", "symi_scale_pitch8", "symi_quant8", "symi_dequant8", "symi_workspace8_bytes", "symi_product8", "symi_expert_fwd8",
 ]
 
 
@@ -111,6 +113,14 @@ class SymiPolicy(ctypes.Structure):
     @property
     def torch_dtype(self):
         return torch.bfloat16 if self.logits_dtype == 1 else torch.float32
+
+
+class SymiScore(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("score", "groups", "top_groups", "group_top")] + [("scale", ctypes.c_float)]
+
+    @classmethod
+    def make(cls, score="sigmoid", groups=1, top_groups=1, group_top=1, scale=1.0):
+        return cls({"softmax": 0, "sigmoid": 1}[score], groups, top_groups, group_top, scale)
 
 
 class SymiAdamWTensor(ctypes.Structure):
@@ -215,13 +225,26 @@ def lib():
             "symi_adamw_step": ([ctx, vp, ctypes.POINTER(SymiAdam), fp, ctypes.c_uint32, vp], ci),
             "symi_adamw_values": ([vp], ctypes.c_longlong),
             "symi_adamw_decode": ([ctx, vp, fp, fp, vp], ci),
+            "symi_norm_fwd": ([ctx, ci, cf, vp, vp, fp, fp, vp, vp, fp, fp, vp], ci),
+            "symi_norm_workspace_bytes": ([cfgp], ctypes.c_size_t),
+            "symi_norm_bwd": ([ctx, ci, vp, vp, fp, fp, fp, vp, vp, fp, fp, vp, vp], ci),
+            "symi_route_scored": ([ctx, ctypes.POINTER(SymiScore), fp, fp, ip, fp, ip, vp], ci),
+            "symi_route_scored_bwd": ([ctx, ctypes.POINTER(SymiScore), fp, ip, fp, fp, fp, vp], ci),
+            "symi_route_bias": ([ctx, ip, cf, fp, vp], ci),
+            "symi_pitch8": ([ci], ci),
+            "symi_scale_pitch8": ([ci], ci),
+            "symi_quant8": ([ctx, vp, ci, ci, ci, ci, vp, vp, vp], ci),
+            "symi_dequant8": ([ctx, vp, vp, ci, ci, ci, ci, vp, vp], ci),
+            "symi_workspace8_bytes": ([cfgp], ctypes.c_size_t),
+            "symi_product8": ([ctx, vp, vp, ip, vp, vp, ci, ci, vp, vp, vp], ci),
+            "symi_expert_fwd8": ([ctx, vp, ip, vp, vp, vp, vp, vp, vp, vp, vp, vp], ci),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
             fn.argtypes = args
             fn.restype = res
         for name, fast in _load_marshal(L).items():
-            (_marshal_ends if name in ENDS else _marshal)[name] = fast
+            (_marshal_ends if name in ENDS else _marshal_way if name in WAY else _marshal)[name] = fast
         _LIB = L
     return _LIB
 
@@ -229,6 +252,9 @@ def lib():
 _marshal = {}   # name -> function of _marshal.so, filled when libsymi.so is loaded: the layer's calls
 _marshal_ends = {}   # and those of the ends of the step
 ENDS = ("symi_embed_fwd", "symi_embed_bwd", "symi_token_logp", "symi_policy_loss", "symi_adamw_step", "symi_adamw_decode")
+_marshal_way = {}   # and those of the way into the experts
+WAY = ("symi_norm_fwd", "symi_norm_bwd", "symi_route_scored", "symi_route_scored_bwd", "symi_route_bias", "symi_quant8", "symi_dequant8",
+       "symi_product8", "symi_expert_fwd8")
 
 
 def _load_marshal(L):
@@ -244,7 +270,7 @@ def _load_marshal(L):
         warnings.warn(f"{path} cannot be loaded, device calls go through ctypes: {e}")
         return {}
     mod.attach({n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in EXPORTS}, SymiCtx, SymiAdam,
-               SymiPolicy, SymiAdamW)
+               SymiPolicy, SymiAdamW, SymiScore)
     return {n: getattr(mod, n) for n in EXPORTS if hasattr(mod, n)}
 
 
@@ -264,12 +290,12 @@ def _device_call(slow):
     return call
 
 
-def _ends_call(slow):
+def _ends_call(slow, marshalled=_marshal_ends):
     """The same for the ends of the step; the ctypes path is `call.through_ctypes`."""
     name = slow.__name__
 
     def call(*args, **kw):
-        fast = None if kw else _marshal_ends.get(name)
+        fast = None if kw else marshalled.get(name)
         rc = fast(*args) if fast else None
         if rc is None:
             return slow(*args, **kw)
@@ -279,6 +305,11 @@ def _ends_call(slow):
     call.__name__ = call.__qualname__ = name
     call.__doc__, call.through_ctypes = slow.__doc__, slow
     return call
+
+
+def _way_call(slow):
+    """The same for the way into the experts."""
+    return _ends_call(slow, _marshal_way)
 
 
 def symi_last_error():
@@ -738,3 +769,119 @@ def symi_adamw_decode(ctx, opt, m, v):
     n = symi_adamw_values(opt)
     _check(lib().symi_adamw_decode(ctx.ptr, opt.ptr, _dev(m, F32, "m", n), _dev(v, F32, "v", n), _stream()),
            "symi_adamw_decode")
+
+
+def symi_norm_workspace_bytes(cfg):
+    return lib().symi_norm_workspace_bytes(ctypes.byref(_cfg_of(cfg)))
+
+
+def symi_workspace8_bytes(cfg):
+    return lib().symi_workspace8_bytes(ctypes.byref(_cfg_of(cfg)))
+
+
+def symi_pitch8(n):
+    """Bytes from row to row of codes of n values."""
+    rc = lib().symi_pitch8(int(n))
+    if rc < 0:
+        _check(rc, "symi_pitch8")
+    return rc
+
+
+def symi_scale_pitch8(n):
+    """Bytes from row to row of their scales."""
+    rc = lib().symi_scale_pitch8(int(n))
+    if rc < 0:
+        _check(rc, "symi_scale_pitch8")
+    return rc
+
+
+def _dev_or_none(t, dtype, name, numel):
+    return None if t is None else _dev(t, dtype, name, numel)
+
+
+@_way_call
+def symi_norm_fwd(ctx, center, eps, X, residual, w, b, R, Y, mean, rstd):
+    dt, n = ctx.torch_dtype, ctx.T * ctx.d
+    _check(lib().symi_norm_fwd(
+        ctx.ptr, int(center), float(eps), _dev(X, dt, "X", n), _dev_or_none(residual, dt, "residual", n), _dev_or_none(w, F32, "w", ctx.d),
+        _dev_or_none(b, F32, "b", ctx.d), _dev_or_none(R, dt, "R", n), _dev(Y, dt, "Y", n), _dev_or_none(mean, F32, "mean", ctx.T),
+        _dev_or_none(rstd, F32, "rstd", ctx.T), _stream()), "symi_norm_fwd")
+
+
+@_way_call
+def symi_norm_bwd(ctx, center, dY, R, mean, rstd, w, dR, dX, dw, db, ws):
+    dt, n = ctx.torch_dtype, ctx.T * ctx.d
+    _check(lib().symi_norm_bwd(
+        ctx.ptr, int(center), _dev(dY, dt, "dY", n), _dev(R, dt, "R", n), _dev_or_none(mean, F32, "mean", ctx.T), _dev(rstd, F32, "rstd", ctx.T),
+        _dev_or_none(w, F32, "w", ctx.d), _dev_or_none(dR, dt, "dR", n), _dev(dX, dt, "dX", n), _dev_or_none(dw, F32, "dw", ctx.d),
+        _dev_or_none(db, F32, "db", ctx.d), _dev(ws, torch.uint8, "ws", symi_norm_workspace_bytes(ctx.cfg)), _stream()), "symi_norm_bwd")
+
+
+@_way_call
+def symi_route_scored(ctx, hp, logits, bias, idx, gate, hist):
+    _check(lib().symi_route_scored(
+        ctx.ptr, ctypes.byref(hp), _dev(logits, F32, "logits", ctx.T * ctx.E), _dev_or_none(bias, F32, "bias", ctx.E),
+        _dev(idx, I32, "idx", ctx.A), _dev(gate, F32, "gate", ctx.A), _dev(hist, I32, "hist", ctx.E), _stream()), "symi_route_scored")
+
+
+@_way_call
+def symi_route_scored_bwd(ctx, hp, logits, idx, gate, dgate, dlogits):
+    _check(lib().symi_route_scored_bwd(
+        ctx.ptr, ctypes.byref(hp), _dev(logits, F32, "logits", ctx.T * ctx.E), _dev(idx, I32, "idx", ctx.A), _dev(gate, F32, "gate", ctx.A),
+        _dev(dgate, F32, "dgate", ctx.A), _dev(dlogits, F32, "dlogits", ctx.T * ctx.E), _stream()), "symi_route_scored_bwd")
+
+
+@_way_call
+def symi_route_bias(ctx, hist, rate, bias):
+    _check(lib().symi_route_bias(ctx.ptr, _dev(hist, I32, "hist", ctx.E), float(rate), _dev(bias, F32, "bias", ctx.E), _stream()),
+           "symi_route_bias")
+
+
+E4M3 = torch.float8_e4m3fn
+
+
+def _room8(groups, rows, n, block):
+    """Elements of the codes and of the scales of such values (what the call refuses counts as none)."""
+    if groups < 0 or rows < 0 or block < 1 or n < 1:
+        return 0, 0
+    blocks = -(-n // 128)
+    return groups * rows * blocks * 128, groups * -(-rows // block) * -(-blocks // 4) * 4
+
+
+@_way_call
+def symi_quant8(ctx, X, groups, rows, n, block, q, s):
+    groups, rows, n, block = int(groups), int(rows), int(n), int(block)
+    codes, scales = _room8(groups, rows, n, block)
+    _check(lib().symi_quant8(ctx.ptr, _dev(X, ctx.torch_dtype, "X", groups * rows * n), groups, rows, n, block, _dev(q, E4M3, "q", codes),
+                             _dev(s, torch.uint8, "s", scales), _stream()), "symi_quant8")
+
+
+@_way_call
+def symi_dequant8(ctx, q, s, groups, rows, n, block, X):
+    groups, rows, n, block = int(groups), int(rows), int(n), int(block)
+    codes, scales = _room8(groups, rows, n, block)
+    _check(lib().symi_dequant8(ctx.ptr, _dev(q, E4M3, "q", codes), _dev(s, torch.uint8, "s", scales), groups, rows, n, block,
+                               _dev(X, ctx.torch_dtype, "X", groups * rows * n), _stream()), "symi_dequant8")
+
+
+@_way_call
+def symi_product8(ctx, Aq, As, slot_offsets, Wq, Ws, R, n, Y, ws):
+    R, n = int(R), int(n)
+    a, a_s = _room8(1, ctx.A, n, 1)
+    w, w_s = _room8(ctx.S_tot, R, n, 128)
+    _check(lib().symi_product8(
+        ctx.ptr, _dev(Aq, E4M3, "Aq", a), _dev(As, torch.uint8, "As", a_s), _dev(slot_offsets, I32, "slot_offsets", ctx.S_tot + 1),
+        _dev(Wq, E4M3, "Wq", w), _dev(Ws, torch.uint8, "Ws", w_s), R, n, _dev(Y, ctx.torch_dtype, "Y", ctx.A * R),
+        _dev(ws, torch.uint8, "ws", symi_workspace8_bytes(ctx.cfg)), _stream()), "symi_product8")
+
+
+@_way_call
+def symi_expert_fwd8(ctx, Xp, slot_offsets, W1q, W1s, W2q, W2s, UV, H, Yp, ws):
+    dt, A, d, f = ctx.torch_dtype, ctx.A, ctx.d, ctx.f
+    w1, w1_s = _room8(ctx.S_tot, 2 * f, d, 128)
+    w2, w2_s = _room8(ctx.S_tot, d, f, 128)
+    _check(lib().symi_expert_fwd8(
+        ctx.ptr, _dev(Xp, dt, "Xp", A * d), _dev(slot_offsets, I32, "slot_offsets", ctx.S_tot + 1), _dev(W1q, E4M3, "W1q", w1),
+        _dev(W1s, torch.uint8, "W1s", w1_s), _dev(W2q, E4M3, "W2q", w2), _dev(W2s, torch.uint8, "W2s", w2_s),
+        _dev_or_none(UV, dt, "UV", A * 2 * f), _dev_or_none(H, dt, "H", A * f), _dev(Yp, dt, "Yp", A * d),
+        _dev(ws, torch.uint8, "ws", symi_workspace8_bytes(ctx.cfg)), _stream()), "symi_expert_fwd8")

@@ -122,7 +122,8 @@ static const char* const g_names[K_COUNT] = {
     "gather_rows", "tile_map", "gemm_fwd1", "gemm_fwd2", "gemm_bwd_dh", "gemm_bwd_dx",
     "gemm_wgrad2", "gemm_wgrad1", "combine", "combine_bwd", "dispatch_bwd", "adam_to_replicas",
     "replica_allreduce", "router_fwd", "router_dx", "router_dw", "slice_sum",
-    "dispatch_one", "embed_fwd", "embed_sort", "embed_sum", "embed_join", "token_logp", "policy_loss", "policy_sum", "adamw", "adamw_decode"};
+    "dispatch_one", "embed_fwd", "embed_sort", "embed_sum", "embed_join", "token_logp", "policy_loss", "policy_sum", "adamw", "adamw_decode",
+    "norm", "norm_bwd", "norm_sum", "route_scored", "route_scored_bwd", "route_bias", "quant8", "dequant8", "tiles8", "product8", "expert8"};
 
 void timing_begin(const symi_ctx* ctx, int kid, hipStream_t st) {
   hipEvent_t e;

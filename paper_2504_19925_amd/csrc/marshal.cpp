@@ -28,7 +28,10 @@ namespace {
   X(symi_adam_to_replicas) X(symi_adam_to_replicas_active) X(symi_workspace_bytes)             \
   X(symi_embed_fwd) X(symi_embed_bwd) X(symi_embed_workspace_bytes) X(symi_token_logp)         \
   X(symi_policy_loss) X(symi_policy_workspace_bytes) X(symi_adamw_step) X(symi_adamw_values)   \
-  X(symi_adamw_decode)
+  X(symi_adamw_decode)                                                                         \
+  X(symi_norm_fwd) X(symi_norm_bwd) X(symi_norm_workspace_bytes) X(symi_route_scored)          \
+  X(symi_route_scored_bwd) X(symi_route_bias) X(symi_quant8) X(symi_dequant8)                  \
+  X(symi_product8) X(symi_expert_fwd8) X(symi_workspace8_bytes)
 
 // entry points of the loaded libsymi.so (addresses handed over by attach)
 struct Entries {
@@ -40,6 +43,7 @@ PyTypeObject* g_ctx_type = nullptr;    // binding.SymiCtx
 PyTypeObject* g_adam_type = nullptr;   // binding.SymiAdam
 PyTypeObject* g_policy_type = nullptr; // binding.SymiPolicy
 PyTypeObject* g_adamw_type = nullptr;  // binding.SymiAdamW
+PyTypeObject* g_score_type = nullptr;  // binding.SymiScore
 PyObject *g_ptr = nullptr, *g_cfg = nullptr, *g_stream = nullptr;   // interned attribute names
 
 // one argument of a C call: converts to the type of the parameter it is passed for
@@ -127,6 +131,14 @@ class Call {
     v.p = &pp_;
     return v;
   }
+  Val score(int i) {
+    Val v;
+    if (Py_TYPE(a_[i]) != g_score_type || !read_ctypes(a_[i], sp_)) { ok = false; return v; }
+    v.p = &sp_;
+    return v;
+  }
+  Val act_or_none(int i, long long n) { return a_[i] == Py_None ? Val() : act(i, n); }
+  Val codes(int i, long long n) { return tensor(i, at::kFloat8_e4m3fn, n); }
   // rows of logits, after policy()
   Val logits(int i, long long ld) { return tensor(i, pp_.logits_dtype == SYMI_BF16 ? at::kBFloat16 : at::kFloat, T * ld); }
   Val logits_or_none(int i, long long ld) { return a_[i] == Py_None ? Val() : logits(i, ld); }
@@ -197,6 +209,7 @@ class Call {
   symi_ctx* ctx_ = nullptr;
   symi_adam hp_;
   symi_policy pp_;
+  symi_score sp_;
   void* stream_ = nullptr;
   bool has_stream_ = false;
 };
@@ -367,11 +380,96 @@ DEF(symi_adamw_decode) {
   return c(g.symi_adamw_decode, v);
 }
 
-// attach({name: address}, SymiCtx, SymiAdam, SymiPolicy, SymiAdamW)
+DEF(symi_norm_fwd) {
+  Call c(a, n, 11);
+  if (!c.ok) Py_RETURN_NONE;
+  const long long x = c.T * c.d;
+  const Val v[] = {c.integer(1), c.real(2), c.act(3, x), c.act_or_none(4, x), c.f32_or_none(5, c.d), c.f32_or_none(6, c.d),
+                   c.act_or_none(7, x), c.act(8, x), c.f32_or_none(9, c.T), c.f32_or_none(10, c.T)};
+  return c(g.symi_norm_fwd, v);
+}
+DEF(symi_norm_bwd) {
+  Call c(a, n, 12);
+  if (!c.ok) Py_RETURN_NONE;
+  const long long x = c.T * c.d;
+  const Val v[] = {c.integer(1), c.act(2, x), c.act(3, x), c.f32_or_none(4, c.T), c.f32(5, c.T), c.f32_or_none(6, c.d),
+                   c.act_or_none(7, x), c.act(8, x), c.f32_or_none(9, c.d), c.f32_or_none(10, c.d),
+                   c.bytes(11, g.symi_norm_workspace_bytes(&c.c))};
+  return c(g.symi_norm_bwd, v);
+}
+DEF(symi_route_scored) {
+  Call c(a, n, 7);
+  if (!c.ok) Py_RETURN_NONE;
+  const Val v[] = {c.score(1), c.f32(2, c.T * c.E), c.f32_or_none(3, c.E), c.i32(4, c.A), c.f32(5, c.A), c.i32(6, c.E)};
+  return c(g.symi_route_scored, v);
+}
+DEF(symi_route_scored_bwd) {
+  Call c(a, n, 7);
+  if (!c.ok) Py_RETURN_NONE;
+  const Val v[] = {c.score(1), c.f32(2, c.T * c.E), c.i32(3, c.A), c.f32(4, c.A), c.f32(5, c.A), c.f32(6, c.T * c.E)};
+  return c(g.symi_route_scored_bwd, v);
+}
+DEF(symi_route_bias) {
+  Call c(a, n, 4);
+  if (!c.ok) Py_RETURN_NONE;
+  const Val v[] = {c.i32(1, c.E), c.real(2), c.f32(3, c.E)};
+  return c(g.symi_route_bias, v);
+}
+// elements of the codes and of the scales of values in 8 bits; sizes that the library refuses are not looked at here
+struct Room8 {
+  bool fine;
+  long long codes = 0, scales = 0;
+  Room8(long long groups, long long rows, long long n, long long block) : fine(groups >= 0 && rows >= 0 && n >= 1 && block >= 1) {
+    if (!fine || groups * rows > 0x7fffffffLL) { fine = false; return; }
+    const long long blocks = (n + 127) / 128;
+    codes = groups * rows * blocks * 128;
+    scales = groups * ((rows + block - 1) / block) * ((blocks + 3) / 4 * 4);
+  }
+};
+DEF(symi_quant8) {
+  Call c(a, n, 8);
+  if (!c.ok) Py_RETURN_NONE;
+  const Val groups = c.integer(2), rows = c.integer(3), cols = c.integer(4), block = c.integer(5);
+  const Room8 r(groups.i, rows.i, cols.i, block.i);
+  if (!c.ok || !r.fine) Py_RETURN_NONE;
+  const Val v[] = {c.act(1, (long long)groups.i * rows.i * cols.i), groups, rows, cols, block, c.codes(6, r.codes), c.bytes(7, r.scales)};
+  return c(g.symi_quant8, v);
+}
+DEF(symi_dequant8) {
+  Call c(a, n, 8);
+  if (!c.ok) Py_RETURN_NONE;
+  const Val groups = c.integer(3), rows = c.integer(4), cols = c.integer(5), block = c.integer(6);
+  const Room8 r(groups.i, rows.i, cols.i, block.i);
+  if (!c.ok || !r.fine) Py_RETURN_NONE;
+  const Val v[] = {c.codes(1, r.codes), c.bytes(2, r.scales), groups, rows, cols, block, c.act(7, (long long)groups.i * rows.i * cols.i)};
+  return c(g.symi_dequant8, v);
+}
+DEF(symi_product8) {
+  Call c(a, n, 10);
+  if (!c.ok) Py_RETURN_NONE;
+  const Val R = c.integer(6), cols = c.integer(7);
+  const Room8 x(1, c.A, cols.i, 1), w(c.S, R.i, cols.i, 128);
+  if (!c.ok || !x.fine || !w.fine) Py_RETURN_NONE;
+  const Val v[] = {c.codes(1, x.codes), c.bytes(2, x.scales), c.i32(3, c.S + 1), c.codes(4, w.codes), c.bytes(5, w.scales), R, cols,
+                   c.act(8, c.A * R.i), c.bytes(9, g.symi_workspace8_bytes(&c.c))};
+  return c(g.symi_product8, v);
+}
+DEF(symi_expert_fwd8) {
+  Call c(a, n, 11);
+  if (!c.ok) Py_RETURN_NONE;
+  const Room8 w1(c.S, 2 * c.f, c.d, 128), w2(c.S, c.d, c.f, 128);
+  if (!w1.fine || !w2.fine) Py_RETURN_NONE;
+  const Val v[] = {c.act(1, c.A * c.d), c.i32(2, c.S + 1), c.codes(3, w1.codes), c.bytes(4, w1.scales), c.codes(5, w2.codes),
+                   c.bytes(6, w2.scales), c.act_or_none(7, c.A * 2 * c.f), c.act_or_none(8, c.A * c.f), c.act(9, c.A * c.d),
+                   c.bytes(10, g.symi_workspace8_bytes(&c.c))};
+  return c(g.symi_expert_fwd8, v);
+}
+
+// attach({name: address}, SymiCtx, SymiAdam, SymiPolicy, SymiAdamW, SymiScore)
 PyObject* attach(PyObject*, PyObject* args) {
-  PyObject *addresses, *ctx_type, *adam_type, *policy_type, *adamw_type;
-  if (!PyArg_ParseTuple(args, "O!O!O!O!O!", &PyDict_Type, &addresses, &PyType_Type, &ctx_type, &PyType_Type, &adam_type,
-                        &PyType_Type, &policy_type, &PyType_Type, &adamw_type))
+  PyObject *addresses, *ctx_type, *adam_type, *policy_type, *adamw_type, *score_type;
+  if (!PyArg_ParseTuple(args, "O!O!O!O!O!O!", &PyDict_Type, &addresses, &PyType_Type, &ctx_type, &PyType_Type, &adam_type,
+                        &PyType_Type, &policy_type, &PyType_Type, &adamw_type, &PyType_Type, &score_type))
     return nullptr;
   Entries e;
 #define X(name)                                                                       \
@@ -390,6 +488,8 @@ PyObject* attach(PyObject*, PyObject* args) {
   Py_INCREF(adam_type);
   Py_INCREF(policy_type);
   Py_INCREF(adamw_type);
+  Py_INCREF(score_type);
+  g_score_type = reinterpret_cast<PyTypeObject*>(score_type);
   g_policy_type = reinterpret_cast<PyTypeObject*>(policy_type);
   g_adamw_type = reinterpret_cast<PyTypeObject*>(adamw_type);
   g_ctx_type = reinterpret_cast<PyTypeObject*>(ctx_type);
@@ -404,7 +504,8 @@ PyMethodDef methods[] = {
     M(symi_dispatch_bwd) M(symi_expert_fwd) M(symi_expert_bwd) M(symi_expert_bwd_slots) M(symi_expert_bwd_active)
     M(symi_replica_allreduce) M(symi_router_fwd) M(symi_router_bwd) M(symi_combine) M(symi_combine_bwd)
     M(symi_adam_to_replicas) M(symi_adam_to_replicas_active) M(symi_embed_fwd) M(symi_embed_bwd) M(symi_token_logp)
-    M(symi_policy_loss) M(symi_adamw_step) M(symi_adamw_decode)
+    M(symi_policy_loss) M(symi_adamw_step) M(symi_adamw_decode) M(symi_norm_fwd) M(symi_norm_bwd) M(symi_route_scored)
+    M(symi_route_scored_bwd) M(symi_route_bias) M(symi_quant8) M(symi_dequant8) M(symi_product8) M(symi_expert_fwd8)
     {"attach", attach, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};

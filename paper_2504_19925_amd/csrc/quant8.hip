@@ -1,0 +1,509 @@
+// symi_quant8 / symi_dequant8 / symi_product8 / symi_expert_fwd8: values in 8 bits with a power of two for every 128 along the reduction,
+// and the experts' products of them.
+//
+// The scales are the powers that v_mfma_scale_f32_16x16x128_f8f6f4 multiplies by itself: one instruction reduces exactly one block of 128, so a
+// product needs no vector work per block.  The instruction is issued with the weight as its first operand: a lane then has 4 consecutive
+// output columns of one row.  A lane holds 32 of the 128 reduction indices of one row of each operand; any 32, as long as they are the same in both.
+//
+// The 8-bit matrix instructions align the products of 8 neighbouring indices to the largest exponent among them and drop what is below 2^-13 of it; sums
+// of those, over the block and in the accumulator, are fp32 (probed with single products of 2^8 and 2^-j, a group's first and others).  Over random
+// values that is 1.5e-5 of a result (2-norm), a hundredth of what rounding it to bf16 is.  fp32 contexts want more: there codes become bf16
+// values, exactly, and the bf16 instruction, which keeps fp32's digits (8e-8), takes them at half the rate; the block's sum is scaled behind it.
+#include <algorithm>
+#include <type_traits>
+
+#include "common.h"
+
+namespace symi {
+
+typedef int intx8 __attribute__((ext_vector_type(8)));
+typedef int intx4_ __attribute__((ext_vector_type(4)));
+typedef float floatx4_ __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8_ __attribute__((ext_vector_type(8)));
+
+constexpr int QB = 128;               // values that share a power
+constexpr int Q_THREADS = 256;
+constexpr int MAX_N8 = 1 << 22;
+
+static int pitch8(int n) { return cdiv(n, QB) * QB; }
+static int scale_pitch8(int n) { return cdiv(cdiv(n, QB), 4) * 4; }
+
+// 8 values in fp32 from memory of the activation dtype
+template <bool BF16>
+__device__ __forceinline__ void load8q(const void* p, long long at, float (&x)[8]) {
+  if constexpr (BF16) {
+    const u32x4_bf16 r = *reinterpret_cast<const u32x4_bf16*>(static_cast<const uint16_t*>(p) + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(r[i] << 16);
+      x[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x4_f32 r = *reinterpret_cast<const f32x4_f32*>(static_cast<const float*>(p) + at + 4 * h);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 * h + i] = r[i];
+    }
+  }
+}
+
+// |x| as an integer, which orders as the value does; 0 for what is not finite
+__device__ __forceinline__ int size_of(float x) {
+  const int u = __float_as_int(x) & 0x7fffffff;
+  return u < 0x7f800000 ? u : 0;
+}
+// s of a block whose largest |x| has these bits: 448 = 1.75 * 2^8, so the exponent counts one more from 1.75 on
+__device__ __forceinline__ int scale_of(int most) { return max(((most + 0x1fffff) >> 23) - 8, 0); }
+__device__ __forceinline__ float inverse_of(int s) { return __int_as_float((254 - s) << 23); }      // 2^(127 - s), s <= 247
+__device__ __forceinline__ float power_of(int s) { return __int_as_float(s > 0 ? s << 23 : 1 << 22); }   // 2^(s - 127)
+
+// x 2^(127 - s) to e4m3, to nearest even; not finite: NaN
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
+  const float x[4] = {a, b, c, d};
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = size_of(x[i]) || (__float_as_int(x[i]) & 0x7fffffff) == 0 ? x[i] * inv : NAN;
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+  return (uint32_t)w;
+}
+
+// 16 lanes a block of a row.  limit: rows from *limit on are left out (nullptr: none are).
+template <bool BF16>
+__global__ __launch_bounds__(Q_THREADS) void quant_rows_kernel(const void* __restrict__ X, uint8_t* __restrict__ q, uint8_t* __restrict__ s,
+                                                               long long rows, int n, int p8, int sp, const int32_t* __restrict__ limit) {
+  if (limit) rows = min(rows, (long long)*limit);
+  const int l16 = threadIdx.x & 15;
+  const long long total = rows * sp, step = (long long)gridDim.x * (Q_THREADS / 16);
+  for (long long i = (long long)blockIdx.x * (Q_THREADS / 16) + (threadIdx.x >> 4); i < total; i += step) {
+    const long long r = i / sp;
+    const int blk = (int)(i - r * sp), c = blk * QB + l16 * 8;
+    if (blk * QB >= p8) {
+      if (l16 == 0) s[i] = 0;
+      continue;
+    }
+    float x[8] = {};
+    if (c < n) load8q<BF16>(X, r * n + c, x);
+    int most = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) most = max(most, size_of(x[j]));
+#pragma unroll
+    for (int m = 8; m >= 1; m >>= 1) most = max(most, __shfl_xor(most, m, 16));
+    const int e = scale_of(most);
+    const float inv = inverse_of(e);
+    *reinterpret_cast<uint2*>(q + r * p8 + c) = make_uint2(codes4(x[0], x[1], x[2], x[3], inv), codes4(x[4], x[5], x[6], x[7], inv));
+    if (l16 == 0) s[i] = (uint8_t)e;
+  }
+}
+
+// A workgroup a block of 128 x 128: 16 lanes a row, 16 rows at a time.
+template <bool BF16>
+__global__ __launch_bounds__(Q_THREADS) void quant_blocks_kernel(const void* __restrict__ X, uint8_t* __restrict__ q, uint8_t* __restrict__ s,
+                                                                 int rows, int n, int p8, int sp, int rb) {
+  __shared__ int part[Q_THREADS / 64];
+  const int bc = blockIdx.x % sp;
+  const long long br_all = blockIdx.x / sp;
+  const int group = (int)(br_all / rb), br = (int)(br_all - (long long)group * rb);
+  const int l16 = threadIdx.x & 15, c = bc * QB + l16 * 8;
+  const long long si = br_all * sp + bc;
+  if (bc * QB >= p8) {
+    if (threadIdx.x == 0) s[si] = 0;
+    return;
+  }
+  float x[8][8];
+  int most = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = br * QB + k * 16 + (threadIdx.x >> 4);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[k][j] = 0.f;
+    if (r < rows && c < n) load8q<BF16>(X, ((long long)group * rows + r) * n + c, x[k]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) most = max(most, size_of(x[k][j]));
+  }
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) most = max(most, __shfl_xor(most, m, 64));
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
+  __syncthreads();
+  most = max(max(part[0], part[1]), max(part[2], part[3]));
+  const int e = scale_of(most);
+  const float inv = inverse_of(e);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = br * QB + k * 16 + (threadIdx.x >> 4);
+    if (r < rows)
+      *reinterpret_cast<uint2*>(q + ((long long)group * rows + r) * p8 + c) =
+          make_uint2(codes4(x[k][0], x[k][1], x[k][2], x[k][3], inv), codes4(x[k][4], x[k][5], x[k][6], x[k][7], inv));
+  }
+  if (threadIdx.x == 0) s[si] = (uint8_t)e;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(Q_THREADS) void dequant_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ s, void* __restrict__ X,
+                                                            long long groups, int rows, int n, int p8, int sp, int rb, int block) {
+  const int per = n / 8;
+  const long long total = groups * rows * per, step = (long long)gridDim.x * Q_THREADS;
+  for (long long i = (long long)blockIdx.x * Q_THREADS + threadIdx.x; i < total; i += step) {
+    const long long row = i / per;
+    const int c = (int)(i - row * per) * 8;
+    const long long group = row / rows;
+    const int r = (int)(row - group * rows);
+    const float scale = power_of(s[(group * rb + r / block) * sp + c / QB]);
+    const uint2 w = *reinterpret_cast<const uint2*>(q + row * p8 + c);
+    float x[8];
+    const uint32_t ww[2] = {w.x, w.y};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)ww[h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)ww[h], true);
+      x[4 * h] = lo[0] * scale;
+      x[4 * h + 1] = lo[1] * scale;
+      x[4 * h + 2] = hi[0] * scale;
+      x[4 * h + 3] = hi[1] * scale;
+    }
+    if constexpr (BF16) {
+      u32x4_bf16 o;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
+      *reinterpret_cast<u32x4_bf16*>(static_cast<uint16_t*>(X) + row * n + c) = o;
+    } else {
+      float* const to = static_cast<float*>(X) + row * n + c;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4_f32 o = {x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
+        *reinterpret_cast<f32x4_f32*>(to + 4 * h) = o;
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- products
+constexpr int P_THREADS = 256;
+constexpr int THIN = 16;   // rows of a thin tile
+
+struct Product8 {
+  const uint8_t *Aq, *As, *Wq, *Ws;
+  const int32_t* slot_offsets;
+  const int32_t* map;   // [0]: tiles, then {first row, slot + 2^16 (rows - 1)} of each
+  void* Y;              // product: [rows, R]
+  uint16_t *UV, *H;     // experts' first product, or nullptr
+  uint8_t *Hq, *Hs;
+  int R, n, p8, sp;     // R: rows of a slot's weight (f in the experts' first product: gate and up rows each)
+  int hp8, hsp;         // pitches of Hq, Hs
+};
+
+// map of tiles of TM rows, slots one after the other
+template <int TM>
+__global__ __launch_bounds__(1024) void tiles8_kernel(const int32_t* __restrict__ offs, int S, int32_t* __restrict__ map) {
+  __shared__ int32_t part[1024];
+  const int tid = threadIdx.x, per = (S + 1023) / 1024, q0 = min(tid * per, S), q1 = min(q0 + per, S);
+  int mine = 0;
+  for (int q = q0; q < q1; ++q) mine += (offs[q + 1] - offs[q] + TM - 1) / TM;
+  part[tid] = mine;
+  __syncthreads();
+  for (int o = 1; o < 1024; o <<= 1) {
+    const int add = tid >= o ? part[tid - o] : 0;
+    __syncthreads();
+    part[tid] += add;
+    __syncthreads();
+  }
+  int t = part[tid] - mine;
+  if (tid == 1023) map[0] = part[1023];
+  for (int q = q0; q < q1; ++q)
+    for (int r = offs[q]; r < offs[q + 1]; r += TM, ++t) {
+      map[4 + 2 * t] = r;
+      map[5 + 2 * t] = q + ((min(offs[q + 1] - r, TM) - 1) << 16);
+    }
+}
+
+__device__ __forceinline__ float sigmoid8(float u) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * u)); }
+
+// 8 codes (half h of 16, in two words) as bf16 values
+__device__ __forceinline__ bf16x8_ widen(int lo, int hi) {
+  const int w[2] = {lo, hi};
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const auto x = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], false), y = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], true);
+    r[2 * i] = __builtin_amdgcn_perm(__float_as_uint(x[1]), __float_as_uint(x[0]), 0x07060302u);
+    r[2 * i + 1] = __builtin_amdgcn_perm(__float_as_uint(y[1]), __float_as_uint(y[0]), 0x07060302u);
+  }
+  struct { uint32_t x[4]; } u = {{r[0], r[1], r[2], r[3]}};
+  return __builtin_bit_cast(bf16x8_, u);
+}
+
+// acc += the products of a block, scaled
+template <bool BF16>
+__device__ __forceinline__ void block_product(floatx4_& acc, const intx8& fw, const intx8& fa, int sw, int sa) {
+  if constexpr (BF16) {
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw, fa, acc, 0, 0, 0, sw, 0, sa);
+  } else {
+    floatx4_ part = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int h = 0; h < 4; ++h) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(fw[2 * h], fw[2 * h + 1]), widen(fa[2 * h], fa[2 * h + 1]), part, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] += ldexpf(part[i], sw + sa - 254);   // one power for all of a weight's block
+  }
+}
+
+// A tile of 16 rows and 256 weight rows: wavefront w has 64 of them, in the experts' first product the gate and up rows of 32 hidden units.
+// Operands come straight from memory, 32 bytes a lane.
+template <bool BF16, bool EXPERT>
+__global__ __launch_bounds__(P_THREADS) void thin_product_kernel(Product8 p) {
+  const int tile = blockIdx.x;
+  if (tile >= p.map[0]) return;
+  const int row0 = p.map[4 + 2 * tile], entry = p.map[5 + 2 * tile], slot = entry & 0xffff, rows = (entry >> 16) + 1;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, quarter = lane >> 4;
+  const int slot_rows = EXPERT ? 2 * p.R : p.R, slot_blocks = (slot_rows + QB - 1) / QB;
+  // first weight row of the wavefront's column tile j
+  const int n0 = EXPERT ? blockIdx.y * 128 + wave * 32 : blockIdx.y * 256 + wave * 64;
+  const int arow = row0 + min(r16, rows - 1);
+  const uint8_t* const a = p.Aq + (long long)arow * p.p8 + quarter * 32;
+  const uint8_t* const as = p.As + (long long)arow * p.sp;
+  const uint8_t* w[4];
+  const uint8_t* ws[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int first = n0 + 16 * (EXPERT ? j & 1 : j);
+    int wr = min(first + r16, p.R - 1);
+    if (EXPERT && j >= 2) wr += p.R;
+    w[j] = p.Wq + ((long long)slot * slot_rows + wr) * p.p8 + quarter * 32;
+    ws[j] = p.Ws + ((long long)slot * slot_blocks + wr / QB) * p.sp;   // of this lane's weight row
+  }
+  floatx4_ acc[4] = {};
+  for (int k = 0; k < p.p8; k += QB) {
+    const int blk = k / QB;
+    intx8 fa;
+    {
+      const intx4_ lo = *reinterpret_cast<const intx4_*>(a + k), hi = *reinterpret_cast<const intx4_*>(a + k + 16);
+      fa = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    const int sa = as[blk];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const intx4_ lo = *reinterpret_cast<const intx4_*>(w[j] + k), hi = *reinterpret_cast<const intx4_*>(w[j] + k + 16);
+      const intx8 fw = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      block_product<BF16>(acc[j], fw, fa, ws[j][blk], sa);
+    }
+  }
+  const int row = row0 + r16;
+  const bool in = r16 < rows;
+  if constexpr (!EXPERT) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int col = n0 + 16 * j + 4 * quarter;
+      if (!in || col >= p.R) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (BF16) static_cast<uint16_t*>(p.Y)[(long long)row * p.R + col + i] = f32_to_bf16(acc[j][i]);
+        else static_cast<float*>(p.Y)[(long long)row * p.R + col + i] = acc[j][i];
+      }
+    }
+  } else {
+    __shared__ int part[4][16];
+    float h[2][4];
+    int most = 0;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int col = n0 + 16 * j + 4 * quarter + i;
+        const float u = acc[j][i], v = acc[j + 2][i];
+        h[j][i] = col < p.R ? u * sigmoid8(u) * v : 0.f;
+        most = max(most, size_of(h[j][i]));
+        if (in && col < p.R && p.UV) {
+          p.UV[(long long)row * 2 * p.R + col] = f32_to_bf16(u);
+          p.UV[(long long)row * 2 * p.R + p.R + col] = f32_to_bf16(v);
+          p.H[(long long)row * p.R + col] = f32_to_bf16(h[j][i]);
+        }
+      }
+    most = max(most, __shfl_xor(most, 16, 64));
+    most = max(most, __shfl_xor(most, 32, 64));
+    if (quarter == 0) part[wave][r16] = most;
+    __syncthreads();
+    most = max(max(part[0][r16], part[1][r16]), max(part[2][r16], part[3][r16]));
+    const int e = scale_of(most);
+    const float inv = inverse_of(e);
+    if (!in) return;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      *reinterpret_cast<uint32_t*>(p.Hq + (long long)row * p.hp8 + n0 + 16 * j + 4 * quarter) = codes4(h[j][0], h[j][1], h[j][2], h[j][3], inv);
+    uint8_t* const hs = p.Hs + (long long)row * p.hsp;
+    if (wave == 0 && quarter == 0) hs[blockIdx.y] = (uint8_t)e;
+    // zeros behind the last block
+    if (blockIdx.y == gridDim.y - 1 && wave == 0 && quarter == 0)
+      for (int b = gridDim.y; b < p.hsp; ++b) hs[b] = 0;
+  }
+}
+
+struct Ws8 {
+  size_t xq, xs, hq, hs, map, total;
+};
+static Ws8 ws8_layout(const symi_cfg* c) {
+  Ws8 L;
+  const size_t A = (size_t)c->T * c->k;
+  size_t off = 0;
+  L.xq = off;
+  off += align_up(A * pitch8(c->d), 256);
+  L.xs = off;
+  off += align_up(A * scale_pitch8(c->d), 256);
+  L.hq = off;
+  off += align_up(A * pitch8(c->f), 256);
+  L.hs = off;
+  off += align_up(A * scale_pitch8(c->f), 256);
+  L.map = off;
+  off += align_up((4 + 2 * (A / THIN + c->S_tot + 1)) * sizeof(int32_t), 256);
+  L.total = off + 256;
+  return L;
+}
+
+static void launch_tiles(const symi_ctx* ctx, const int32_t* offs, int32_t* map, hipStream_t st) {
+  SYMI_TIMED(ctx, K_TILES8, st, (tiles8_kernel<THIN><<<1, 1024, 0, st>>>(offs, ctx->cfg.S_tot, map)));
+}
+
+static void launch_quant_rows(const symi_ctx* ctx, bool bf16, const void* X, void* q, void* s, long long rows, int n, const int32_t* limit,
+                              hipStream_t st) {
+  const int sp = scale_pitch8(n);
+  const int grid = (int)std::min<long long>((rows * sp + 15) / 16, 1 << 20);
+  if (bf16)
+    SYMI_TIMED(ctx, K_QUANT8, st, (quant_rows_kernel<true><<<grid, Q_THREADS, 0, st>>>(X, (uint8_t*)q, (uint8_t*)s, rows, n, pitch8(n), sp, limit)));
+  else
+    SYMI_TIMED(ctx, K_QUANT8, st, (quant_rows_kernel<false><<<grid, Q_THREADS, 0, st>>>(X, (uint8_t*)q, (uint8_t*)s, rows, n, pitch8(n), sp, limit)));
+}
+
+static int check_codes(const void* q, const void* s, const char* who) {
+  SYMI_REQUIRE(((size_t)q & 15) == 0, who, "codes must be 16-byte aligned");
+  SYMI_REQUIRE(((size_t)s & 3) == 0, who, "scales must be 4-byte aligned");
+  return SYMI_OK;
+}
+
+static int check_values(int groups, int rows, int n, int block, const char* who) {
+  SYMI_REQUIRE(groups >= 0 && rows >= 0, who, "negative number of groups or rows");
+  SYMI_REQUIRE(n >= 8 && n % 8 == 0 && n <= MAX_N8, who, "n must be a multiple of 8, from 8 to 2^22");
+  SYMI_REQUIRE(block == 1 || block == QB, who, "block must be 1 or 128");
+  if ((long long)groups * rows > 0x7fffffffLL) {
+    set_error("%s: more than 2^31 - 1 rows", who);
+    return SYMI_EUNSUPPORTED;
+  }
+  return SYMI_OK;
+}
+
+}  // namespace symi
+
+using namespace symi;
+
+extern "C" int symi_pitch8(int n) {
+  if (check_values(1, 1, n, 1, "symi_pitch8")) return SYMI_EINVAL;
+  return pitch8(n);
+}
+extern "C" int symi_scale_pitch8(int n) {
+  if (check_values(1, 1, n, 1, "symi_scale_pitch8")) return SYMI_EINVAL;
+  return scale_pitch8(n);
+}
+
+extern "C" size_t symi_workspace8_bytes(const symi_cfg* cfg) {
+  if (check_cfg(cfg, "symi_workspace8_bytes") != SYMI_OK) return 0;
+  return ws8_layout(cfg).total;
+}
+
+extern "C" int symi_quant8(const symi_ctx* ctx, const void* X, int groups, int rows, int n, int block, void* q, void* s, void* stream) {
+  SYMI_ENTER(ctx, "symi_quant8");
+  if (int rc = check_values(groups, rows, n, block, "symi_quant8")) return rc;
+  if (groups == 0 || rows == 0) return SYMI_OK;
+  SYMI_REQUIRE(X && q && s, "symi_quant8", "NULL pointer");
+  if (int rc = check_codes(q, s, "symi_quant8")) return rc;
+  hipStream_t st = as_stream(stream);
+  const bool bf16 = cfg->dtype == SYMI_BF16;
+  if (block == 1) {
+    launch_quant_rows(ctx, bf16, X, q, s, (long long)groups * rows, n, nullptr, st);
+  } else {
+    const int sp = scale_pitch8(n), rb = cdiv(rows, QB);
+    const long long blocks = (long long)groups * rb * sp;
+    if (blocks > 0x7fffffffLL) {
+      set_error("symi_quant8: more than 2^31 - 1 blocks");
+      return SYMI_EUNSUPPORTED;
+    }
+    if (bf16)
+      SYMI_TIMED(ctx, K_QUANT8, st, (quant_blocks_kernel<true><<<(unsigned)blocks, Q_THREADS, 0, st>>>(X, (uint8_t*)q, (uint8_t*)s, rows, n, pitch8(n), sp, rb)));
+    else
+      SYMI_TIMED(ctx, K_QUANT8, st, (quant_blocks_kernel<false><<<(unsigned)blocks, Q_THREADS, 0, st>>>(X, (uint8_t*)q, (uint8_t*)s, rows, n, pitch8(n), sp, rb)));
+  }
+  SYMI_LAUNCH_CHECK("symi_quant8");
+  return SYMI_OK;
+}
+
+extern "C" int symi_dequant8(const symi_ctx* ctx, const void* q, const void* s, int groups, int rows, int n, int block, void* X, void* stream) {
+  SYMI_ENTER(ctx, "symi_dequant8");
+  if (int rc = check_values(groups, rows, n, block, "symi_dequant8")) return rc;
+  if (groups == 0 || rows == 0) return SYMI_OK;
+  SYMI_REQUIRE(X && q && s, "symi_dequant8", "NULL pointer");
+  if (int rc = check_codes(q, s, "symi_dequant8")) return rc;
+  hipStream_t st = as_stream(stream);
+  const int sp = scale_pitch8(n), rb = cdiv(rows, block);
+  const long long pieces = (long long)groups * rows * (n / 8);
+  const int grid = (int)std::min<long long>((pieces + Q_THREADS - 1) / Q_THREADS, 1 << 20);
+  if (cfg->dtype == SYMI_BF16)
+    SYMI_TIMED(ctx, K_DEQUANT8, st, (dequant_kernel<true><<<grid, Q_THREADS, 0, st>>>((const uint8_t*)q, (const uint8_t*)s, X, groups, rows, n, pitch8(n), sp, rb, block)));
+  else
+    SYMI_TIMED(ctx, K_DEQUANT8, st, (dequant_kernel<false><<<grid, Q_THREADS, 0, st>>>((const uint8_t*)q, (const uint8_t*)s, X, groups, rows, n, pitch8(n), sp, rb, block)));
+  SYMI_LAUNCH_CHECK("symi_dequant8");
+  return SYMI_OK;
+}
+
+extern "C" int symi_product8(const symi_ctx* ctx, const void* Aq, const void* As, const int32_t* slot_offsets, const void* Wq, const void* Ws,
+                             int R, int n, void* Y, void* ws, void* stream) {
+  SYMI_ENTER(ctx, "symi_product8");
+  if (int rc = check_values(1, R, n, 1, "symi_product8")) return rc;
+  SYMI_REQUIRE(R >= 8 && R % 8 == 0 && R <= MAX_N8, "symi_product8", "R must be a multiple of 8, from 8 to 2^22");
+  if (cfg->T == 0) return SYMI_OK;
+  SYMI_REQUIRE(Aq && As && slot_offsets && Wq && Ws && Y && ws, "symi_product8", "NULL pointer");
+  if (int rc = check_codes(Aq, As, "symi_product8")) return rc;
+  if (int rc = check_codes(Wq, Ws, "symi_product8")) return rc;
+  hipStream_t st = as_stream(stream);
+  int32_t* const map = reinterpret_cast<int32_t*>(align_up((size_t)ws, 256) + ws8_layout(cfg).map);
+  launch_tiles(ctx, slot_offsets, map, st);
+  const Product8 p = {(const uint8_t*)Aq, (const uint8_t*)As, (const uint8_t*)Wq, (const uint8_t*)Ws, slot_offsets, map, Y,
+                      nullptr, nullptr, nullptr, nullptr, R, n, pitch8(n), scale_pitch8(n), 0, 0};
+  const dim3 grid(cfg->T * cfg->k / THIN + cfg->S_tot, cdiv(R, 256));
+  if (cfg->dtype == SYMI_BF16) SYMI_TIMED(ctx, K_PRODUCT8, st, (thin_product_kernel<true, false><<<grid, P_THREADS, 0, st>>>(p)));
+  else SYMI_TIMED(ctx, K_PRODUCT8, st, (thin_product_kernel<false, false><<<grid, P_THREADS, 0, st>>>(p)));
+  SYMI_LAUNCH_CHECK("symi_product8");
+  return SYMI_OK;
+}
+
+extern "C" int symi_expert_fwd8(const symi_ctx* ctx, const void* Xp, const int32_t* slot_offsets, const void* W1q, const void* W1s, const void* W2q,
+                                const void* W2s, void* UV, void* H, void* Yp, void* ws, void* stream) {
+  SYMI_ENTER(ctx, "symi_expert_fwd8");
+  if (cfg->dtype != SYMI_BF16) {
+    set_error("symi_expert_fwd8: 8-bit experts need a bf16 context");
+    return SYMI_EUNSUPPORTED;
+  }
+  SYMI_REQUIRE((UV != nullptr) == (H != nullptr), "symi_expert_fwd8", "UV and H: both or neither");
+  if (cfg->T == 0) return SYMI_OK;
+  SYMI_REQUIRE(Xp && slot_offsets && W1q && W1s && W2q && W2s && Yp && ws, "symi_expert_fwd8", "NULL pointer");
+  if (int rc = check_codes(W1q, W1s, "symi_expert_fwd8")) return rc;
+  if (int rc = check_codes(W2q, W2s, "symi_expert_fwd8")) return rc;
+  hipStream_t st = as_stream(stream);
+  const Ws8 L = ws8_layout(cfg);
+  uint8_t* const base = reinterpret_cast<uint8_t*>(align_up((size_t)ws, 256));
+  const int d = cfg->d, f = cfg->f, A = cfg->T * cfg->k;
+  int32_t* const map = reinterpret_cast<int32_t*>(base + L.map);
+  launch_tiles(ctx, slot_offsets, map, st);
+  launch_quant_rows(ctx, true, Xp, base + L.xq, base + L.xs, A, d, slot_offsets + cfg->S_tot, st);
+  Product8 p = {base + L.xq, base + L.xs, (const uint8_t*)W1q, (const uint8_t*)W1s, slot_offsets, map, nullptr, (uint16_t*)UV, (uint16_t*)H,
+                base + L.hq, base + L.hs, f, d, pitch8(d), scale_pitch8(d), pitch8(f), scale_pitch8(f)};
+  const int tiles = A / THIN + cfg->S_tot;
+  SYMI_TIMED(ctx, K_EXPERT8, st, (thin_product_kernel<true, true><<<dim3(tiles, cdiv(f, 128)), P_THREADS, 0, st>>>(p)));
+  p.Aq = base + L.hq;
+  p.As = base + L.hs;
+  p.Wq = (const uint8_t*)W2q;
+  p.Ws = (const uint8_t*)W2s;
+  p.Y = Yp;
+  p.R = d;
+  p.n = f;
+  p.p8 = pitch8(f);
+  p.sp = scale_pitch8(f);
+  SYMI_TIMED(ctx, K_PRODUCT8, st, (thin_product_kernel<true, false><<<dim3(tiles, cdiv(d, 256)), P_THREADS, 0, st>>>(p)));
+  SYMI_LAUNCH_CHECK("symi_expert_fwd8");
+  return SYMI_OK;
+}
