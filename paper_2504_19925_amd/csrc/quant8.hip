@@ -12,16 +12,10 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "common.h"
+#include "quant8.h"
 
 namespace symi {
 
-typedef int intx8 __attribute__((ext_vector_type(8)));
-typedef int intx4_ __attribute__((ext_vector_type(4)));
-typedef float floatx4_ __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8_ __attribute__((ext_vector_type(8)));
-
-constexpr int QB = 128;               // values that share a power
 constexpr int Q_THREADS = 256;
 constexpr int MAX_N8 = 1 << 22;
 
@@ -46,27 +40,6 @@ __device__ __forceinline__ void load8q(const void* p, long long at, float (&x)[8
       for (int i = 0; i < 4; ++i) x[4 * h + i] = r[i];
     }
   }
-}
-
-// |x| as an integer, which orders as the value does; 0 for what is not finite
-__device__ __forceinline__ int size_of(float x) {
-  const int u = __float_as_int(x) & 0x7fffffff;
-  return u < 0x7f800000 ? u : 0;
-}
-// s of a block whose largest |x| has these bits: 448 = 1.75 * 2^8, so the exponent counts one more from 1.75 on
-__device__ __forceinline__ int scale_of(int most) { return max(((most + 0x1fffff) >> 23) - 8, 0); }
-__device__ __forceinline__ float inverse_of(int s) { return __int_as_float((254 - s) << 23); }      // 2^(127 - s), s <= 247
-__device__ __forceinline__ float power_of(int s) { return __int_as_float(s > 0 ? s << 23 : 1 << 22); }   // 2^(s - 127)
-
-// x 2^(127 - s) to e4m3, to nearest even; not finite: NaN
-__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
-  const float x[4] = {a, b, c, d};
-  float y[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = size_of(x[i]) || (__float_as_int(x[i]) & 0x7fffffff) == 0 ? x[i] * inv : NAN;
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
-  return (uint32_t)w;
 }
 
 // 16 lanes a block of a row.  limit: rows from *limit on are left out (nullptr: none are).
@@ -181,17 +154,6 @@ __global__ __launch_bounds__(Q_THREADS) void dequant_kernel(const uint8_t* __res
 constexpr int P_THREADS = 256;
 constexpr int THIN = 16;   // rows of a thin tile
 
-struct Product8 {
-  const uint8_t *Aq, *As, *Wq, *Ws;
-  const int32_t* slot_offsets;
-  const int32_t* map;   // [0]: tiles, then {first row, slot + 2^16 (rows - 1)} of each
-  void* Y;              // product: [rows, R]
-  uint16_t *UV, *H;     // experts' first product, or nullptr
-  uint8_t *Hq, *Hs;
-  int R, n, p8, sp;     // R: rows of a slot's weight (f in the experts' first product: gate and up rows each)
-  int hp8, hsp;         // pitches of Hq, Hs
-};
-
 // map of tiles of TM rows, slots one after the other
 template <int TM>
 __global__ __launch_bounds__(1024) void tiles8_kernel(const int32_t* __restrict__ offs, int S, int32_t* __restrict__ map) {
@@ -215,8 +177,6 @@ __global__ __launch_bounds__(1024) void tiles8_kernel(const int32_t* __restrict_
       map[5 + 2 * t] = q + ((min(offs[q + 1] - r, TM) - 1) << 16);
     }
 }
-
-__device__ __forceinline__ float sigmoid8(float u) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * u)); }
 
 // 8 codes (half h of 16, in two words) as bf16 values
 __device__ __forceinline__ bf16x8_ widen(int lo, int hi) {
@@ -357,8 +317,23 @@ static Ws8 ws8_layout(const symi_cfg* c) {
   return L;
 }
 
+// Whether the products of a context take the tiles of 256 rows
+static bool many_rows(const symi_cfg* c) { return c->dtype == SYMI_BF16 && (long long)c->T * c->k > 32LL * c->S_tot; }
+
 static void launch_tiles(const symi_ctx* ctx, const int32_t* offs, int32_t* map, hipStream_t st) {
-  SYMI_TIMED(ctx, K_TILES8, st, (tiles8_kernel<THIN><<<1, 1024, 0, st>>>(offs, ctx->cfg.S_tot, map)));
+  if (many_rows(&ctx->cfg)) SYMI_TIMED(ctx, K_TILES8, st, (tiles8_kernel<256><<<1, 1024, 0, st>>>(offs, ctx->cfg.S_tot, map)));
+  else SYMI_TIMED(ctx, K_TILES8, st, (tiles8_kernel<THIN><<<1, 1024, 0, st>>>(offs, ctx->cfg.S_tot, map)));
+}
+
+static void launch_product(const symi_ctx* ctx, const Product8& p, bool expert, hipStream_t st) {
+  if (many_rows(&ctx->cfg)) return launch_gemm8(ctx, p, expert, st);
+  const int tiles = ctx->cfg.T * ctx->cfg.k / THIN + ctx->cfg.S_tot;
+  if (expert)
+    SYMI_TIMED(ctx, K_EXPERT8, st, (thin_product_kernel<true, true><<<dim3(tiles, cdiv(p.R, 128)), P_THREADS, 0, st>>>(p)));
+  else if (ctx->cfg.dtype == SYMI_BF16)
+    SYMI_TIMED(ctx, K_PRODUCT8, st, (thin_product_kernel<true, false><<<dim3(tiles, cdiv(p.R, 256)), P_THREADS, 0, st>>>(p)));
+  else
+    SYMI_TIMED(ctx, K_PRODUCT8, st, (thin_product_kernel<false, false><<<dim3(tiles, cdiv(p.R, 256)), P_THREADS, 0, st>>>(p)));
 }
 
 static void launch_quant_rows(const symi_ctx* ctx, bool bf16, const void* X, void* q, void* s, long long rows, int n, const int32_t* limit,
@@ -464,9 +439,7 @@ extern "C" int symi_product8(const symi_ctx* ctx, const void* Aq, const void* As
   launch_tiles(ctx, slot_offsets, map, st);
   const Product8 p = {(const uint8_t*)Aq, (const uint8_t*)As, (const uint8_t*)Wq, (const uint8_t*)Ws, slot_offsets, map, Y,
                       nullptr, nullptr, nullptr, nullptr, R, n, pitch8(n), scale_pitch8(n), 0, 0};
-  const dim3 grid(cfg->T * cfg->k / THIN + cfg->S_tot, cdiv(R, 256));
-  if (cfg->dtype == SYMI_BF16) SYMI_TIMED(ctx, K_PRODUCT8, st, (thin_product_kernel<true, false><<<grid, P_THREADS, 0, st>>>(p)));
-  else SYMI_TIMED(ctx, K_PRODUCT8, st, (thin_product_kernel<false, false><<<grid, P_THREADS, 0, st>>>(p)));
+  launch_product(ctx, p, false, st);
   SYMI_LAUNCH_CHECK("symi_product8");
   return SYMI_OK;
 }
@@ -492,8 +465,7 @@ extern "C" int symi_expert_fwd8(const symi_ctx* ctx, const void* Xp, const int32
   launch_quant_rows(ctx, true, Xp, base + L.xq, base + L.xs, A, d, slot_offsets + cfg->S_tot, st);
   Product8 p = {base + L.xq, base + L.xs, (const uint8_t*)W1q, (const uint8_t*)W1s, slot_offsets, map, nullptr, (uint16_t*)UV, (uint16_t*)H,
                 base + L.hq, base + L.hs, f, d, pitch8(d), scale_pitch8(d), pitch8(f), scale_pitch8(f)};
-  const int tiles = A / THIN + cfg->S_tot;
-  SYMI_TIMED(ctx, K_EXPERT8, st, (thin_product_kernel<true, true><<<dim3(tiles, cdiv(f, 128)), P_THREADS, 0, st>>>(p)));
+  launch_product(ctx, p, true, st);
   p.Aq = base + L.hq;
   p.As = base + L.hs;
   p.Wq = (const uint8_t*)W2q;
@@ -503,7 +475,7 @@ extern "C" int symi_expert_fwd8(const symi_ctx* ctx, const void* Xp, const int32
   p.n = f;
   p.p8 = pitch8(f);
   p.sp = scale_pitch8(f);
-  SYMI_TIMED(ctx, K_PRODUCT8, st, (thin_product_kernel<true, false><<<dim3(tiles, cdiv(d, 256)), P_THREADS, 0, st>>>(p)));
+  launch_product(ctx, p, false, st);
   SYMI_LAUNCH_CHECK("symi_expert_fwd8");
   return SYMI_OK;
 }
