@@ -2,6 +2,11 @@
 //
 // mean = sum R / d, rstd = 1 / sqrt(sum (R - mean)^2 / d + eps), Y = (R - mean) rstd w + b;
 // with xh = (R - mean) rstd and g = dY w: dX = rstd (g - sum g / d - xh sum(g xh) / d) + dR, dw = sum dY xh, db = sum dY.
+//
+// Bound by bytes: a row is read once, stays in registers from its sums to its results and is written once; w and b are read once a workgroup.
+// 65536 rows of 4096 in bf16 with a residual sum: forward 385 us (5.6 TB/s), gradients 390 us (5.5 TB/s, 9 of them the sums over the workgroups).  What
+// it takes for that is few rows at a time, next to each other in memory: the forward pass with 16 to 24 KB of loads on their way to a compute unit 385, with
+// twice as many 407; the gradients with 512 workgroups of every 512th row 390, with 1024 of them 407, with 512 of consecutive rows 424.
 #include <math.h>
 
 #include <algorithm>
@@ -11,52 +16,106 @@
 
 namespace symi {
 
-constexpr int NORM_THREADS = 256;
-constexpr int NORM_CHUNKS = 512;   // partial sums of dw and db at most
+constexpr int WIDE_THREADS = 1024;
+constexpr int NORM_PARTS = 512;        // workgroups of the gradients, and so partial sums of dw and db, at most
+constexpr int NORM_FLYING = 24576;     // bytes on their way to a compute unit
+constexpr int NORM_IN_REGS = 16384, NORM_BWD_IN_REGS = 8192;   // widest rows that stay in registers
 
-// 8 consecutive values of a row, in registers as fp32.
-template <bool BF16>
-__device__ __forceinline__ void load8(const void* p, long long at, float (&x)[8]) {
-  if constexpr (BF16) {
-    const u32x4_bf16 r = *reinterpret_cast<const u32x4_bf16*>(static_cast<const uint16_t*>(p) + at);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(r[i] << 16);
-      x[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
-    }
-  } else {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const f32x4_f32 r = *reinterpret_cast<const f32x4_f32*>(static_cast<const float*>(p) + at + 4 * h);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[4 * h + i] = r[i];
+// 8 consecutive values of a row as they lie in memory: 16 or 32 bytes.
+template <bool BF16> struct Eight {
+  typedef uint32_t Raw __attribute__((ext_vector_type(4)));
+  Raw r[BF16 ? 1 : 2];
+  __device__ __forceinline__ void load(const void* p, long long at) {
+    if constexpr (BF16) {
+      r[0] = __builtin_bit_cast(Raw, *reinterpret_cast<const u32x4_bf16*>(static_cast<const uint16_t*>(p) + at));
+    } else {
+      const float* const q = static_cast<const float*>(p) + at;
+      r[0] = __builtin_bit_cast(Raw, *reinterpret_cast<const f32x4_f32*>(q));
+      r[1] = __builtin_bit_cast(Raw, *reinterpret_cast<const f32x4_f32*>(q + 4));
     }
   }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int h = 0; h < (BF16 ? 1 : 2); ++h) r[h] = Raw{0, 0, 0, 0};
+  }
+  __device__ __forceinline__ void unpack(float (&x)[8]) const {
+    if constexpr (BF16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(r[0][i] << 16);
+        x[2 * i + 1] = __uint_as_float(r[0][i] & 0xffff0000u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r[i >> 2][i & 3]);
+    }
+  }
+  __device__ __forceinline__ void pack(const float (&x)[8]) {
+    if constexpr (BF16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[0][i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i >> 2][i & 3] = __float_as_uint(x[i]);
+    }
+  }
+  __device__ __forceinline__ void store(void* p, long long at) const {
+    if constexpr (BF16) {
+      *reinterpret_cast<u32x4_bf16*>(static_cast<uint16_t*>(p) + at) = __builtin_bit_cast(u32x4_bf16, r[0]);
+    } else {
+      float* const q = static_cast<float*>(p) + at;
+      *reinterpret_cast<f32x4_f32*>(q) = __builtin_bit_cast(f32x4_f32, r[0]);
+      *reinterpret_cast<f32x4_f32*>(q + 4) = __builtin_bit_cast(f32x4_f32, r[1]);
+    }
+  }
+};
+// 8 of w or b, or what stands for them
+__device__ __forceinline__ void load_weights(const float* p, int c, int d, float none, float (&x)[8]) {
+  if (p && c < d) {
+    Eight<false> e;
+    e.load(p, c);
+    e.unpack(x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = none;
+  }
+}
+template <bool BF16>
+__device__ __forceinline__ void load8(const void* p, long long at, float (&x)[8]) {
+  Eight<BF16> e;
+  e.load(p, at);
+  e.unpack(x);
 }
 template <bool BF16>
 __device__ __forceinline__ void store8(void* p, long long at, const float (&x)[8]) {
-  if constexpr (BF16) {
-    u32x4_bf16 r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
-    *reinterpret_cast<u32x4_bf16*>(static_cast<uint16_t*>(p) + at) = r;
-  } else {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const f32x4_f32 r = {x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
-      *reinterpret_cast<f32x4_f32*>(static_cast<float*>(p) + at + 4 * h) = r;
-    }
-  }
+  Eight<BF16> e;
+  e.pack(x);
+  e.store(p, at);
 }
-template <bool BF16>
-__device__ __forceinline__ float as_stored(float x) {
-  if constexpr (BF16) return bf16_to_f32(f32_to_bf16(x)); else return x;
+// Sum over groups of LANES (16 or 64) lanes, which all get it: rotations within 16 lanes, then two broadcasts of a row's last lane, as operands of the
+// additions themselves (through ds_bpermute a sum over 64 lanes took 0.3 us).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float plus_dpp(float x) {
+  return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, ROWS, 0xf, false));
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float x) {
+  static_assert(LANES == 16 || LANES == 64, "a row of lanes or all of them");
+  x = plus_dpp<0x128, 0xf>(x);   // row_ror:8
+  x = plus_dpp<0x124, 0xf>(x);
+  x = plus_dpp<0x122, 0xf>(x);
+  x = plus_dpp<0x121, 0xf>(x);
+  if constexpr (LANES == 64) {
+    x = plus_dpp<0x142, 0xa>(x);   // row_bcast:15 into rows 1 and 3
+    x = plus_dpp<0x143, 0xc>(x);   // row_bcast:31 into rows 2 and 3
+    x = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+  }
+  return x;
 }
 
 // Sum over a workgroup, in the same order always; every thread gets it.
 __device__ __forceinline__ float block_sum(float x, float* part) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, 64);
+  x = lanes_sum<64>(x);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
   __syncthreads();
@@ -65,23 +124,26 @@ __device__ __forceinline__ float block_sum(float x, float* part) {
   return s;
 }
 
-// One workgroup a row; a thread reads back what it wrote itself.
+// Rows beyond that: one workgroup a row, read three times; a thread reads back what it wrote itself.
 template <bool BF16>
-__global__ __launch_bounds__(NORM_THREADS) void norm_kernel(const void* X, const void* res, const float* __restrict__ w,
-                                                            const float* __restrict__ b, void* R, void* Y, float* __restrict__ mean_out,
-                                                            float* __restrict__ rstd_out, int d, int center, float eps) {
-  __shared__ float part[NORM_THREADS / 64];
+__global__ __launch_bounds__(WIDE_THREADS) void norm_wide_kernel(const void* X, const void* res, const float* __restrict__ w,
+                                                                 const float* __restrict__ b, void* R, void* Y, float* __restrict__ mean_out,
+                                                                 float* __restrict__ rstd_out, int d, int center, float eps) {
+  __shared__ float part[WIDE_THREADS / 64];
   const long long row = (long long)blockIdx.x * d;
   float s = 0.f;
-  for (int c = threadIdx.x * 8; c < d; c += NORM_THREADS * 8) {
+  for (int c = threadIdx.x * 8; c < d; c += WIDE_THREADS * 8) {
     float x[8];
     load8<BF16>(X, row + c, x);
     if (res) {
       float y[8];
       load8<BF16>(res, row + c, y);
+      Eight<BF16> e;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = as_stored<BF16>(x[i] + y[i]);
-      store8<BF16>(R, row + c, x);
+      for (int i = 0; i < 8; ++i) x[i] += y[i];
+      e.pack(x);
+      e.store(R, row + c);
+      e.unpack(x);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) s += x[i];
@@ -89,14 +151,14 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_kernel(const void* X, const
   const void* const from = res ? R : X;
   const float mean = center ? block_sum(s, part) / (float)d : 0.f;
   float q = 0.f;
-  for (int c = threadIdx.x * 8; c < d; c += NORM_THREADS * 8) {
+  for (int c = threadIdx.x * 8; c < d; c += WIDE_THREADS * 8) {
     float x[8];
     load8<BF16>(from, row + c, x);
 #pragma unroll
     for (int i = 0; i < 8; ++i) q += (x[i] - mean) * (x[i] - mean);
   }
   const float rstd = 1.f / sqrtf(block_sum(q, part) / (float)d + eps);
-  for (int c = threadIdx.x * 8; c < d; c += NORM_THREADS * 8) {
+  for (int c = threadIdx.x * 8; c < d; c += WIDE_THREADS * 8) {
     float x[8];
     load8<BF16>(from, row + c, x);
 #pragma unroll
@@ -109,15 +171,119 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_kernel(const void* X, const
   }
 }
 
+// A row in the registers of LANES threads, NV pieces of 8 values each; what they are goes by d alone, and with it every sum's order.
+template <int LANES>
+struct Rows {
+  static constexpr int THREADS = LANES > 256 ? LANES : 256;
+  static constexpr int AT_ONCE = THREADS / LANES;   // rows of a workgroup
+  // groups of threads whose sums for dw and db are added up in the end
+  static constexpr int GROUPS = LANES <= 64 ? THREADS / 64 : AT_ONCE;
+};
+
+// Sum over the threads of a row; the two partial arrays take turns, so that one barrier a sum is enough.
+template <int LANES>
+__device__ __forceinline__ float row_sum(float x, float (*part)[16], int& turn) {
+  x = lanes_sum<(LANES < 64 ? LANES : 64)>(x);
+  if constexpr (LANES > 64) {
+    if ((threadIdx.x & 63) == 0) part[turn][threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = 0.f;
+#pragma unroll
+    for (int w = 0; w < LANES / 64; ++w) x += part[turn][threadIdx.x / LANES * (LANES / 64) + w];
+    turn ^= 1;
+  }
+  return x;
+}
+
+// Workgroups go through the rows with w and b in registers, the next row's loads in flight.
+template <bool BF16, int LANES, int NV, bool RES>
+__global__ __launch_bounds__(Rows<LANES>::THREADS) void norm_kernel(const void* X, const void* res, const float* __restrict__ w,
+                                                                        const float* __restrict__ b, void* R, void* Y, float* __restrict__ mean_out,
+                                                                        float* __restrict__ rstd_out, int T, int d, int center, float eps) {
+  using G = Rows<LANES>;
+  __shared__ float part[2][16];
+  int turn = 0;
+  const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+  float ww[NV][8], bb[NV][8];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = (v * LANES + l) * 8;
+    load_weights(w, c, d, 1.f, ww[v]);
+    load_weights(b, c, d, 0.f, bb[v]);
+  }
+  const int step = gridDim.x * G::AT_ONCE;
+  Eight<BF16> x[NV], y[NV];
+  auto fetch = [&](long long t) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * LANES + l) * 8;
+      x[v].clear();
+      if (RES) y[v].clear();
+      if (c < d && t < T) {
+        x[v].load(X, t * d + c);
+        if (RES) y[v].load(res, t * d + c);
+      }
+    }
+  };
+  long long t = (long long)blockIdx.x * G::AT_ONCE + sub;
+  fetch(t);
+  for (long long t0 = (long long)blockIdx.x * G::AT_ONCE; t0 < T; t0 += step, t += step) {
+    const bool in = t < T;
+    float r[NV][8], s = 0.f;
+    Eight<BF16> kept;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * LANES + l) * 8;
+      x[v].unpack(r[v]);
+      if (RES) {
+        float z[8];
+        y[v].unpack(z);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[v][i] += z[i];
+        kept.pack(r[v]);
+        kept.unpack(r[v]);
+        if (c < d && in) kept.store(R, t * d + c);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += r[v][i];
+    }
+    fetch(t + step);
+    const float mean = center ? row_sum<LANES>(s, part, turn) / (float)d : 0.f;
+    float q = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if ((v * LANES + l) * 8 < d)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          r[v][i] -= mean;
+          q += r[v][i] * r[v][i];
+        }
+    }
+    const float rstd = 1.f / sqrtf(row_sum<LANES>(q, part, turn) / (float)d + eps);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * LANES + l) * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[v][i] = r[v][i] * rstd * ww[v][i] + bb[v][i];
+      kept.pack(r[v]);
+      if (c < d && in) kept.store(Y, t * d + c);
+    }
+    if (l == 0 && in) {
+      if (mean_out) mean_out[t] = mean;
+      if (rstd_out) rstd_out[t] = rstd;
+    }
+  }
+}
+
 template <bool BF16>
-__global__ __launch_bounds__(NORM_THREADS) void norm_bwd_kernel(const void* dY, const void* R, const float* __restrict__ mean_in,
+__global__ __launch_bounds__(WIDE_THREADS) void norm_bwd_wide_kernel(const void* dY, const void* R, const float* __restrict__ mean_in,
                                                                 const float* __restrict__ rstd_in, const float* __restrict__ w, const void* dR,
                                                                 void* dX, int d, int center) {
-  __shared__ float part[NORM_THREADS / 64];
+  __shared__ float part[WIDE_THREADS / 64];
   const long long row = (long long)blockIdx.x * d;
   const float mean = center ? mean_in[blockIdx.x] : 0.f, rstd = rstd_in[blockIdx.x];
   float level = 0.f, along = 0.f;
-  for (int c = threadIdx.x * 8; c < d; c += NORM_THREADS * 8) {
+  for (int c = threadIdx.x * 8; c < d; c += WIDE_THREADS * 8) {
     float g[8], x[8];
     load8<BF16>(dY, row + c, g);
     load8<BF16>(R, row + c, x);
@@ -130,7 +296,7 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_bwd_kernel(const void* dY, 
   }
   level = center ? block_sum(level, part) / (float)d : 0.f;
   along = block_sum(along, part) / (float)d;
-  for (int c = threadIdx.x * 8; c < d; c += NORM_THREADS * 8) {
+  for (int c = threadIdx.x * 8; c < d; c += WIDE_THREADS * 8) {
     float g[8], x[8], r[8] = {};
     load8<BF16>(dY, row + c, g);
     load8<BF16>(R, row + c, x);
@@ -142,12 +308,12 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_bwd_kernel(const void* dY, 
   }
 }
 
-// Sums over a chunk of rows; a thread has 8 columns.
+// Wide rows' sums over a chunk of rows; a thread has 8 columns.
 template <bool BF16>
-__global__ __launch_bounds__(NORM_THREADS) void norm_columns_kernel(const void* dY, const void* R, const float* __restrict__ mean_in,
+__global__ __launch_bounds__(256) void norm_columns_kernel(const void* dY, const void* R, const float* __restrict__ mean_in,
                                                                     const float* __restrict__ rstd_in, float* __restrict__ part, int T, int d,
                                                                     int center, int chunk, int want_w, int want_b) {
-  const int c = (blockIdx.x * NORM_THREADS + threadIdx.x) * 8;
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
   if (c >= d) return;
   const int t0 = blockIdx.y * chunk, t1 = min(T, t0 + chunk);
   float sw[8] = {}, sb[8] = {};
@@ -170,21 +336,184 @@ __global__ __launch_bounds__(NORM_THREADS) void norm_columns_kernel(const void* 
   }
 }
 
-__global__ __launch_bounds__(NORM_THREADS) void norm_sum_kernel(const float* __restrict__ part, float* __restrict__ dw, float* __restrict__ db,
-                                                                int chunks, int d) {
-  const int c = blockIdx.x * NORM_THREADS + threadIdx.x;
-  if (c >= d) return;
-  float sw = 0.f, sb = 0.f;
-  for (int k = 0; k < chunks; ++k) {
-    if (dw) sw += part[(long long)k * 2 * d + c];
-    if (db) sb += part[(long long)k * 2 * d + d + c];
+// Gradient of the rows and the workgroup's sums for dw and db in one pass, a thread having the same columns of every row.  At any time the workgroups
+// are at neighbouring rows.
+template <bool BF16, int LANES, int NV, bool RES>
+__global__ __launch_bounds__(Rows<LANES>::THREADS) void norm_bwd_kernel(const void* dY, const void* R, const float* __restrict__ mean_in,
+                                                                            const float* __restrict__ rstd_in, const float* __restrict__ w, const void* dR,
+                                                                            void* dX, float* __restrict__ part_out, int T, int d, int center,
+                                                                            int want_w, int want_b) {
+  using G = Rows<LANES>;
+  __shared__ float part[4][16];
+  const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float ww[NV][8], sw[NV][8] = {}, sb[NV][8] = {};
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    load_weights(w, (v * LANES + l) * 8, d, 1.f, ww[v]);
   }
-  if (dw) dw[c] = sw;
-  if (db) db[c] = sb;
+  const int step = gridDim.x * G::AT_ONCE;
+  Eight<BF16> g[NV], x[NV], y[NV];
+  float mean = 0.f, rstd = 0.f;
+  auto fetch = [&](long long t) {
+    const bool in = t < T;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * LANES + l) * 8;
+      g[v].clear();
+      x[v].clear();
+      if (RES) y[v].clear();
+      if (c < d && in) {
+        g[v].load(dY, t * d + c);
+        x[v].load(R, t * d + c);
+        if (RES) y[v].load(dR, t * d + c);
+      }
+    }
+    mean = in && center ? mean_in[t] : 0.f;
+    rstd = in ? rstd_in[t] : 0.f;
+  };
+  long long t = (long long)blockIdx.x * G::AT_ONCE + sub;
+  fetch(t);
+  int turn = 0;
+  for (long long t0 = (long long)blockIdx.x * G::AT_ONCE; t0 < T; t0 += step, t += step) {
+    const bool in = t < T;
+    float gg[NV][8], xh[NV][8], rr[NV][8];
+    const float scale = rstd;
+    float level = 0.f, along = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      g[v].unpack(gg[v]);
+      x[v].unpack(xh[v]);
+      if (RES) y[v].unpack(rr[v]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        xh[v][i] = in && (v * LANES + l) * 8 < d ? (xh[v][i] - mean) * scale : 0.f;   // no row: nothing that could be NaN
+        sw[v][i] += gg[v][i] * xh[v][i];
+        sb[v][i] += gg[v][i];
+        gg[v][i] *= ww[v][i];
+        level += gg[v][i];
+        along += gg[v][i] * xh[v][i];
+      }
+    }
+    fetch(t + step);
+    // both sums over the row in one exchange
+    level = lanes_sum<(LANES < 64 ? LANES : 64)>(level);
+    along = lanes_sum<(LANES < 64 ? LANES : 64)>(along);
+    if constexpr (LANES > 64) {
+      if (lane == 0) {
+        part[turn][wave] = level;
+        part[turn + 1][wave] = along;
+      }
+      __syncthreads();
+      level = along = 0.f;
+#pragma unroll
+      for (int k = 0; k < LANES / 64; ++k) {
+        level += part[turn][sub * (LANES / 64) + k];
+        along += part[turn + 1][sub * (LANES / 64) + k];
+      }
+      turn ^= 2;
+    }
+    level = center ? level / (float)d : 0.f;
+    along /= (float)d;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * LANES + l) * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) gg[v][i] = (gg[v][i] - level - xh[v][i] * along) * scale + (RES ? rr[v][i] : 0.f);
+      Eight<BF16> out;
+      out.pack(gg[v]);
+      if (c < d && in) out.store(dX, t * d + c);
+    }
+  }
+  if (!want_w && !want_b) return;
+  // the sums of the rows that the workgroup had at once: of a wavefront by exchange, of its wavefronts one after the other by the first
+  float* const to = part_out + (long long)blockIdx.x * 2 * d;
+  if constexpr (LANES < 64) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int m = LANES; m < 64; m <<= 1)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          sw[v][i] += __shfl_xor(sw[v][i], m, 64);
+          sb[v][i] += __shfl_xor(sb[v][i], m, 64);
+        }
+  }
+  if constexpr (G::GROUPS > 1) {
+    __shared__ float4 turned[G::GROUPS - 1][NV * 4][LANES];
+    const int group = LANES <= 64 ? wave : sub;
+    const bool first = LANES >= 64 || lane < LANES;   // one lane of those that have the same sums
+    if (group && first)
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          turned[group - 1][4 * v + h][l] = make_float4(sw[v][4 * h], sw[v][4 * h + 1], sw[v][4 * h + 2], sw[v][4 * h + 3]);
+          turned[group - 1][4 * v + 2 + h][l] = make_float4(sb[v][4 * h], sb[v][4 * h + 1], sb[v][4 * h + 2], sb[v][4 * h + 3]);
+        }
+    __syncthreads();
+    if (group || !first) return;
+#pragma unroll
+    for (int q = 0; q < G::GROUPS - 1; ++q)
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float4 x = turned[q][4 * v + h][l], y = turned[q][4 * v + 2 + h][l];
+          sw[v][4 * h] += x.x; sw[v][4 * h + 1] += x.y; sw[v][4 * h + 2] += x.z; sw[v][4 * h + 3] += x.w;
+          sb[v][4 * h] += y.x; sb[v][4 * h + 1] += y.y; sb[v][4 * h + 2] += y.z; sb[v][4 * h + 3] += y.w;
+        }
+  }
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = (v * LANES + l) * 8;
+    if (c < d)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (want_w) to[c + i] = sw[v][i];
+        if (want_b) to[d + c + i] = sb[v][i];
+      }
+  }
 }
 
-// Rows per partial sum: what T and d decide.
-static int norm_chunk(const symi_cfg* c) { return std::max(1, cdiv(c->T, NORM_CHUNKS)); }
+// Column sums of the partial sums: wavefront w of 16 takes every 16th chunk of 64 columns, and the wavefronts are added in order.
+constexpr int SUM_WAVES = 16;
+__global__ __launch_bounds__(SUM_WAVES * 64) void norm_sum_kernel(const float* __restrict__ part, float* __restrict__ dw, float* __restrict__ db,
+                                                                  int chunks, int d) {
+  __shared__ float s[SUM_WAVES][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c = blockIdx.x * 64 + lane;
+  float* const to = blockIdx.y ? db : dw;
+  if (!to) return;
+  const float* const from = part + (long long)blockIdx.y * d + c;
+  float x = 0.f;
+  if (c < d)
+#pragma unroll 8
+    for (int k = wave; k < chunks; k += SUM_WAVES) x += from[(long long)k * 2 * d];
+  s[wave][lane] = x;
+  __syncthreads();
+  if (wave == 0 && c < d) {
+    x = 0.f;
+#pragma unroll
+    for (int w = 0; w < SUM_WAVES; ++w) x += s[w][lane];
+    to[c] = x;
+  }
+}
+
+// Threads of a row and pieces of 8 values each: one piece where that is a whole number of wavefronts.
+static void norm_shape(int d, int& lanes, int& nv) {
+  const int pieces = d / 8;
+  lanes = pieces <= 32 ? 16 : pieces <= 128 ? 64 : pieces <= 256 ? 128 : pieces <= 1024 ? 512 : 1024;
+  nv = pieces <= lanes ? 1 : 2;
+}
+static int rows_at_once(int lanes) { return lanes >= 256 ? 1 : 256 / lanes; }
+
+// Partial sums for dw and db, which is workgroups: what T and d decide.
+static int norm_parts(const symi_cfg* c) {
+  if (c->d > NORM_BWD_IN_REGS) return std::min(c->T, NORM_PARTS);
+  int lanes, nv;
+  norm_shape(c->d, lanes, nv);
+  return std::min(cdiv(c->T, rows_at_once(lanes)), NORM_PARTS);
+}
 
 }  // namespace symi
 
@@ -192,7 +521,7 @@ using namespace symi;
 
 extern "C" size_t symi_norm_workspace_bytes(const symi_cfg* cfg) {
   if (check_cfg(cfg, "symi_norm_workspace_bytes") != SYMI_OK) return 0;
-  return align_up((size_t)cdiv(cfg->T, norm_chunk(cfg)) * 2 * cfg->d * sizeof(float), 256) + 256;
+  return align_up((size_t)norm_parts(cfg) * 2 * cfg->d * sizeof(float), 256) + 256;
 }
 
 extern "C" int symi_norm_fwd(const symi_ctx* ctx, int center, float eps, const void* X, const void* residual, const float* w,
@@ -204,10 +533,36 @@ extern "C" int symi_norm_fwd(const symi_ctx* ctx, int center, float eps, const v
   if (cfg->T == 0) return SYMI_OK;
   SYMI_REQUIRE(X && Y, "symi_norm_fwd", "NULL pointer");
   hipStream_t st = as_stream(stream);
-  if (cfg->dtype == SYMI_BF16)
-    SYMI_TIMED(ctx, K_NORM, st, (norm_kernel<true><<<cfg->T, NORM_THREADS, 0, st>>>(X, residual, w, b, R, Y, mean, rstd, cfg->d, center, eps)));
-  else
-    SYMI_TIMED(ctx, K_NORM, st, (norm_kernel<false><<<cfg->T, NORM_THREADS, 0, st>>>(X, residual, w, b, R, Y, mean, rstd, cfg->d, center, eps)));
+  const int T = cfg->T, d = cfg->d;
+  const bool bf16 = cfg->dtype == SYMI_BF16;
+  if (d > NORM_IN_REGS) {
+    if (bf16) SYMI_TIMED(ctx, K_NORM, st, (norm_wide_kernel<true><<<T, WIDE_THREADS, 0, st>>>(X, residual, w, b, R, Y, mean, rstd, d, center, eps)));
+    else SYMI_TIMED(ctx, K_NORM, st, (norm_wide_kernel<false><<<T, WIDE_THREADS, 0, st>>>(X, residual, w, b, R, Y, mean, rstd, d, center, eps)));
+  } else {
+    int lanes, nv;
+    norm_shape(d, lanes, nv);
+    const int flying = std::max(lanes, 256) * nv * (bf16 ? 16 : 32) * (residual ? 2 : 1);   // bytes that a workgroup has on their way
+    const int grid = std::min(cdiv(T, rows_at_once(lanes)), ctx->cus * std::max(1, NORM_FLYING / flying));
+#define NORM_CASE(LL, NN)                                                                                                              \
+  case LL * 8 + NN:                                                                                                                    \
+    if (bf16 && residual)                                                                                                              \
+      SYMI_TIMED(ctx, K_NORM, st, (norm_kernel<true, LL, NN, true><<<grid, Rows<LL>::THREADS, 0, st>>>(X, residual, w, b, R, Y, mean, rstd, T, d, center, eps)));   \
+    else if (bf16)                                                                                                                     \
+      SYMI_TIMED(ctx, K_NORM, st, (norm_kernel<true, LL, NN, false><<<grid, Rows<LL>::THREADS, 0, st>>>(X, residual, w, b, R, Y, mean, rstd, T, d, center, eps)));  \
+    else if (residual)                                                                                                                 \
+      SYMI_TIMED(ctx, K_NORM, st, (norm_kernel<false, LL, NN, true><<<grid, Rows<LL>::THREADS, 0, st>>>(X, residual, w, b, R, Y, mean, rstd, T, d, center, eps)));  \
+    else                                                                                                                               \
+      SYMI_TIMED(ctx, K_NORM, st, (norm_kernel<false, LL, NN, false><<<grid, Rows<LL>::THREADS, 0, st>>>(X, residual, w, b, R, Y, mean, rstd, T, d, center, eps))); \
+    break;
+#define NORM_CASES NORM_CASE(16, 1) NORM_CASE(16, 2) NORM_CASE(64, 1) NORM_CASE(64, 2) NORM_CASE(128, 2) NORM_CASE(512, 1) NORM_CASE(512, 2)
+    switch (lanes * 8 + nv) {
+      NORM_CASES NORM_CASE(1024, 2)
+      default:
+        set_error("symi_norm_fwd: no kernel for %d threads x %d pieces a row", lanes, nv);
+        return SYMI_EUNSUPPORTED;
+    }
+#undef NORM_CASE
+  }
   SYMI_LAUNCH_CHECK("symi_norm_fwd");
   return SYMI_OK;
 }
@@ -221,22 +576,43 @@ extern "C" int symi_norm_bwd(const symi_ctx* ctx, int center, const void* dY, co
   SYMI_REQUIRE(ws || !(dw || db), "symi_norm_bwd", "NULL workspace");
   hipStream_t st = as_stream(stream);
   float* const part = reinterpret_cast<float*>(align_up((size_t)ws, 256));
-  const int chunk = norm_chunk(cfg), chunks = cdiv(T, chunk);
+  const int parts = norm_parts(cfg);
   const bool bf16 = cfg->dtype == SYMI_BF16;
-  if (T > 0 && (dw || db)) {
-    const dim3 grid(cdiv(d, NORM_THREADS * 8), chunks);
-    if (bf16)
-      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_columns_kernel<true><<<grid, NORM_THREADS, 0, st>>>(dY, R, mean, rstd, part, T, d, center, chunk, dw != nullptr, db != nullptr)));
-    else
-      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_columns_kernel<false><<<grid, NORM_THREADS, 0, st>>>(dY, R, mean, rstd, part, T, d, center, chunk, dw != nullptr, db != nullptr)));
+  const int want_w = dw != nullptr, want_b = db != nullptr;
+  if (T > 0 && d > NORM_BWD_IN_REGS) {
+    const dim3 grid(cdiv(d, 256 * 8), parts);
+    if (bf16) {
+      if (want_w || want_b)
+        SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_columns_kernel<true><<<grid, 256, 0, st>>>(dY, R, mean, rstd, part, T, d, center, cdiv(T, parts), want_w, want_b)));
+      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_wide_kernel<true><<<T, WIDE_THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, d, center)));
+    } else {
+      if (want_w || want_b)
+        SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_columns_kernel<false><<<grid, 256, 0, st>>>(dY, R, mean, rstd, part, T, d, center, cdiv(T, parts), want_w, want_b)));
+      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_wide_kernel<false><<<T, WIDE_THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, d, center)));
+    }
+  } else if (T > 0) {
+    int lanes, nv;
+    norm_shape(d, lanes, nv);
+#define NORM_CASE(LL, NN)                                                                                                              \
+  case LL * 8 + NN:                                                                                                                    \
+    if (bf16 && dR)                                                                                                                    \
+      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_kernel<true, LL, NN, true><<<parts, Rows<LL>::THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, part, T, d, center, want_w, want_b)));   \
+    else if (bf16)                                                                                                                     \
+      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_kernel<true, LL, NN, false><<<parts, Rows<LL>::THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, part, T, d, center, want_w, want_b)));  \
+    else if (dR)                                                                                                                       \
+      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_kernel<false, LL, NN, true><<<parts, Rows<LL>::THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, part, T, d, center, want_w, want_b)));  \
+    else                                                                                                                               \
+      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_kernel<false, LL, NN, false><<<parts, Rows<LL>::THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, part, T, d, center, want_w, want_b))); \
+    break;
+    switch (lanes * 8 + nv) {
+      NORM_CASES
+      default:
+        set_error("symi_norm_bwd: no kernel for %d threads x %d pieces a row", lanes, nv);
+        return SYMI_EUNSUPPORTED;
+    }
+#undef NORM_CASE
   }
-  if (T > 0) {
-    if (bf16)
-      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_kernel<true><<<T, NORM_THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, d, center)));
-    else
-      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_kernel<false><<<T, NORM_THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, d, center)));
-  }
-  if (dw || db) SYMI_TIMED(ctx, K_NORM_SUM, st, (norm_sum_kernel<<<cdiv(d, NORM_THREADS), NORM_THREADS, 0, st>>>(part, dw, db, chunks, d)));
+  if (dw || db) SYMI_TIMED(ctx, K_NORM_SUM, st, (norm_sum_kernel<<<dim3(cdiv(d, 64), 2), SUM_WAVES * 64, 0, st>>>(part, dw, db, parts, d)));
   SYMI_LAUNCH_CHECK("symi_norm_bwd");
   return SYMI_OK;
 }
