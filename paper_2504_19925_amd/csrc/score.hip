@@ -1,7 +1,13 @@
 // symi_route_scored / symi_route_scored_bwd / symi_route_bias: routing by softmax or sigmoid scores, with a bias and groups.
 //
-// A wavefront has a token; lane l holds the classes l, l + 64, ...  What classes are compared by is binary64, so that the choice is that of
-// the formula also where scores are a rounding apart.
+// The choice is that of binary64, but hardly any token needs it: a token is chosen for in fp32, with the runner-up of the last choice, and where two
+// neighbours in that order, or two groups, are nearer than twice what fp32 can be off (nearest), or classes are missing, its wavefront goes
+// through it again in binary64 (choose_exactly).  Of 65536 tokens with 128 classes that is one in some thousand.  Without a bias classes are compared by their
+// logits, exactly.
+//
+// G lanes hold a token's classes, up to 32 each in pieces of 4: piece p = v G + g lies in lane g, so that loads are whole lines, and the k rounds of
+// largest, runner-up, ... scan few lanes' registers, with a butterfly of log2 G steps in DPP operands.  Sums of exponentials are taken along a tree over the
+// pieces, the same for every G, so that a token's gates do not depend on its batch.
 #include <limits.h>
 #include <math.h>
 
@@ -11,8 +17,10 @@
 
 namespace symi {
 
-constexpr int SCORE_WAVES = 4;
+constexpr int SCORE_WAVES = 4, SCORE_MOST = 8;   // wavefronts of a workgroup: as a rule, where it holds the whole batch
 constexpr int SCORE_MAX_K = 16;
+constexpr float LOG2E = 1.44269504f;
+constexpr float U32 = 5.9604645e-8f;    // 2^-24
 
 // 1 / (1 + exp(-z)), with its digits also where exp(-z) is infinite
 __device__ __forceinline__ float sigmoid_of(float z) {
@@ -27,7 +35,45 @@ struct ScoreArgs {
   int32_t* hist;
   int T, E, k, renorm, sigmoid, groups, per, top_groups, group_top;   // per: classes of a group
   float scale;
+  int alone;   // one workgroup holds the whole batch and stores its counts
 };
+
+// What a wavefront has in LDS besides the workgroup's counts and groups of classes.
+struct ScoreLds {
+  float* of;            // [tokens][E]: what groups are compared by; in choose_exactly [E] doubles
+  float* group;         // [tokens][groups]
+  int* chosen;          // [tokens][k]; ~class: it only fills up
+  unsigned* kept;       // [tokens][2]: bits of the groups that stay
+  float2* softmax;      // [tokens]: largest logit, sum
+  unsigned* flags;      // [tokens]: 1: to be looked at exactly, 2: not a number
+};
+constexpr unsigned NEAR = 1, NOT_A_NUMBER = 2;
+__host__ __device__ inline int score_lds_of(int E, int tokens) { return ((tokens > 2 ? tokens * 4 : 8) * E + 15) / 16 * 16; }
+__host__ __device__ inline int score_lds_bytes(int E, int k, int groups, int tokens) {   // a multiple of 16
+  return score_lds_of(E, tokens) + (tokens * (20 + 4 * groups + 4 * k) + 15) / 16 * 16;
+}
+__device__ __forceinline__ ScoreLds score_lds(char* p, int E, int k, int groups, int tokens) {
+  ScoreLds L;
+  L.of = reinterpret_cast<float*>(p);
+  p += score_lds_of(E, tokens);
+  L.kept = reinterpret_cast<unsigned*>(p);
+  p += tokens * 8;
+  L.softmax = reinterpret_cast<float2*>(p);
+  p += tokens * 8;
+  L.flags = reinterpret_cast<unsigned*>(p);
+  p += tokens * 4;
+  L.group = reinterpret_cast<float*>(p);
+  p += tokens * groups * 4;
+  L.chosen = reinterpret_cast<int*>(p);
+  return L;
+}
+
+// Orders a wavefront's own LDS operations, which the hardware carries out as they come.
+__device__ __forceinline__ void wave_sync() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("" ::: "memory");
+}
 
 __device__ __forceinline__ double wave_max(double x) {
 #pragma unroll
@@ -40,119 +86,342 @@ __device__ __forceinline__ double wave_sum(double x) {
   return x;
 }
 
-template <int NV>
-__global__ __launch_bounds__(SCORE_WAVES * 64) void score_kernel(ScoreArgs a) {
-  extern __shared__ char smem[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int32_t* const hist = reinterpret_cast<int32_t*>(smem);
-  double* const by_s = reinterpret_cast<double*>(smem + (a.E * sizeof(int32_t) + 15) / 16 * 16) + wave * a.E;   // groups only
-  for (int e = threadIdx.x; e < a.E; e += SCORE_WAVES * 64) hist[e] = 0;
-  __syncthreads();
-  for (long long t = (long long)blockIdx.x * SCORE_WAVES + wave; t < a.T; t += (long long)gridDim.x * SCORE_WAVES) {
-    float z[NV];
-    double by[NV], of[NV];   // what classes and groups are compared by; -inf: not to be chosen
-    bool nan = false;
-    double top = -INFINITY;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int e = v * 64 + lane;
-      z[v] = e < a.E ? a.logits[t * a.E + e] : -INFINITY;
-      nan |= z[v] != z[v] || (!a.sigmoid && z[v] == INFINITY);
-      top = fmax(top, (double)z[v]);
-    }
-    nan = __ballot(nan) != 0;
-    double sum = 0.;
-    if (!a.sigmoid) {
-      top = wave_max(top);
-#pragma unroll
-      for (int v = 0; v < NV; ++v) sum += z[v] > -INFINITY ? exp((double)z[v] - top) : 0.;
-      sum = wave_sum(sum);
-    }
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int e = v * 64 + lane;
-      const double s = a.sigmoid ? 1. / (1. + exp(-(double)z[v])) : exp((double)z[v] - top) / sum;
-      by[v] = a.bias ? s + (double)(e < a.E ? a.bias[e] : 0.f) : (double)z[v];
-      of[v] = !a.bias && a.group_top > 1 ? s : by[v];
-      if (!(z[v] > -INFINITY) || !(by[v] > -INFINITY)) by[v] = of[v] = -INFINITY;
-    }
-    if (a.groups > 1) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v)
-        if (v * 64 + lane < a.E) by_s[v * 64 + lane] = of[v];
-      __builtin_amdgcn_wave_barrier();
-      double best = -INFINITY, second = -INFINITY;
-      if (lane < a.groups)
-        for (int i = 0; i < a.per; ++i) {
-          const double x = by_s[lane * a.per + i];
-          if (x > best) { second = best; best = x; } else if (x > second) second = x;
+// The choice for one token by a whole wavefront, in binary64: lane l looks at the classes l, l + 64, ...
+__device__ __noinline__ void choose_exactly(const ScoreArgs& a, const float* __restrict__ row, double* by, int* chosen) {
+  const int lane = threadIdx.x & 63;
+  double top = -INFINITY, sum = 0.;
+  if (!a.sigmoid && (a.bias || a.group_top > 1)) {
+    for (int e = lane; e < a.E; e += 64) top = fmax(top, (double)row[e]);
+    top = wave_max(top);
+    for (int e = lane; e < a.E; e += 64) sum += row[e] > -INFINITY ? exp((double)row[e] - top) : 0.;
+    sum = wave_sum(sum);
+  }
+  auto score = [&](float z) { return a.sigmoid ? 1. / (1. + exp(-(double)z)) : exp((double)z - top) / sum; };
+  // what classes are compared by; -inf: not to be chosen
+  auto value = [&](int e, float z, bool of_group) {
+    const double c = a.bias ? score(z) + (double)a.bias[e] : (double)z;
+    if (!(z > -INFINITY) || !(c > -INFINITY)) return -(double)INFINITY;
+    return of_group && !a.bias && a.group_top > 1 ? score(z) : c;
+  };
+  unsigned long long kept = ~0ull;
+  if (a.groups > 1) {
+    for (int e = lane; e < a.E; e += 64) by[e] = value(e, row[e], true);
+    wave_sync();
+    double best = -INFINITY, second = -INFINITY;
+    if (lane < a.groups)
+      for (int i = 0; i < a.per; ++i) {
+        const double x = by[lane * a.per + i];
+        if (x > best) {
+          second = best;
+          best = x;
+        } else if (x > second) {
+          second = x;
         }
-      const double mine = a.group_top > 1 && second > -INFINITY ? best + second : best;
-      int rank = 0;
-      for (int g = 0; g < a.groups; ++g) {
-        const double x = __shfl(mine, g, 64);
-        rank += x > mine || (x == mine && g < lane);
       }
-      const unsigned long long kept = __ballot(lane < a.groups && rank < a.top_groups);
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int e = v * 64 + lane;
-        if (e < a.E && !(kept >> (e / a.per) & 1)) by[v] = -INFINITY;
+    const double mine = a.group_top > 1 && second > -INFINITY ? best + second : best;
+    int rank = 0;
+    for (int g = 0; g < a.groups; ++g) {
+      const double x = __shfl(mine, g, 64);
+      rank += x > mine || (x == mine && g < lane);
+    }
+    kept = __ballot(lane < a.groups && rank < a.top_groups);
+    wave_sync();
+  }
+  for (int e = lane; e < a.E; e += 64) {
+    const double x = value(e, row[e], false);
+    by[e] = kept >> (a.groups > 1 ? e / a.per : 0) & 1 ? x : -INFINITY;
+  }
+  wave_sync();
+  unsigned taken = 0;
+  for (int j = 0; j < a.k; ++j) {
+    double b = -INFINITY;
+    int at = INT_MAX;
+    for (int v = 0, e = lane; e < a.E; ++v, e += 64)
+      if (!(taken >> v & 1) && (by[e] > b || at == INT_MAX)) {
+        b = by[e];
+        at = e;
       }
-      __builtin_amdgcn_wave_barrier();
-    }
-    unsigned taken = 0;
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-      if (v * 64 + lane >= a.E) taken |= 1u << v;
-    // lane j keeps the j-th choice
-    int my_idx = 0;
-    float my_z = -INFINITY;
-    bool real = false;
-    for (int j = 0; j < a.k; ++j) {
-      double b = -INFINITY;
-      int at = INT_MAX;
-      float zb = 0.f;
-#pragma unroll
-      for (int v = 0; v < NV; ++v)
-        if (!(taken >> v & 1) && (by[v] > b || at == INT_MAX)) { b = by[v]; at = v * 64 + lane; zb = z[v]; }
-#pragma unroll
-      for (int m = 32; m >= 1; m >>= 1) {
-        const double ob = __shfl_xor(b, m, 64);
-        const int oat = __shfl_xor(at, m, 64);
-        const float oz = __shfl_xor(zb, m, 64);
-        if (ob > b || (ob == b && oat < at)) { b = ob; at = oat; zb = oz; }
+    for (int m = 32; m >= 1; m >>= 1) {
+      const double ob = __shfl_xor(b, m, 64);
+      const int oat = __shfl_xor(at, m, 64);
+      if (ob > b || (ob == b && oat < at)) {
+        b = ob;
+        at = oat;
       }
-      if ((at & 63) == lane) taken |= 1u << (at >> 6);
-      if (j == lane) { my_idx = at; my_z = zb; real = b > -INFINITY; }
     }
-    // gates, relative to the largest of the k
-    float g;
-    if (a.renorm) {
-      const float part = a.sigmoid ? fminf(my_z, 0.f) : my_z;
-      float m = real ? part : -INFINITY;
+    if ((at & 63) == lane) taken |= 1u << (at >> 6);
+    if (lane == 0) chosen[j] = b > -INFINITY ? at : ~at;
+  }
+}
+
+// (value, class) of G lanes: the largest value, of equal ones the lowest class.
+template <int CTRL>
+__device__ __forceinline__ void better_of(float& b, int& at) {
+  const float ob = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(b), CTRL, 0xf, 0xf, false));
+  const int oat = __builtin_amdgcn_update_dpp(0, at, CTRL, 0xf, 0xf, false);
+  const bool other = ob > b || (ob == b && oat < at);
+  b = other ? ob : b;
+  at = other ? oat : at;
+}
+template <int G>
+__device__ __forceinline__ void best_of(float& b, int& at) {
 #pragma unroll
-      for (int o = 8; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-      g = real ? expf(part - m) : 0.f;
-      if (a.sigmoid && real) g /= 1.f + expf(-fabsf(my_z));
-      float s = g;
-#pragma unroll
-      for (int o = 8; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
-      g = real ? g / s : 0.f;
-    } else if (a.sigmoid) {
-      g = real ? sigmoid_of(my_z) : 0.f;
-    } else {
-      g = real ? expf(my_z - (float)top) / (float)sum : 0.f;
+  for (int m = 32; m >= 16; m >>= 1)
+    if (m < G) {
+      const float ob = __shfl_xor(b, m, 64);
+      const int oat = __shfl_xor(at, m, 64);
+      const bool other = ob > b || (ob == b && oat < at);
+      b = other ? ob : b;
+      at = other ? oat : at;
     }
-    if (lane < a.k) {
-      a.idx[t * a.k + lane] = my_idx;
-      a.gate[t * a.k + lane] = nan ? NAN : a.scale * g;
-      atomicAdd(&hist[my_idx], 1);
-    }
+  if constexpr (G >= 16) better_of<0x140>(b, at);   // row_mirror
+  if constexpr (G >= 8) better_of<0x141>(b, at);    // row_half_mirror
+  if constexpr (G >= 4) better_of<0x4e>(b, at);     // quad_perm 2, 3, 0, 1
+  if constexpr (G >= 2) better_of<0xb1>(b, at);     // quad_perm 1, 0, 3, 2
+}
+
+// How near two values compared in fp32 may be to each other for their order to be that of binary64.  In units of U32 a sigmoid is off by at most
+// 4 (an exponent of 2 |z| and 2, s (1 - s) |z| < 0.23, the sum and the reciprocal), a softmax by 45 (3 |x| + 2 of the exponential, |x| exp(-|x|) <
+// 0.37, and of the sum the mean of that, at most 3 ln E + 2, with 12 additions); adding the bias, of at most `bias`, rounds once more.  Twice that, and some.
+__device__ __forceinline__ float nearest(bool sigmoid, float bias) { return ((sigmoid ? 16.f : 128.f) + 4.f * (bias + 1.f)) * U32; }
+
+template <int G, int NV>
+__global__ __launch_bounds__(SCORE_MOST * 64) void score_kernel(ScoreArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  constexpr int TOKENS = 64 / G;        // of a wavefront
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int g = lane & (G - 1), sub = lane / G;
+  const int E = a.E, E4 = (E + 3) / 4 * 4;
+  int32_t* const hist = reinterpret_cast<int32_t*>(smem);
+  uint8_t* const group_of = reinterpret_cast<uint8_t*>(smem + E4 * 4);       // [E4]
+  char* const mine = smem + E4 * 4 + (E4 + 15) / 16 * 16 + (size_t)wave * score_lds_bytes(E, a.k, a.groups, TOKENS);
+  const ScoreLds L = score_lds(mine, E, a.k, a.groups, TOKENS);
+  const bool grouped = a.groups > 1 && a.top_groups < a.groups;
+  __shared__ int most_bias;
+  if (threadIdx.x == 0) most_bias = 0;
+  __syncthreads();
+  for (int e = threadIdx.x; e < E4; e += blockDim.x) {
+    hist[e] = 0;
+    if (grouped) group_of[e] = (uint8_t)min(e / a.per, a.groups - 1);
+    const int b = a.bias && e < E ? __float_as_int(a.bias[e]) & 0x7fffffff : 0;
+    if (b > 0 && b < 0x7f800000) atomicMax(&most_bias, b);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < a.E; e += SCORE_WAVES * 64)
-    if (hist[e]) atomicAdd(&a.hist[e], hist[e]);
+  const float closest = nearest(a.sigmoid, __int_as_float(most_bias));
+  const bool by_score = a.bias != nullptr, scored_groups = grouped && (by_score || a.group_top > 1);
+  const bool need_softmax = !a.sigmoid && (by_score || scored_groups || !a.renorm);
+
+  for (long long t0 = (long long)blockIdx.x * waves * TOKENS; t0 < a.T; t0 += (long long)gridDim.x * waves * TOKENS) {
+    const long long t = t0 + wave * TOKENS + sub;
+    const bool valid = t < a.T;
+    const float* const row = a.logits + (valid ? t : 0) * E;
+    float z[NV * 4];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * G + g) * 4;
+      if (valid && c + 3 < E) {
+        const f32x4_f32 q = *reinterpret_cast<const f32x4_f32*>(row + c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[4 * v + i] = q[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[4 * v + i] = valid && c + i < E ? row[c + i] : -INFINITY;
+      }
+    }
+    bool nan = false;
+    float top = -INFINITY, inv_sum = 0.f, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV * 4; ++i) {
+      nan |= z[i] != z[i];
+      top = fmaxf(top, z[i]);
+    }
+    if (!a.sigmoid) {
+#pragma unroll
+      for (int m = G >> 1; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
+      nan |= top == INFINITY;
+    }
+    if (need_softmax) {
+      float part[NV];
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        part[v] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[v] += z[4 * v + i] > -INFINITY ? __builtin_amdgcn_exp2f((z[4 * v + i] - top) * LOG2E) : 0.f;
+      }
+#pragma unroll
+      for (int h = NV / 2; h >= 1; h >>= 1)
+#pragma unroll
+        for (int v = 0; v < h; ++v) part[v] += part[v + h];
+      sum = part[0];
+#pragma unroll
+      for (int m = G >> 1; m >= 1; m >>= 1) sum += __shfl_xor(sum, m, 64);
+      inv_sum = 1.f / sum;
+    }
+    auto score = [&](float x) {
+      return a.sigmoid ? __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-x * LOG2E)) : __builtin_amdgcn_exp2f((x - top) * LOG2E) * inv_sum;
+    };
+    if (g == 0) {
+      L.flags[sub] = 0;
+      L.softmax[sub] = make_float2(top, sum);
+      L.kept[2 * sub] = L.kept[2 * sub + 1] = 0;
+    }
+    wave_sync();
+    if (nan) atomicOr(&L.flags[sub], NOT_A_NUMBER);
+
+    // what classes are compared by, in z's place; -inf: not to be chosen.  What groups are compared by goes to LDS.
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * G + g) * 4;
+      float of[4], bias[4] = {};
+      if (by_score) {
+        if (c + 3 < E) {
+          const f32x4_f32 q = *reinterpret_cast<const f32x4_f32*>(a.bias + c);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) bias[i] = q[i];
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) bias[i] = c + i < E ? a.bias[c + i] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = z[4 * v + i];
+        const bool live = x > -INFINITY;
+        float s = 0.f;
+        if (by_score || scored_groups) s = score(x);
+        float y = by_score ? s + bias[i] : x;
+        if (!live || !(y > -INFINITY)) y = -INFINITY;
+        of[i] = !by_score && scored_groups && live ? s : y;
+        z[4 * v + i] = y;
+      }
+      if (grouped && c < E) {
+        float* const to = L.of + sub * E + c;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (c + i < E) to[i] = of[i];
+      }
+    }
+    if (grouped) {
+      wave_sync();
+      const int pairs = TOKENS * a.groups;
+      for (int p = lane; p < pairs; p += 64) {
+        const int tok = p / a.groups, gr = p - tok * a.groups;
+        const float* const from = L.of + tok * E + gr * a.per;
+        float best = -INFINITY, second = -INFINITY;
+        int at = lane % a.per;              // every lane begins elsewhere: they would meet in the same banks
+        for (int i = 0; i < a.per; ++i) {
+          const float x = from[at];
+          second = fmaxf(second, fminf(best, x));
+          best = fmaxf(best, x);
+          at = at + 1 == a.per ? 0 : at + 1;
+        }
+        L.group[p] = a.group_top > 1 && second > -INFINITY ? best + second : best;
+      }
+      wave_sync();
+      for (int p = lane; p < pairs; p += 64) {
+        const int tok = p / a.groups, gr = p - tok * a.groups;
+        const float mine_ = L.group[p];
+        int rank = 0;
+        bool near = false;
+        for (int i = 0; i < a.groups; ++i) {
+          const float x = L.group[tok * a.groups + i];
+          rank += x > mine_ || (x == mine_ && i < gr);
+          near |= scored_groups && i != gr && mine_ > -INFINITY && !(fabsf(x - mine_) > 2.f * closest);
+        }
+        if (rank < a.top_groups) atomicOr(&L.kept[2 * tok + (gr >> 5)], 1u << (gr & 31));
+        if (near) atomicOr(&L.flags[tok], NEAR);
+      }
+      wave_sync();
+      const unsigned lo = L.kept[2 * sub], hi = L.kept[2 * sub + 1];
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int c = (v * G + g) * 4;
+        const unsigned ids = c < E ? *reinterpret_cast<const unsigned*>(group_of + c) : 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const unsigned id = ids >> (8 * i) & 0xff;
+          if (!((id & 32 ? hi : lo) >> (id & 31) & 1)) z[4 * v + i] = -INFINITY;
+        }
+      }
+    }
+
+    // the rounds; by score one more, for the distance to the first that is not chosen
+    unsigned taken = 0;
+    bool near = false;
+    float before = INFINITY;
+    const int rounds = a.k + (by_score && a.k < E ? 1 : 0);
+    for (int j = 0; j < rounds; ++j) {
+      float b = -INFINITY;
+      int bc = 0;
+#pragma unroll
+      for (int i = 0; i < NV * 4; ++i) {
+        const bool better = z[i] > b && !(taken >> i & 1u);
+        b = better ? z[i] : b;
+        bc = better ? i : bc;
+      }
+      const int own = b > -INFINITY ? ((bc >> 2) * G + g) * 4 + (bc & 3) : INT_MAX;
+      int at = own;
+      best_of<G>(b, at);
+      if (at == own) taken |= 1u << bc;
+      if (j < a.k) {
+        near |= at == INT_MAX;                      // somebody has to fill up
+        if (g == 0) L.chosen[sub * a.k + j] = at;
+      }
+      if (by_score && j > 0 && at != INT_MAX) near |= !(before - b > closest);
+      before = b;
+    }
+    if (near && g == 0) atomicOr(&L.flags[sub], NEAR);
+    wave_sync();
+    unsigned long long again = __ballot(g == 0 && valid && (L.flags[sub] & NEAR));
+    while (again) {
+      const int tok = (__ffsll((unsigned long long)again) - 1) / G;
+      again &= again - 1;
+      choose_exactly(a, a.logits + (t0 + wave * TOKENS + tok) * E, reinterpret_cast<double*>(L.of), L.chosen + tok * a.k);
+      wave_sync();
+    }
+
+    // gates relative to the largest of the k: 16 lanes a token
+    const int j = lane & 15;
+    for (int u = 0; u < TOKENS; u += 4) {
+      const int tok = u + (lane >> 4);
+      const long long tt = t0 + wave * TOKENS + tok;
+      const bool here = tok < TOKENS && tt < a.T && j < a.k;
+      const int c = here ? L.chosen[tok * a.k + j] : -1;
+      const bool real = c >= 0;
+      const float x = real ? a.logits[tt * E + c] : 0.f;
+      float gate;
+      if (a.renorm) {
+        const float low = a.sigmoid ? fminf(x, 0.f) : x;
+        float m = real ? low : -INFINITY;
+#pragma unroll
+        for (int o = 8; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+        gate = real ? expf(low - m) : 0.f;
+        if (a.sigmoid && real) gate /= 1.f + expf(-fabsf(x));
+        float s = gate;
+#pragma unroll
+        for (int o = 8; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
+        gate = real ? gate / s : 0.f;
+      } else if (a.sigmoid) {
+        gate = real ? sigmoid_of(x) : 0.f;
+      } else {
+        const float2 q = L.softmax[here ? tok : 0];
+        gate = real ? expf(x - q.x) / q.y : 0.f;
+      }
+      if (here) {
+        const int e = real ? c : ~c;
+        a.idx[tt * a.k + j] = e;
+        a.gate[tt * a.k + j] = L.flags[tok] & NOT_A_NUMBER ? NAN : a.scale * gate;
+        atomicAdd(&hist[e], 1);
+      }
+    }
+    wave_sync();
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < E; e += blockDim.x) {
+    if (a.alone) a.hist[e] = hist[e];
+    else if (hist[e]) atomicAdd(&a.hist[e], hist[e]);
+  }
 }
 
 struct ScoreBwdArgs {
@@ -164,48 +433,63 @@ struct ScoreBwdArgs {
   float scale;
 };
 
-// dz of the chosen: renormalised g (dg - sum g dg), sigmoid: times (1 - s); a plain softmax: p_e ([e chosen] dg - sum p dg) for every class.
+// dz of the chosen: renormalised g (dg - sum g dg), sigmoid: times (1 - s); a plain softmax: p_e ([e chosen] dg - sum p dg) for every class.  16 lanes a token:
+// they put what the k classes get into a row of zeros in LDS and write the row.
 __global__ __launch_bounds__(SCORE_WAVES * 64) void score_bwd_kernel(ScoreBwdArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (long long t = (long long)blockIdx.x * SCORE_WAVES + wave; t < a.T; t += (long long)gridDim.x * SCORE_WAVES) {
-    const float* const row = a.logits + t * a.E;
+  extern __shared__ __attribute__((aligned(16))) float rows[];
+  const int j = threadIdx.x & 15, sub = threadIdx.x >> 4;
+  constexpr int AT_ONCE = SCORE_WAVES * 4;
+  const int E = a.E, E4 = (E + 3) / 4 * 4;
+  float* const out = rows + sub * E4;
+  const bool dense = !a.sigmoid && !a.renorm;
+  for (long long t = (long long)blockIdx.x * AT_ONCE + sub; t < a.T; t += (long long)gridDim.x * AT_ONCE) {
+    const float* const row = a.logits + t * E;
     int at = -1;
     float g = 0.f, dg = 0.f, z = 0.f;
-    if (lane < a.k) {
-      at = a.idx[t * a.k + lane];
-      g = a.gate[t * a.k + lane] / a.scale;
-      dg = a.dgate[t * a.k + lane] * a.scale;
-      if (g == 0.f || (unsigned)at >= (unsigned)a.E) at = -1;   // only filled up
-      else z = row[at];
+    if (j < a.k) {
+      at = a.idx[t * a.k + j];
+      g = a.gate[t * a.k + j] / a.scale;
+      dg = a.dgate[t * a.k + j] * a.scale;
+      if (g == 0.f || (unsigned)at >= (unsigned)E) at = -1;   // only filled up
+      else if (a.sigmoid) z = row[at];
     }
+    for (int c = j * 4; c < E4; c += 64) *reinterpret_cast<float4*>(out + c) = make_float4(0.f, 0.f, 0.f, 0.f);
     if (at < 0) g = dg = 0.f;
     float dot = g * dg;
 #pragma unroll
     for (int o = 8; o >= 1; o >>= 1) dot += __shfl_xor(dot, o, 64);
-    dot = __shfl(dot, 0, 64);
     float dz = a.renorm ? g * (dg - dot) : g * dg;
     if (a.sigmoid) dz *= sigmoid_of(-z);
-    const bool dense = !a.sigmoid && !a.renorm;
     float top = -INFINITY, sum = 0.f;
     if (dense) {
-      for (int e = lane; e < a.E; e += 64) top = fmaxf(top, row[e]);
+      for (int e = j; e < E; e += 16) top = fmaxf(top, row[e]);
 #pragma unroll
-      for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-      for (int e = lane; e < a.E; e += 64) sum += row[e] > -INFINITY ? expf(row[e] - top) : row[e] == -INFINITY ? 0.f : NAN;
+      for (int o = 8; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+      for (int e = j; e < E; e += 16) sum += row[e] == -INFINITY ? 0.f : expf(row[e] - top);
 #pragma unroll
-      for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
+      for (int o = 8; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
     }
-    for (int e0 = 0; e0 < a.E; e0 += 64) {
-      const int e = e0 + lane;
-      float out = 0.f;
-      if (dense && e < a.E) out = row[e] > -INFINITY ? -expf(row[e] - top) / sum * dot : row[e] == -INFINITY ? 0.f : NAN;
-      for (int j = 0; j < a.k; ++j) {
-        const int c = __shfl(at, j, 64);
-        const float x = __shfl(dz, j, 64);
-        if (c == e) out += x;
+    wave_sync();
+    if (at >= 0) out[at] = dz;
+    wave_sync();
+    for (int c = j * 4; c < E; c += 64) {
+      const float4 q = *reinterpret_cast<const float4*>(out + c);
+      float x[4] = {q.x, q.y, q.z, q.w};
+      if (dense)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (c + i < E) x[i] -= row[c + i] == -INFINITY ? 0.f : expf(row[c + i] - top) / sum * dot;
+      float* const to = a.dlogits + t * E + c;
+      if (c + 3 < E) {
+        const f32x4_f32 y = {x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<f32x4_f32*>(to) = y;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (c + i < E) to[i] = x[i];
       }
-      if (e < a.E) a.dlogits[t * a.E + e] = out;
     }
+    wave_sync();
   }
 }
 
@@ -237,7 +521,16 @@ static int check_score(const symi_cfg* c, const symi_score* hp, const char* who)
   return SYMI_OK;
 }
 
-static int score_grid(int T) { return std::min(cdiv(T, SCORE_WAVES), 4096); }
+
+// Lanes of a token: few, with up to 32 classes each; a small batch is spread over more of them, so that the chip is filled.
+static void score_shape(int E, int T, int& G, int& NV) {
+  const int vecs = cdiv(E, 4);
+  G = 1;
+  while (G * 8 < vecs) G <<= 1;
+  while (G < vecs && G < 64 && (long long)T * G < 512LL * 256) G <<= 1;
+  const int need = cdiv(vecs, G);
+  NV = need <= 1 ? 1 : need <= 2 ? 2 : need <= 4 ? 4 : 8;
+}
 
 }  // namespace symi
 
@@ -249,17 +542,35 @@ extern "C" int symi_route_scored(const symi_ctx* ctx, const symi_score* hp, cons
   if (int rc = check_score(cfg, hp, "symi_route_scored")) return rc;
   SYMI_REQUIRE(hist && (cfg->T == 0 || (logits && idx && gate)), "symi_route_scored", "NULL pointer");
   hipStream_t st = as_stream(stream);
-  const int E = cfg->E;
-  launch_fill_i32(ctx, hist, E, 0, st);
-  if (cfg->T > 0) {
-    const ScoreArgs a = {logits, bias, idx, gate, hist, cfg->T, E, cfg->k, cfg->renorm, hp->score == SYMI_SIGMOID, hp->groups, E / hp->groups,
-                         hp->top_groups, hp->group_top, hp->scale};
-    const size_t sh = align_up(E * sizeof(int32_t), 16) + (hp->groups > 1 ? SCORE_WAVES * E * sizeof(double) : 0);
-    const int grid = score_grid(cfg->T), threads = SCORE_WAVES * 64;
-    if (E <= 64) SYMI_TIMED(ctx, K_SCORE, st, (score_kernel<1><<<grid, threads, sh, st>>>(a)));
-    else if (E <= 128) SYMI_TIMED(ctx, K_SCORE, st, (score_kernel<2><<<grid, threads, sh, st>>>(a)));
-    else if (E <= 256) SYMI_TIMED(ctx, K_SCORE, st, (score_kernel<4><<<grid, threads, sh, st>>>(a)));
-    else SYMI_TIMED(ctx, K_SCORE, st, (score_kernel<16><<<grid, threads, sh, st>>>(a)));
+  const int E = cfg->E, T = cfg->T, k = cfg->k;
+  int G, NV;
+  score_shape(E, T, G, NV);
+  const int per_wave = 64 / G;
+  const int E4 = cdiv(E, 4) * 4, of_all = E4 * 4 + cdiv(E4, 16) * 16, of_wave = score_lds_bytes(E, k, hp->groups, per_wave);
+  // a small batch: one workgroup, which needs no cleared counts
+  const bool alone = T > 0 && (long long)T * E * (k + 2) <= 32768 && T <= SCORE_MOST * per_wave && of_all + cdiv(T, per_wave) * of_wave <= 65536;
+  if (!alone) launch_fill_i32(ctx, hist, E, 0, st);
+  if (T > 0) {
+    const ScoreArgs a = {logits, bias, idx, gate, hist, T, E, k, cfg->renorm, hp->score == SYMI_SIGMOID, hp->groups, E / hp->groups,
+                         hp->top_groups, hp->group_top, hp->scale, alone};
+    int waves = alone ? cdiv(T, per_wave) : SCORE_WAVES;
+    while (waves > 1 && of_all + waves * of_wave > 65536) waves /= 2;
+    const size_t sh = of_all + waves * of_wave;
+    const int grid = alone ? 1 : std::min(cdiv(T, per_wave * waves), 16 / waves * ctx->cus);
+#define SYMI_SCORE_CASE(GG, NN)                                                                            \
+  case GG * 16 + NN:                                                                                       \
+    SYMI_TIMED(ctx, K_SCORE, st, (score_kernel<GG, NN><<<grid, waves * 64, sh, st>>>(a)));                 \
+    break;
+#define SYMI_SCORE_G(GG) SYMI_SCORE_CASE(GG, 1) SYMI_SCORE_CASE(GG, 2) SYMI_SCORE_CASE(GG, 4) SYMI_SCORE_CASE(GG, 8)
+    switch (G * 16 + NV) {
+      SYMI_SCORE_G(1) SYMI_SCORE_G(2) SYMI_SCORE_G(4) SYMI_SCORE_G(8) SYMI_SCORE_G(16) SYMI_SCORE_G(32)
+      SYMI_SCORE_CASE(64, 1) SYMI_SCORE_CASE(64, 2) SYMI_SCORE_CASE(64, 4)
+      default:
+        set_error("symi_route_scored: no kernel for %d lanes x %d pieces per token", G, NV);
+        return SYMI_EUNSUPPORTED;
+    }
+#undef SYMI_SCORE_G
+#undef SYMI_SCORE_CASE
   }
   SYMI_LAUNCH_CHECK("symi_route_scored");
   return SYMI_OK;
@@ -273,7 +584,9 @@ extern "C" int symi_route_scored_bwd(const symi_ctx* ctx, const symi_score* hp, 
   SYMI_REQUIRE(logits && idx && gate && dgate && dlogits, "symi_route_scored_bwd", "NULL pointer");
   hipStream_t st = as_stream(stream);
   const ScoreBwdArgs a = {logits, idx, gate, dgate, dlogits, cfg->T, cfg->E, cfg->k, cfg->renorm, hp->score == SYMI_SIGMOID, hp->scale};
-  SYMI_TIMED(ctx, K_SCORE_BWD, st, (score_bwd_kernel<<<score_grid(cfg->T), SCORE_WAVES * 64, 0, st>>>(a)));
+  const int grid = std::min(cdiv(cfg->T, SCORE_WAVES * 4), 8 * ctx->cus);
+  const size_t sh = (size_t)SCORE_WAVES * 4 * cdiv(cfg->E, 4) * 4 * sizeof(float);
+  SYMI_TIMED(ctx, K_SCORE_BWD, st, (score_bwd_kernel<<<grid, SCORE_WAVES * 64, sh, st>>>(a)));
   SYMI_LAUNCH_CHECK("symi_route_scored_bwd");
   return SYMI_OK;
 }
