@@ -17,8 +17,9 @@
 
 namespace symi {
 
-constexpr int SCORE_WAVES = 4, SCORE_MOST = 8;   // wavefronts of a workgroup: as a rule, where it holds the whole batch
-constexpr int SCORE_MAX_K = 16;
+constexpr int SCORE_MOST = 16;          // wavefronts of a workgroup at most
+constexpr int SCORE_LDS = 156 * 1024;   // of a workgroup at most
+constexpr int BWD_WAVES = 4;
 constexpr float LOG2E = 1.44269504f;
 constexpr float U32 = 5.9604645e-8f;    // 2^-24
 
@@ -86,8 +87,58 @@ __device__ __forceinline__ double wave_sum(double x) {
   return x;
 }
 
+// The word that the lane has to compare with in step STEP of a butterfly over 64 lanes: 0, 1: the other half, the other row of 16 lanes (the swap
+// gives a pair that is the same in both); 2 .. 5: mirrored in a row, in half of it, and in four.
+template <int STEP>
+__device__ __forceinline__ void partner(int x, int& one, int& other) {
+  if constexpr (STEP == 0) {
+    const auto r = __builtin_amdgcn_permlane32_swap((unsigned)x, (unsigned)x, false, false);
+    one = (int)r[0];
+    other = (int)r[1];
+  } else if constexpr (STEP == 1) {
+    const auto r = __builtin_amdgcn_permlane16_swap((unsigned)x, (unsigned)x, false, false);
+    one = (int)r[0];
+    other = (int)r[1];
+  } else {
+    constexpr int ctrl = STEP == 2 ? 0x140 : STEP == 3 ? 0x141 : STEP == 4 ? 0x4e : 0xb1;
+    one = x;
+    other = __builtin_amdgcn_update_dpp(0, x, ctrl, 0xf, 0xf, false);
+  }
+}
+template <int STEP>
+__device__ __forceinline__ void better_of(float& b, int& at) {
+  int x, y, i, j;
+  partner<STEP>(__float_as_int(b), x, y);
+  partner<STEP>(at, i, j);
+  const float p = __int_as_float(x), q = __int_as_float(y);
+  const bool second = q > p || (q == p && j < i);
+  b = second ? q : p;
+  at = second ? j : i;
+}
+template <int STEP>
+__device__ __forceinline__ void better_of(double& b, int& at) {
+  int xl, yl, xh, yh, i, j;
+  partner<STEP>(__double2loint(b), xl, yl);
+  partner<STEP>(__double2hiint(b), xh, yh);
+  partner<STEP>(at, i, j);
+  const double p = __hiloint2double(xh, xl), q = __hiloint2double(yh, yl);
+  const bool second = q > p || (q == p && j < i);
+  b = second ? q : p;
+  at = second ? j : i;
+}
+// (value, class) of G lanes: the largest value, of equal ones the lowest class.
+template <int G, class V>
+__device__ __forceinline__ void best_of(V& b, int& at) {
+  if constexpr (G >= 64) better_of<0>(b, at);
+  if constexpr (G >= 32) better_of<1>(b, at);
+  if constexpr (G >= 16) better_of<2>(b, at);
+  if constexpr (G >= 8) better_of<3>(b, at);
+  if constexpr (G >= 4) better_of<4>(b, at);
+  if constexpr (G >= 2) better_of<5>(b, at);
+}
+
 // The choice for one token by a whole wavefront, in binary64: lane l looks at the classes l, l + 64, ...
-__device__ __noinline__ void choose_exactly(const ScoreArgs& a, const float* __restrict__ row, double* by, int* chosen) {
+__device__ __forceinline__ void choose_exactly(const ScoreArgs& a, const float* __restrict__ row, double* by, int* chosen) {
   const int lane = threadIdx.x & 63;
   double top = -INFINITY, sum = 0.;
   if (!a.sigmoid && (a.bias || a.group_top > 1)) {
@@ -141,44 +192,10 @@ __device__ __noinline__ void choose_exactly(const ScoreArgs& a, const float* __r
         b = by[e];
         at = e;
       }
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) {
-      const double ob = __shfl_xor(b, m, 64);
-      const int oat = __shfl_xor(at, m, 64);
-      if (ob > b || (ob == b && oat < at)) {
-        b = ob;
-        at = oat;
-      }
-    }
+    best_of<64>(b, at);
     if ((at & 63) == lane) taken |= 1u << (at >> 6);
     if (lane == 0) chosen[j] = b > -INFINITY ? at : ~at;
   }
-}
-
-// (value, class) of G lanes: the largest value, of equal ones the lowest class.
-template <int CTRL>
-__device__ __forceinline__ void better_of(float& b, int& at) {
-  const float ob = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(b), CTRL, 0xf, 0xf, false));
-  const int oat = __builtin_amdgcn_update_dpp(0, at, CTRL, 0xf, 0xf, false);
-  const bool other = ob > b || (ob == b && oat < at);
-  b = other ? ob : b;
-  at = other ? oat : at;
-}
-template <int G>
-__device__ __forceinline__ void best_of(float& b, int& at) {
-#pragma unroll
-  for (int m = 32; m >= 16; m >>= 1)
-    if (m < G) {
-      const float ob = __shfl_xor(b, m, 64);
-      const int oat = __shfl_xor(at, m, 64);
-      const bool other = ob > b || (ob == b && oat < at);
-      b = other ? ob : b;
-      at = other ? oat : at;
-    }
-  if constexpr (G >= 16) better_of<0x140>(b, at);   // row_mirror
-  if constexpr (G >= 8) better_of<0x141>(b, at);    // row_half_mirror
-  if constexpr (G >= 4) better_of<0x4e>(b, at);     // quad_perm 2, 3, 0, 1
-  if constexpr (G >= 2) better_of<0xb1>(b, at);     // quad_perm 1, 0, 3, 2
 }
 
 // How near two values compared in fp32 may be to each other for their order to be that of binary64.  In units of U32 a sigmoid is off by at most
@@ -194,29 +211,17 @@ __global__ __launch_bounds__(SCORE_MOST * 64) void score_kernel(ScoreArgs a) {
   const int g = lane & (G - 1), sub = lane / G;
   const int E = a.E, E4 = (E + 3) / 4 * 4;
   int32_t* const hist = reinterpret_cast<int32_t*>(smem);
-  uint8_t* const group_of = reinterpret_cast<uint8_t*>(smem + E4 * 4);       // [E4]
-  char* const mine = smem + E4 * 4 + (E4 + 15) / 16 * 16 + (size_t)wave * score_lds_bytes(E, a.k, a.groups, TOKENS);
+  float* const bias_s = reinterpret_cast<float*>(smem + E4 * 4);             // [E4]
+  uint8_t* const group_of = reinterpret_cast<uint8_t*>(smem + E4 * 8);       // [E4]
+  char* const mine = smem + E4 * 8 + (E4 + 15) / 16 * 16 + (size_t)wave * score_lds_bytes(E, a.k, a.groups, TOKENS);
   const ScoreLds L = score_lds(mine, E, a.k, a.groups, TOKENS);
   const bool grouped = a.groups > 1 && a.top_groups < a.groups;
-  __shared__ int most_bias;
-  if (threadIdx.x == 0) most_bias = 0;
-  __syncthreads();
-  for (int e = threadIdx.x; e < E4; e += blockDim.x) {
-    hist[e] = 0;
-    if (grouped) group_of[e] = (uint8_t)min(e / a.per, a.groups - 1);
-    const int b = a.bias && e < E ? __float_as_int(a.bias[e]) & 0x7fffffff : 0;
-    if (b > 0 && b < 0x7f800000) atomicMax(&most_bias, b);
-  }
-  __syncthreads();
-  const float closest = nearest(a.sigmoid, __int_as_float(most_bias));
   const bool by_score = a.bias != nullptr, scored_groups = grouped && (by_score || a.group_top > 1);
   const bool need_softmax = !a.sigmoid && (by_score || scored_groups || !a.renorm);
-
-  for (long long t0 = (long long)blockIdx.x * waves * TOKENS; t0 < a.T; t0 += (long long)gridDim.x * waves * TOKENS) {
-    const long long t = t0 + wave * TOKENS + sub;
+  float z[NV * 4];
+  auto fetch = [&](long long t) {
     const bool valid = t < a.T;
     const float* const row = a.logits + (valid ? t : 0) * E;
-    float z[NV * 4];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = (v * G + g) * 4;
@@ -229,6 +234,27 @@ __global__ __launch_bounds__(SCORE_MOST * 64) void score_kernel(ScoreArgs a) {
         for (int i = 0; i < 4; ++i) z[4 * v + i] = valid && c + i < E ? row[c + i] : -INFINITY;
       }
     }
+  };
+  const long long first = (long long)blockIdx.x * waves * TOKENS + wave * TOKENS, step = (long long)gridDim.x * waves * TOKENS;
+  fetch(first + sub);
+  float largest = 0.f;      // |bias|
+  for (int e = threadIdx.x; e < E4; e += blockDim.x) {
+    hist[e] = 0;
+    if (grouped) group_of[e] = (uint8_t)min(e / a.per, a.groups - 1);
+    const float b = a.bias && e < E ? a.bias[e] : 0.f;
+    bias_s[e] = b;
+    if (fabsf(b) < INFINITY) largest = fmaxf(largest, fabsf(b));
+  }
+  __shared__ float largest_of[16];
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) largest = fmaxf(largest, __shfl_xor(largest, m, 64));
+  if (lane == 0) largest_of[wave] = largest;
+  __syncthreads();
+  for (int w = 0; w < waves; ++w) largest = fmaxf(largest, largest_of[w]);
+  const float closest = nearest(a.sigmoid, largest);
+
+  for (long long t0 = first; t0 < a.T; t0 += step, fetch(t0 + sub)) {
+    const bool valid = t0 + sub < a.T;
     bool nan = false;
     float top = -INFINITY, inv_sum = 0.f, sum = 0.f;
 #pragma unroll
@@ -275,14 +301,11 @@ __global__ __launch_bounds__(SCORE_MOST * 64) void score_kernel(ScoreArgs a) {
       const int c = (v * G + g) * 4;
       float of[4], bias[4] = {};
       if (by_score) {
-        if (c + 3 < E) {
-          const f32x4_f32 q = *reinterpret_cast<const f32x4_f32*>(a.bias + c);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) bias[i] = q[i];
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) bias[i] = c + i < E ? a.bias[c + i] : 0.f;
-        }
+        const float4 q = c < E ? *reinterpret_cast<const float4*>(bias_s + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+        bias[0] = q.x;
+        bias[1] = q.y;
+        bias[2] = q.z;
+        bias[3] = q.w;
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -377,7 +400,7 @@ __global__ __launch_bounds__(SCORE_MOST * 64) void score_kernel(ScoreArgs a) {
     while (again) {
       const int tok = (__ffsll((unsigned long long)again) - 1) / G;
       again &= again - 1;
-      choose_exactly(a, a.logits + (t0 + wave * TOKENS + tok) * E, reinterpret_cast<double*>(L.of), L.chosen + tok * a.k);
+      choose_exactly(a, a.logits + (t0 + tok) * E, reinterpret_cast<double*>(L.of), L.chosen + tok * a.k);
       wave_sync();
     }
 
@@ -385,7 +408,7 @@ __global__ __launch_bounds__(SCORE_MOST * 64) void score_kernel(ScoreArgs a) {
     const int j = lane & 15;
     for (int u = 0; u < TOKENS; u += 4) {
       const int tok = u + (lane >> 4);
-      const long long tt = t0 + wave * TOKENS + tok;
+      const long long tt = t0 + tok;
       const bool here = tok < TOKENS && tt < a.T && j < a.k;
       const int c = here ? L.chosen[tok * a.k + j] : -1;
       const bool real = c >= 0;
@@ -435,10 +458,10 @@ struct ScoreBwdArgs {
 
 // dz of the chosen: renormalised g (dg - sum g dg), sigmoid: times (1 - s); a plain softmax: p_e ([e chosen] dg - sum p dg) for every class.  16 lanes a token:
 // they put what the k classes get into a row of zeros in LDS and write the row.
-__global__ __launch_bounds__(SCORE_WAVES * 64) void score_bwd_kernel(ScoreBwdArgs a) {
+__global__ __launch_bounds__(BWD_WAVES * 64) void score_bwd_kernel(ScoreBwdArgs a) {
   extern __shared__ __attribute__((aligned(16))) float rows[];
   const int j = threadIdx.x & 15, sub = threadIdx.x >> 4;
-  constexpr int AT_ONCE = SCORE_WAVES * 4;
+  constexpr int AT_ONCE = BWD_WAVES * 4;
   const int E = a.E, E4 = (E + 3) / 4 * 4;
   float* const out = rows + sub * E4;
   const bool dense = !a.sigmoid && !a.renorm;
@@ -546,17 +569,18 @@ extern "C" int symi_route_scored(const symi_ctx* ctx, const symi_score* hp, cons
   int G, NV;
   score_shape(E, T, G, NV);
   const int per_wave = 64 / G;
-  const int E4 = cdiv(E, 4) * 4, of_all = E4 * 4 + cdiv(E4, 16) * 16, of_wave = score_lds_bytes(E, k, hp->groups, per_wave);
+  const int E4 = cdiv(E, 4) * 4, of_all = E4 * 8 + cdiv(E4, 16) * 16, of_wave = score_lds_bytes(E, k, hp->groups, per_wave);
   // a small batch: one workgroup, which needs no cleared counts
-  const bool alone = T > 0 && (long long)T * E * (k + 2) <= 32768 && T <= SCORE_MOST * per_wave && of_all + cdiv(T, per_wave) * of_wave <= 65536;
+  const bool alone = T > 0 && (long long)T * E * (k + 2) <= 32768 && T <= SCORE_MOST * per_wave && of_all + cdiv(T, per_wave) * of_wave <= SCORE_LDS;
   if (!alone) launch_fill_i32(ctx, hist, E, 0, st);
   if (T > 0) {
     const ScoreArgs a = {logits, bias, idx, gate, hist, T, E, k, cfg->renorm, hp->score == SYMI_SIGMOID, hp->groups, E / hp->groups,
                          hp->top_groups, hp->group_top, hp->scale, alone};
-    int waves = alone ? cdiv(T, per_wave) : SCORE_WAVES;
-    while (waves > 1 && of_all + waves * of_wave > 65536) waves /= 2;
+    // every workgroup adds its counts to the same E words, one after the other: as few of them as fill the chip
+    int waves = alone ? cdiv(T, per_wave) : 1;
+    while (!alone && waves < SCORE_MOST && cdiv(T, per_wave * waves) > ctx->cus && of_all + 2 * waves * of_wave <= SCORE_LDS) waves *= 2;
     const size_t sh = of_all + waves * of_wave;
-    const int grid = alone ? 1 : std::min(cdiv(T, per_wave * waves), 16 / waves * ctx->cus);
+    const int grid = alone ? 1 : std::min(cdiv(T, per_wave * waves), std::max(1, 16 / waves) * ctx->cus);
 #define SYMI_SCORE_CASE(GG, NN)                                                                            \
   case GG * 16 + NN:                                                                                       \
     SYMI_TIMED(ctx, K_SCORE, st, (score_kernel<GG, NN><<<grid, waves * 64, sh, st>>>(a)));                 \
@@ -584,9 +608,9 @@ extern "C" int symi_route_scored_bwd(const symi_ctx* ctx, const symi_score* hp, 
   SYMI_REQUIRE(logits && idx && gate && dgate && dlogits, "symi_route_scored_bwd", "NULL pointer");
   hipStream_t st = as_stream(stream);
   const ScoreBwdArgs a = {logits, idx, gate, dgate, dlogits, cfg->T, cfg->E, cfg->k, cfg->renorm, hp->score == SYMI_SIGMOID, hp->scale};
-  const int grid = std::min(cdiv(cfg->T, SCORE_WAVES * 4), 8 * ctx->cus);
-  const size_t sh = (size_t)SCORE_WAVES * 4 * cdiv(cfg->E, 4) * 4 * sizeof(float);
-  SYMI_TIMED(ctx, K_SCORE_BWD, st, (score_bwd_kernel<<<grid, SCORE_WAVES * 64, sh, st>>>(a)));
+  const int grid = std::min(cdiv(cfg->T, BWD_WAVES * 4), 8 * ctx->cus);
+  const size_t sh = (size_t)BWD_WAVES * 4 * cdiv(cfg->E, 4) * 4 * sizeof(float);
+  SYMI_TIMED(ctx, K_SCORE_BWD, st, (score_bwd_kernel<<<grid, BWD_WAVES * 64, sh, st>>>(a)));
   SYMI_LAUNCH_CHECK("symi_route_scored_bwd");
   return SYMI_OK;
 }
