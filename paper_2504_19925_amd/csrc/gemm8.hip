@@ -383,26 +383,171 @@ __device__ __forceinline__ void gemm8_tile(const Product8& p, uint8_t* const lds
 
 // Workgroup b runs on XCD b mod 8, each with an L2 of its own.  An XCD takes an eighth of the tiles in a row: of every 8 row tiles (of one slot,
 // where it has that many) all column tiles, the row index fastest.
+__device__ __forceinline__ bool deal8(int mts, int ntx, int& mt, int& bn) {
+  const int n_tiles = mts * ntx, chunk = (n_tiles + 7) / 8;
+  const int s = blockIdx.x >> 3, tile = (blockIdx.x & 7) * chunk + s;
+  if (s >= chunk || tile >= n_tiles) return false;
+  const int round = tile / (8 * ntx), in = tile - round * 8 * ntx, rows = min(8, mts - 8 * round);
+  bn = __builtin_amdgcn_readfirstlane(in / rows);
+  mt = __builtin_amdgcn_readfirstlane(8 * round + in % rows);
+  return true;
+}
+
 template <bool EXPERT>
 __global__ __launch_bounds__(G8_THREADS) void gemm8_kernel(Product8 p, int ntx) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[G8_LDS];
-  const int mts = p.map[0], n_tiles = mts * ntx, chunk = (n_tiles + 7) / 8;
-  const int s = blockIdx.x >> 3, tile = (blockIdx.x & 7) * chunk + s;
-  if (s >= chunk || tile >= n_tiles) return;
-  const int round = tile / (8 * ntx), in = tile - round * 8 * ntx, rows = min(8, mts - 8 * round);
-  const int bn = __builtin_amdgcn_readfirstlane(in / rows), mt = __builtin_amdgcn_readfirstlane(8 * round + in % rows);
+  int mt, bn;
+  if (!deal8(p.map[0], ntx, mt, bn)) return;
   const int row0 = __builtin_amdgcn_readfirstlane(p.map[4 + 2 * mt]), entry = __builtin_amdgcn_readfirstlane(p.map[5 + 2 * mt]);
   const int slot = entry & 0xffff, row1 = row0 + (entry >> 16) + 1;
   if (row1 - row0 <= G8_M / 2) gemm8_tile<EXPERT, 4>(p, lds, row0, row1, slot, bn);
   else gemm8_tile<EXPERT, 8>(p, lds, row0, row1, slot, bn);
 }
 
+// ---- fp32 contexts: codes become bf16 values on their way into the bf16 instruction, which keeps fp32's digits and has half the rate.
+// A tile of 128 x 128, 64 x 64 a wavefront, two or three workgroups a unit: while one widens codes (an instruction for two) another has the matrix pipes.  A step's
+// 32 KB go through registers into LDS, loaded a step ahead.  Powers are put into the values as they are widened, exactly, while every power of the wavefront's
+// step is between 2^-100 and 2^100; else a block's sum is scaled behind it, which knows no limits.
+constexpr int W8_M = 128, W8_N = 128;
+
+template <bool SCALED>
+__device__ __forceinline__ void widen16(const intx4_ q, float scale, bf16x8_ (&out)[2]) {   // 16 codes
+  typedef __bf16 bf16x2_ __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const unsigned w = (unsigned)q[2 * h + i];
+      const bf16x2_ lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, SCALED ? scale : 1.f, false);
+      const bf16x2_ hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, SCALED ? scale : 1.f, true);
+      out[h][4 * i] = lo[0];
+      out[h][4 * i + 1] = lo[1];
+      out[h][4 * i + 2] = hi[0];
+      out[h][4 * i + 3] = hi[1];
+    }
+}
+
+__global__ __launch_bounds__(G8_THREADS, 2) void wide8_kernel(Product8 p, int ntx) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[(W8_M + W8_N) * QB];
+  int mt, bn;
+  if (!deal8(p.map[0], ntx, mt, bn)) return;
+  const int row0 = __builtin_amdgcn_readfirstlane(p.map[4 + 2 * mt]), entry = __builtin_amdgcn_readfirstlane(p.map[5 + 2 * mt]);
+  const int slot = entry & 0xffff, last = entry >> 16, n0 = bn * W8_N;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1, quarter = lane >> 4, r16 = lane & 15;
+  const int pitch = p.p8, nk = pitch / QB, slot_blocks = (p.R + QB - 1) / QB;
+  const uint8_t* const a_base = p.Aq + (long long)row0 * pitch;
+  const uint8_t* const w_base = p.Wq + ((long long)slot * p.R + n0) * pitch;
+  // thread -> rows tid / 8 + 32 i, chunk tid % 8
+  unsigned from_a[4], from_w[4], to[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = tid / 8 + 32 * i;
+    from_a[i] = (unsigned)min(r, last) * (unsigned)pitch + (tid & 7) * 16;
+    from_w[i] = (unsigned)min(r, p.R - 1 - n0) * (unsigned)pitch + (tid & 7) * 16;
+    to[i] = r * QB + ((tid & 7) ^ (r >> 1 & 7)) * 16;
+  }
+  const uint8_t* sa_from[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sa_from[i] = p.As + (long long)(row0 + min(wm * 64 + 16 * i + r16, last)) * p.sp;
+  const uint8_t* const sw_from = p.Ws + ((long long)slot * slot_blocks + bn) * p.sp;   // a tile's columns are one block of rows of the weight
+  intx4_ ra[4], rw[4];
+  int pa[4], pw;
+  auto fetch = [&](int k) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      ra[i] = *reinterpret_cast<const intx4_*>(a_base + (long long)k * QB + from_a[i]);
+      rw[i] = *reinterpret_cast<const intx4_*>(w_base + (long long)k * QB + from_w[i]);
+      pa[i] = sa_from[i][k];
+    }
+    pw = sw_from[k];
+  };
+  floatx4_ acc[4][4] = {};
+  fetch(0);
+  for (int k = 0; k < nk; ++k) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      *reinterpret_cast<intx4_*>(lds + to[i]) = ra[i];
+      *reinterpret_cast<intx4_*>(lds + W8_M * QB + to[i]) = rw[i];
+    }
+    int sa[4];
+    bool far = (unsigned)(pw - 27) > 200u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sa[i] = pa[i];
+      far |= (unsigned)(sa[i] - 27) > 200u;
+    }
+    const int sw = pw;
+    __syncthreads();
+    if (k + 1 < nk) fetch(k + 1);
+    auto read = [&](int operand, int block, int x) {
+      const int r = block * 16 + r16;
+      return *reinterpret_cast<const intx4_*>(lds + operand * W8_M * QB + r * QB + ((4 * x + quarter) ^ (r >> 1 & 7)) * 16);
+    };
+    if (!__any(far)) {
+      const float scale_w = power_of(sw);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        bf16x8_ w[4][2];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) widen16<true>(read(1, wn * 4 + j, x), scale_w, w[j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          bf16x8_ a[2];
+          widen16<true>(read(0, wm * 4 + i, x), power_of(sa[i]), a);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[j][h], a[h], acc[i][j], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        bf16x8_ a[2][2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) widen16<false>(read(0, wm * 4 + i, x), 1.f, a[x]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          floatx4_ part = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            bf16x8_ w[2];
+            widen16<false>(read(1, wn * 4 + j, x), 1.f, w);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[h], a[x][h], part, 0, 0, 0);
+          }
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[i][j][c] += ldexpf(part[c], sw + sa[i] - 254);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = wm * 64 + 16 * i + r16;
+    if (r > last) continue;
+    float* const y = static_cast<float*>(p.Y) + (long long)(row0 + r) * p.R + n0 + wn * 64 + 4 * quarter;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (n0 + wn * 64 + 16 * j + 4 * quarter < p.R) *reinterpret_cast<f32x4_f32*>(y + 16 * j) = __builtin_bit_cast(f32x4_f32, acc[i][j]);
+  }
+}
+
+static unsigned grid8(const symi_ctx* ctx, int rows, int ntx) {
+  const long long tiles = ((long long)ctx->cfg.T * ctx->cfg.k / rows + ctx->cfg.S_tot) * ntx;
+  return (unsigned)((tiles + 7) / 8 * 8);
+}
+
 void launch_gemm8(const symi_ctx* ctx, const Product8& p, bool expert, hipStream_t st) {
+  if (ctx->cfg.dtype != SYMI_BF16) {
+    const int ntx = cdiv(p.R, W8_N);
+    SYMI_TIMED(ctx, K_PRODUCT8, st, (wide8_kernel<<<grid8(ctx, W8_M, ntx), G8_THREADS, 0, st>>>(p, ntx)));
+    return;
+  }
   const int ntx = expert ? cdiv(p.R, G8_N / 2) : cdiv(p.R, G8_N);
-  const long long tiles = ((long long)ctx->cfg.T * ctx->cfg.k / G8_M + ctx->cfg.S_tot) * ntx;
-  const unsigned grid = (unsigned)((tiles + 7) / 8 * 8);
-  if (expert) SYMI_TIMED(ctx, K_EXPERT8, st, (gemm8_kernel<true><<<grid, G8_THREADS, 0, st>>>(p, ntx)));
-  else SYMI_TIMED(ctx, K_PRODUCT8, st, (gemm8_kernel<false><<<grid, G8_THREADS, 0, st>>>(p, ntx)));
+  if (expert) SYMI_TIMED(ctx, K_EXPERT8, st, (gemm8_kernel<true><<<grid8(ctx, G8_M, ntx), G8_THREADS, 0, st>>>(p, ntx)));
+  else SYMI_TIMED(ctx, K_PRODUCT8, st, (gemm8_kernel<false><<<grid8(ctx, G8_M, ntx), G8_THREADS, 0, st>>>(p, ntx)));
 }
 
 }  // namespace symi

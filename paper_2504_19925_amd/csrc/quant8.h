@@ -45,7 +45,7 @@ struct Product8 {
 
 __device__ __forceinline__ float sigmoid8(float u) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * u)); }
 
-// gemm8.hip: tiles of 256 rows and weight rows, bf16 contexts; map: entries of 256 rows
+// gemm8.hip: many rows; map: tiles of 256 rows in bf16 contexts, of 128 in fp32 ones
 void launch_gemm8(const symi_ctx* ctx, const Product8& p, bool expert, hipStream_t st);
 
 }  // namespace symi

@@ -317,11 +317,12 @@ static Ws8 ws8_layout(const symi_cfg* c) {
   return L;
 }
 
-// Whether the products of a context take the tiles of 256 rows
-static bool many_rows(const symi_cfg* c) { return c->dtype == SYMI_BF16 && (long long)c->T * c->k > 32LL * c->S_tot; }
+// Whether the products of a context take large tiles
+static bool many_rows(const symi_cfg* c) { return (long long)c->T * c->k > 32LL * c->S_tot; }
 
 static void launch_tiles(const symi_ctx* ctx, const int32_t* offs, int32_t* map, hipStream_t st) {
-  if (many_rows(&ctx->cfg)) SYMI_TIMED(ctx, K_TILES8, st, (tiles8_kernel<256><<<1, 1024, 0, st>>>(offs, ctx->cfg.S_tot, map)));
+  if (many_rows(&ctx->cfg) && ctx->cfg.dtype == SYMI_F32) SYMI_TIMED(ctx, K_TILES8, st, (tiles8_kernel<128><<<1, 1024, 0, st>>>(offs, ctx->cfg.S_tot, map)));
+  else if (many_rows(&ctx->cfg)) SYMI_TIMED(ctx, K_TILES8, st, (tiles8_kernel<256><<<1, 1024, 0, st>>>(offs, ctx->cfg.S_tot, map)));
   else SYMI_TIMED(ctx, K_TILES8, st, (tiles8_kernel<THIN><<<1, 1024, 0, st>>>(offs, ctx->cfg.S_tot, map)));
 }
 
