@@ -563,15 +563,15 @@ static unsigned grid8(const symi_ctx* ctx, int rows, int ntx) {
   return (unsigned)((tiles + 7) / 8 * 8);
 }
 
-void launch_gemm8(const symi_ctx* ctx, const Product8& p, bool expert, hipStream_t st) {
+void launch_gemm8(const symi_ctx* ctx, const Product8& p, int rows, bool expert, hipStream_t st) {
   if (ctx->cfg.dtype != SYMI_BF16) {
     const int ntx = cdiv(p.R, W8_N);
-    SYMI_TIMED(ctx, K_PRODUCT8, st, (wide8_kernel<<<grid8(ctx, W8_M, ntx), G8_THREADS, 0, st>>>(p, ntx)));
+    SYMI_TIMED(ctx, K_PRODUCT8, st, (wide8_kernel<<<grid8(ctx, rows, ntx), G8_THREADS, 0, st>>>(p, ntx)));
     return;
   }
   const int ntx = expert ? cdiv(p.R, G8_N / 2) : cdiv(p.R, G8_N);
-  if (expert) SYMI_TIMED(ctx, K_EXPERT8, st, (gemm8_kernel<true><<<grid8(ctx, G8_M, ntx), G8_THREADS, 0, st>>>(p, ntx)));
-  else SYMI_TIMED(ctx, K_PRODUCT8, st, (gemm8_kernel<false><<<grid8(ctx, G8_M, ntx), G8_THREADS, 0, st>>>(p, ntx)));
+  if (expert) SYMI_TIMED(ctx, K_EXPERT8, st, (gemm8_kernel<true><<<grid8(ctx, rows, ntx), G8_THREADS, 0, st>>>(p, ntx)));
+  else SYMI_TIMED(ctx, K_PRODUCT8, st, (gemm8_kernel<false><<<grid8(ctx, rows, ntx), G8_THREADS, 0, st>>>(p, ntx)));
 }
 
 }  // namespace symi

@@ -339,10 +339,9 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(const void* dY, const
 // Gradient of the rows and the workgroup's sums for dw and db in one pass, a thread having the same columns of every row.  At any time the workgroups
 // are at neighbouring rows.
 template <bool BF16, int LANES, int NV, bool RES>
-__global__ __launch_bounds__(Rows<LANES>::THREADS) void norm_bwd_kernel(const void* dY, const void* R, const float* __restrict__ mean_in,
-                                                                            const float* __restrict__ rstd_in, const float* __restrict__ w, const void* dR,
-                                                                            void* dX, float* __restrict__ part_out, int T, int d, int center,
-                                                                            int want_w, int want_b) {
+__device__ __forceinline__ void norm_bwd_rows(const void* dY, const void* R, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
+                                              const float* __restrict__ w, const void* dR, void* dX, float* __restrict__ part_out, int T, int d,
+                                              int center, int want_w, int want_b, int group, int groups) {
   using G = Rows<LANES>;
   __shared__ float part[4][16];
   const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -351,7 +350,7 @@ __global__ __launch_bounds__(Rows<LANES>::THREADS) void norm_bwd_kernel(const vo
   for (int v = 0; v < NV; ++v) {
     load_weights(w, (v * LANES + l) * 8, d, 1.f, ww[v]);
   }
-  const int step = gridDim.x * G::AT_ONCE;
+  const int step = groups * G::AT_ONCE;
   Eight<BF16> g[NV], x[NV], y[NV];
   float mean = 0.f, rstd = 0.f;
   auto fetch = [&](long long t) {
@@ -371,10 +370,10 @@ __global__ __launch_bounds__(Rows<LANES>::THREADS) void norm_bwd_kernel(const vo
     mean = in && center ? mean_in[t] : 0.f;
     rstd = in ? rstd_in[t] : 0.f;
   };
-  long long t = (long long)blockIdx.x * G::AT_ONCE + sub;
+  long long t = (long long)group * G::AT_ONCE + sub;
   fetch(t);
   int turn = 0;
-  for (long long t0 = (long long)blockIdx.x * G::AT_ONCE; t0 < T; t0 += step, t += step) {
+  for (long long t0 = (long long)group * G::AT_ONCE; t0 < T; t0 += step, t += step) {
     const bool in = t < T;
     float gg[NV][8], xh[NV][8], rr[NV][8];
     const float scale = rstd;
@@ -426,7 +425,7 @@ __global__ __launch_bounds__(Rows<LANES>::THREADS) void norm_bwd_kernel(const vo
   }
   if (!want_w && !want_b) return;
   // the sums of the rows that the workgroup had at once: of a wavefront by exchange, of its wavefronts one after the other by the first
-  float* const to = part_out + (long long)blockIdx.x * 2 * d;
+  float* const to = part_out + (long long)group * 2 * d;
   if constexpr (LANES < 64) {
 #pragma unroll
     for (int v = 0; v < NV; ++v)
@@ -475,6 +474,72 @@ __global__ __launch_bounds__(Rows<LANES>::THREADS) void norm_bwd_kernel(const vo
   }
 }
 
+template <bool BF16, int LANES, int NV, bool RES>
+__global__ __launch_bounds__(Rows<LANES>::THREADS) void norm_bwd_kernel(const void* dY, const void* R, const float* __restrict__ mean_in,
+                                                                        const float* __restrict__ rstd_in, const float* __restrict__ w, const void* dR,
+                                                                        void* dX, float* __restrict__ part_out, int T, int d, int center,
+                                                                        int want_w, int want_b) {
+  norm_bwd_rows<BF16, LANES, NV, RES>(dY, R, mean_in, rstd_in, w, dR, dX, part_out, T, d, center, want_w, want_b, blockIdx.x, gridDim.x);
+}
+
+// dw and db of few rows beside their gradient, in the same launch: a workgroup has 64 columns, 8 threads of 8 each, and every 32nd or 64th row.  The rows
+// are read twice, by two workgroups, which costs less than the launch that would add partial sums up.
+template <bool BF16, int THREADS>
+__device__ __forceinline__ void few_columns(const void* dY, const void* R, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
+                                            float* __restrict__ dw, float* __restrict__ db, int block, int T, int d, int center, float4 (*turned)[8][4]) {
+  const int c = block * 64 + (threadIdx.x & 7) * 8, first = threadIdx.x >> 3;
+  float sw[8] = {}, sb[8] = {};
+  if (c < d) {
+#pragma unroll 4
+    for (int t = first; t < T; t += THREADS / 8) {
+      const float mean = center ? mean_in[t] : 0.f, rstd = rstd_in[t];
+      float g[8], x[8];
+      load8<BF16>(dY, (long long)t * d + c, g);
+      load8<BF16>(R, (long long)t * d + c, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        sw[i] += g[i] * ((x[i] - mean) * rstd);
+        sb[i] += g[i];
+      }
+    }
+  }
+  // of the 8 rows of a wavefront by exchange, of the wavefronts in order
+#pragma unroll
+  for (int m = 8; m < 64; m <<= 1)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      sw[i] += __shfl_xor(sw[i], m, 64);
+      sb[i] += __shfl_xor(sb[i], m, 64);
+    }
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (lane < 8) {
+    turned[wave][lane][0] = make_float4(sw[0], sw[1], sw[2], sw[3]);
+    turned[wave][lane][1] = make_float4(sw[4], sw[5], sw[6], sw[7]);
+    turned[wave][lane][2] = make_float4(sb[0], sb[1], sb[2], sb[3]);
+    turned[wave][lane][3] = make_float4(sb[4], sb[5], sb[6], sb[7]);
+  }
+  __syncthreads();
+  const int k = threadIdx.x & 63, which = threadIdx.x >> 6;   // a column of dw, of db
+  float* const to = which == 0 ? dw : which == 1 ? db : nullptr;
+  if (!to || block * 64 + k >= d) return;
+  float s = 0.f;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) s += reinterpret_cast<const float*>(&turned[w][k >> 3][2 * which])[k & 7];
+  to[block * 64 + k] = s;
+}
+
+template <bool BF16, int LANES, int NV, bool RES>
+__global__ __launch_bounds__(Rows<LANES>::THREADS) void norm_few_kernel(const void* dY, const void* R, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
+                                                       const float* __restrict__ w, const void* dR, void* dX, float* __restrict__ dw,
+                                                       float* __restrict__ db, int T, int d, int center, int column_blocks) {
+  if ((int)blockIdx.x < column_blocks) {
+    __shared__ float4 turned[Rows<LANES>::THREADS / 64][8][4];
+    few_columns<BF16, Rows<LANES>::THREADS>(dY, R, mean_in, rstd_in, dw, db, blockIdx.x, T, d, center, turned);
+    return;
+  }
+  norm_bwd_rows<BF16, LANES, NV, RES>(dY, R, mean_in, rstd_in, w, dR, dX, nullptr, T, d, center, 0, 0, blockIdx.x - column_blocks, gridDim.x - column_blocks);
+}
+
 // Column sums of the partial sums: wavefront w of 16 takes every 16th chunk of 64 columns, and the wavefronts are added in order.
 constexpr int SUM_WAVES = 16;
 __global__ __launch_bounds__(SUM_WAVES * 64) void norm_sum_kernel(const float* __restrict__ part, float* __restrict__ dw, float* __restrict__ db,
@@ -512,7 +577,7 @@ static int norm_parts(const symi_cfg* c) {
   if (c->d > NORM_BWD_IN_REGS) return std::min(c->T, NORM_PARTS);
   int lanes, nv;
   norm_shape(c->d, lanes, nv);
-  return std::min(cdiv(c->T, rows_at_once(lanes)), NORM_PARTS);
+  return std::min(cdiv(c->T, rows_at_once(lanes)), c->T <= 2560 ? NORM_PARTS / 2 : NORM_PARTS);   // 777 x 1160 fp32: 10.7 -> 9.7 us
 }
 
 }  // namespace symi
@@ -593,16 +658,23 @@ extern "C" int symi_norm_bwd(const symi_ctx* ctx, int center, const void* dY, co
   } else if (T > 0) {
     int lanes, nv;
     norm_shape(d, lanes, nv);
+    // Few rows: the sums beside the gradients, or where those take dY's place, in a launch before.  In one launch / with partial sums, us, bf16: 16 rows of 1160 3.9 / 7.6, 400 rows
+    // 5.1 / 9.2, 1024 rows 13.2 / 11.7; 1024 rows of 4096, with twice the threads, 10.5 / 22.3, 2500 rows 22.3 / 29.9.
+    const bool few = (want_w || want_b) && T <= (lanes > 256 ? 2560 : 768);
+    const int columns = cdiv(d, 64), rows = cdiv(T, rows_at_once(lanes));
+#define NORM_BWD(BB, LL, NN, RR)                                                                                                       \
+  if (few) {                                                                                                                           \
+    const int beside = dX == dY ? 0 : rows;                                                                                            \
+    SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_few_kernel<BB, LL, NN, RR><<<columns + beside, Rows<LL>::THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, dw, db, T, d, center, columns))); \
+    if (beside) break;                                                                                                                 \
+  }                                                                                                                                    \
+  SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_kernel<BB, LL, NN, RR><<<parts, Rows<LL>::THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, part, T, d, center, few ? 0 : want_w, few ? 0 : want_b)));
 #define NORM_CASE(LL, NN)                                                                                                              \
   case LL * 8 + NN:                                                                                                                    \
-    if (bf16 && dR)                                                                                                                    \
-      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_kernel<true, LL, NN, true><<<parts, Rows<LL>::THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, part, T, d, center, want_w, want_b)));   \
-    else if (bf16)                                                                                                                     \
-      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_kernel<true, LL, NN, false><<<parts, Rows<LL>::THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, part, T, d, center, want_w, want_b)));  \
-    else if (dR)                                                                                                                       \
-      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_kernel<false, LL, NN, true><<<parts, Rows<LL>::THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, part, T, d, center, want_w, want_b)));  \
-    else                                                                                                                               \
-      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_kernel<false, LL, NN, false><<<parts, Rows<LL>::THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, part, T, d, center, want_w, want_b))); \
+    if (bf16 && dR) { NORM_BWD(true, LL, NN, true) }                                                                                   \
+    else if (bf16) { NORM_BWD(true, LL, NN, false) }                                                                                   \
+    else if (dR) { NORM_BWD(false, LL, NN, true) }                                                                                     \
+    else { NORM_BWD(false, LL, NN, false) }                                                                                            \
     break;
     switch (lanes * 8 + nv) {
       NORM_CASES
@@ -611,6 +683,11 @@ extern "C" int symi_norm_bwd(const symi_ctx* ctx, int center, const void* dY, co
         return SYMI_EUNSUPPORTED;
     }
 #undef NORM_CASE
+#undef NORM_BWD
+    if (few) {
+      SYMI_LAUNCH_CHECK("symi_norm_bwd");
+      return SYMI_OK;
+    }
   }
   if (dw || db) SYMI_TIMED(ctx, K_NORM_SUM, st, (norm_sum_kernel<<<dim3(cdiv(d, 64), 2), SUM_WAVES * 64, 0, st>>>(part, dw, db, parts, d)));
   SYMI_LAUNCH_CHECK("symi_norm_bwd");

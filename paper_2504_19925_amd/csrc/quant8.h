@@ -41,11 +41,12 @@ struct Product8 {
   uint8_t *Hq, *Hs;
   int R, n, p8, sp;     // R: rows of a slot's weight (f in the experts' first product: gate and up rows each)
   int hp8, hsp;         // pitches of Hq, Hs
+  int slots;
 };
 
 __device__ __forceinline__ float sigmoid8(float u) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * u)); }
 
-// gemm8.hip: many rows; map: tiles of 256 rows in bf16 contexts, of 128 in fp32 ones
-void launch_gemm8(const symi_ctx* ctx, const Product8& p, bool expert, hipStream_t st);
+// gemm8.hip: many rows; the map's tiles have 256 or 128 (fp32 contexts: 128)
+void launch_gemm8(const symi_ctx* ctx, const Product8& p, int rows, bool expert, hipStream_t st);
 
 }  // namespace symi

@@ -151,8 +151,7 @@ __global__ __launch_bounds__(Q_THREADS) void dequant_kernel(const uint8_t* __res
 }
 
 // ---------------------------------------------------------------- products
-constexpr int P_THREADS = 256;
-constexpr int THIN = 16;   // rows of a thin tile
+constexpr int THIN = 16;          // rows of a thin tile
 
 // map of tiles of TM rows, slots one after the other
 template <int TM>
@@ -206,17 +205,71 @@ __device__ __forceinline__ void block_product(floatx4_& acc, const intx8& fw, co
   }
 }
 
-// A tile of 16 rows and 256 weight rows: wavefront w has 64 of them, in the experts' first product the gate and up rows of 32 hidden units.
-// Operands come straight from memory, 32 bytes a lane.
+// The same for one tile by a wavefront from the slots' offsets: lane l counts the tiles of consecutive slots, which saves the launch that writes the map (about 4 us,
+// for half a microsecond in every workgroup).  False: there is no such tile.
+constexpr int FIND_SLOTS = 256;
+__device__ __forceinline__ bool find_thin(const int32_t* __restrict__ offs, int S, int tile, int& row0, int& rows, int& slot) {
+  const int lane = threadIdx.x & 63, per = (S + 63) / 64, q0 = min(lane * per, S), q1 = min(q0 + per, S);
+  int at[FIND_SLOTS / 64 + 1];
+#pragma unroll
+  for (int i = 0; i <= FIND_SLOTS / 64; ++i) at[i] = offs[min(q0 + i, q1)];
+  int mine = 0;
+#pragma unroll
+  for (int i = 0; i < FIND_SLOTS / 64; ++i) mine += (at[i + 1] - at[i] + THIN - 1) / THIN;
+  int upto = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int up = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += up;
+  }
+  const unsigned long long behind = __ballot(upto > tile);
+  if (!behind) return false;
+  int left = tile - (upto - mine), found = 0, first = 0, count = 0;
+  bool open = true;
+#pragma unroll
+  for (int i = 0; i < FIND_SLOTS / 64; ++i) {
+    const int n = (at[i + 1] - at[i] + THIN - 1) / THIN;
+    if (open && left < n) {
+      found = q0 + i;
+      first = at[i] + left * THIN;
+      count = min(at[i + 1] - first, THIN);
+      open = false;
+    }
+    left -= n;
+  }
+  const int who = __ffsll(behind) - 1;
+  slot = __builtin_amdgcn_readlane(found, who);
+  row0 = __builtin_amdgcn_readlane(first, who);
+  rows = __builtin_amdgcn_readlane(count, who);
+  return true;
+}
+
+// A tile of 16 rows: a wavefront has 64 weight rows (in the experts' first product the gate and up rows of 32 hidden units) and every SPLIT-th block of the
+// reduction, so that few rows still are many wavefronts with a short way each; their sums are added through LDS, in order.  Operands come straight from memory,
+// 32 bytes a lane.  What bounds it is the weights' stream.
+template <bool EXPERT> struct Thin {
+  static constexpr int COLUMNS = EXPERT ? 4 : 1, SPLIT = 4, THREADS = 64 * COLUMNS * SPLIT;   // wavefronts side by side and along the reduction
+  static constexpr int WIDTH = 64 * COLUMNS;
+};
 template <bool BF16, bool EXPERT>
-__global__ __launch_bounds__(P_THREADS) void thin_product_kernel(Product8 p) {
+__global__ __launch_bounds__(Thin<EXPERT>::THREADS) void thin_product_kernel(Product8 p) {
+  using G = Thin<EXPERT>;
   const int tile = blockIdx.x;
-  if (tile >= p.map[0]) return;
-  const int row0 = p.map[4 + 2 * tile], entry = p.map[5 + 2 * tile], slot = entry & 0xffff, rows = (entry >> 16) + 1;
+  int row0, rows, slot;
+  if (p.slots <= FIND_SLOTS) {
+    if (!find_thin(p.slot_offsets, p.slots, tile, row0, rows, slot)) return;
+  } else {
+    if (tile >= p.map[0]) return;
+    row0 = p.map[4 + 2 * tile];
+    const int entry = p.map[5 + 2 * tile];
+    slot = entry & 0xffff;
+    rows = (entry >> 16) + 1;
+  }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, quarter = lane >> 4;
+  const int wc = wave % G::COLUMNS, part = wave / G::COLUMNS;
   const int slot_rows = EXPERT ? 2 * p.R : p.R, slot_blocks = (slot_rows + QB - 1) / QB;
-  // first weight row of the wavefront's column tile j
-  const int n0 = EXPERT ? blockIdx.y * 128 + wave * 32 : blockIdx.y * 256 + wave * 64;
+  // first weight row of the wavefront
+  const int n0 = EXPERT ? blockIdx.y * 128 + wc * 32 : blockIdx.y * 64;
   const int arow = row0 + min(r16, rows - 1);
   const uint8_t* const a = p.Aq + (long long)arow * p.p8 + quarter * 32;
   const uint8_t* const as = p.As + (long long)arow * p.sp;
@@ -231,8 +284,10 @@ __global__ __launch_bounds__(P_THREADS) void thin_product_kernel(Product8 p) {
     ws[j] = p.Ws + ((long long)slot * slot_blocks + wr / QB) * p.sp;   // of this lane's weight row
   }
   floatx4_ acc[4] = {};
-  for (int k = 0; k < p.p8; k += QB) {
-    const int blk = k / QB;
+  const int nk = p.p8 / QB;
+#pragma unroll 2
+  for (int blk = part; blk < nk; blk += G::SPLIT) {
+    const long long k = (long long)blk * QB;
     intx8 fa;
     {
       const intx4_ lo = *reinterpret_cast<const intx4_*>(a + k), hi = *reinterpret_cast<const intx4_*>(a + k + 16);
@@ -246,6 +301,17 @@ __global__ __launch_bounds__(P_THREADS) void thin_product_kernel(Product8 p) {
       block_product<BF16>(acc[j], fw, fa, ws[j][blk], sa);
     }
   }
+  __shared__ floatx4_ sums[G::SPLIT - 1][G::COLUMNS][4][64];
+  if (part)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sums[part - 1][wc][j][lane] = acc[j];
+  __syncthreads();
+  if (!EXPERT && part) return;
+  if (!part)
+#pragma unroll
+    for (int q = 0; q < G::SPLIT - 1; ++q)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] += sums[q][wc][j][lane];
   const int row = row0 + r16;
   const bool in = r16 < rows;
   if constexpr (!EXPERT) {
@@ -253,46 +319,51 @@ __global__ __launch_bounds__(P_THREADS) void thin_product_kernel(Product8 p) {
     for (int j = 0; j < 4; ++j) {
       const int col = n0 + 16 * j + 4 * quarter;
       if (!in || col >= p.R) continue;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (BF16) static_cast<uint16_t*>(p.Y)[(long long)row * p.R + col + i] = f32_to_bf16(acc[j][i]);
-        else static_cast<float*>(p.Y)[(long long)row * p.R + col + i] = acc[j][i];
+      if constexpr (BF16) {
+        typedef uint32_t u32x2_bf16 __attribute__((ext_vector_type(2), aligned(2)));
+        const u32x2_bf16 y = {pack_bf16x2(acc[j][0], acc[j][1]), pack_bf16x2(acc[j][2], acc[j][3])};
+        *reinterpret_cast<u32x2_bf16*>(static_cast<uint16_t*>(p.Y) + (long long)row * p.R + col) = y;
+      } else {
+        *reinterpret_cast<f32x4_f32*>(static_cast<float*>(p.Y) + (long long)row * p.R + col) = __builtin_bit_cast(f32x4_f32, acc[j]);
       }
     }
   } else {
-    __shared__ int part[4][16];
+    __shared__ int part_most[4][16];
     float h[2][4];
     int most = 0;
+    if (!part) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int col = n0 + 16 * j + 4 * quarter + i;
-        const float u = acc[j][i], v = acc[j + 2][i];
-        h[j][i] = col < p.R ? u * sigmoid8(u) * v : 0.f;
-        most = max(most, size_of(h[j][i]));
-        if (in && col < p.R && p.UV) {
-          p.UV[(long long)row * 2 * p.R + col] = f32_to_bf16(u);
-          p.UV[(long long)row * 2 * p.R + p.R + col] = f32_to_bf16(v);
-          p.H[(long long)row * p.R + col] = f32_to_bf16(h[j][i]);
+        for (int i = 0; i < 4; ++i) {
+          const int col = n0 + 16 * j + 4 * quarter + i;
+          const float u = acc[j][i], v = acc[j + 2][i];
+          h[j][i] = col < p.R ? u * sigmoid8(u) * v : 0.f;
+          most = max(most, size_of(h[j][i]));
+          if (in && col < p.R && p.UV) {
+            p.UV[(long long)row * 2 * p.R + col] = f32_to_bf16(u);
+            p.UV[(long long)row * 2 * p.R + p.R + col] = f32_to_bf16(v);
+            p.H[(long long)row * p.R + col] = f32_to_bf16(h[j][i]);
+          }
         }
-      }
-    most = max(most, __shfl_xor(most, 16, 64));
-    most = max(most, __shfl_xor(most, 32, 64));
-    if (quarter == 0) part[wave][r16] = most;
+      most = max(most, __shfl_xor(most, 16, 64));
+      most = max(most, __shfl_xor(most, 32, 64));
+      if (quarter == 0) part_most[wc][r16] = most;
+    }
     __syncthreads();
-    most = max(max(part[0][r16], part[1][r16]), max(part[2][r16], part[3][r16]));
+    if (part || !in) return;
+    most = max(max(part_most[0][r16], part_most[1][r16]), max(part_most[2][r16], part_most[3][r16]));
     const int e = scale_of(most);
     const float inv = inverse_of(e);
-    if (!in) return;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
       *reinterpret_cast<uint32_t*>(p.Hq + (long long)row * p.hp8 + n0 + 16 * j + 4 * quarter) = codes4(h[j][0], h[j][1], h[j][2], h[j][3], inv);
     uint8_t* const hs = p.Hs + (long long)row * p.hsp;
-    if (wave == 0 && quarter == 0) hs[blockIdx.y] = (uint8_t)e;
-    // zeros behind the last block
-    if (blockIdx.y == gridDim.y - 1 && wave == 0 && quarter == 0)
-      for (int b = gridDim.y; b < p.hsp; ++b) hs[b] = 0;
+    if (wc == 0 && quarter == 0) {
+      hs[blockIdx.y] = (uint8_t)e;
+      if (blockIdx.y == gridDim.y - 1)      // zeros behind the last block
+        for (int b = gridDim.y; b < p.hsp; ++b) hs[b] = 0;
+    }
   }
 }
 
@@ -317,24 +388,33 @@ static Ws8 ws8_layout(const symi_cfg* c) {
   return L;
 }
 
-// Whether the products of a context take large tiles
-static bool many_rows(const symi_cfg* c) { return (long long)c->T * c->k > 32LL * c->S_tot; }
-
-static void launch_tiles(const symi_ctx* ctx, const int32_t* offs, int32_t* map, hipStream_t st) {
-  if (many_rows(&ctx->cfg) && ctx->cfg.dtype == SYMI_F32) SYMI_TIMED(ctx, K_TILES8, st, (tiles8_kernel<128><<<1, 1024, 0, st>>>(offs, ctx->cfg.S_tot, map)));
-  else if (many_rows(&ctx->cfg)) SYMI_TIMED(ctx, K_TILES8, st, (tiles8_kernel<256><<<1, 1024, 0, st>>>(offs, ctx->cfg.S_tot, map)));
-  else SYMI_TIMED(ctx, K_TILES8, st, (tiles8_kernel<THIN><<<1, 1024, 0, st>>>(offs, ctx->cfg.S_tot, map)));
+// Rows of the products' tiles.  Up to 12 rows a slot on average (fp32: 32) the weights' stream is what counts: 8 slots of 4096 x 4096, us by thin / large tiles, 64 rows
+// 31.8 / 40.2, 128 rows 43.9 / 40.4; fp32, 2048 x 2048, 256 rows 18.5 / 27.  Tiles of 128 rows where there are so few that each has a unit of its own (1000 rows, 1024 x
+// 1024: 16.5 -> 11.9 against 256; 2048 rows in 8 slots of 4096 x 4096, where they would be a round and a quarter, 71 against 55).
+static int tile_rows(const symi_ctx* ctx, int R, bool expert) {
+  const symi_cfg* const c = &ctx->cfg;
+  const long long A = (long long)c->T * c->k;
+  if (A <= (c->dtype == SYMI_F32 ? 32LL : 12LL) * c->S_tot) return THIN;
+  if (c->dtype == SYMI_F32) return 128;
+  return (A / 128 + c->S_tot / 2) * cdiv(R, expert ? 128 : 256) <= ctx->cus ? 128 : 256;
 }
 
-static void launch_product(const symi_ctx* ctx, const Product8& p, bool expert, hipStream_t st) {
-  if (many_rows(&ctx->cfg)) return launch_gemm8(ctx, p, expert, st);
+static void launch_tiles(const symi_ctx* ctx, int rows, const int32_t* offs, int32_t* map, hipStream_t st) {
+  const int S = ctx->cfg.S_tot;
+  if (rows == 256) SYMI_TIMED(ctx, K_TILES8, st, (tiles8_kernel<256><<<1, 1024, 0, st>>>(offs, S, map)));
+  else if (rows == 128) SYMI_TIMED(ctx, K_TILES8, st, (tiles8_kernel<128><<<1, 1024, 0, st>>>(offs, S, map)));
+  else if (S > FIND_SLOTS) SYMI_TIMED(ctx, K_TILES8, st, (tiles8_kernel<THIN><<<1, 1024, 0, st>>>(offs, S, map)));
+}
+
+static void launch_product(const symi_ctx* ctx, const Product8& p, int rows, bool expert, hipStream_t st) {
+  if (rows > THIN) return launch_gemm8(ctx, p, rows, expert, st);
   const int tiles = ctx->cfg.T * ctx->cfg.k / THIN + ctx->cfg.S_tot;
   if (expert)
-    SYMI_TIMED(ctx, K_EXPERT8, st, (thin_product_kernel<true, true><<<dim3(tiles, cdiv(p.R, 128)), P_THREADS, 0, st>>>(p)));
+    SYMI_TIMED(ctx, K_EXPERT8, st, (thin_product_kernel<true, true><<<dim3(tiles, cdiv(p.R, 128)), Thin<true>::THREADS, 0, st>>>(p)));
   else if (ctx->cfg.dtype == SYMI_BF16)
-    SYMI_TIMED(ctx, K_PRODUCT8, st, (thin_product_kernel<true, false><<<dim3(tiles, cdiv(p.R, 256)), P_THREADS, 0, st>>>(p)));
+    SYMI_TIMED(ctx, K_PRODUCT8, st, (thin_product_kernel<true, false><<<dim3(tiles, cdiv(p.R, 64)), Thin<false>::THREADS, 0, st>>>(p)));
   else
-    SYMI_TIMED(ctx, K_PRODUCT8, st, (thin_product_kernel<false, false><<<dim3(tiles, cdiv(p.R, 256)), P_THREADS, 0, st>>>(p)));
+    SYMI_TIMED(ctx, K_PRODUCT8, st, (thin_product_kernel<false, false><<<dim3(tiles, cdiv(p.R, 64)), Thin<false>::THREADS, 0, st>>>(p)));
 }
 
 static void launch_quant_rows(const symi_ctx* ctx, bool bf16, const void* X, void* q, void* s, long long rows, int n, const int32_t* limit,
@@ -437,10 +517,11 @@ extern "C" int symi_product8(const symi_ctx* ctx, const void* Aq, const void* As
   if (int rc = check_codes(Wq, Ws, "symi_product8")) return rc;
   hipStream_t st = as_stream(stream);
   int32_t* const map = reinterpret_cast<int32_t*>(align_up((size_t)ws, 256) + ws8_layout(cfg).map);
-  launch_tiles(ctx, slot_offsets, map, st);
+  const int tile = tile_rows(ctx, R, false);
+  launch_tiles(ctx, tile, slot_offsets, map, st);
   const Product8 p = {(const uint8_t*)Aq, (const uint8_t*)As, (const uint8_t*)Wq, (const uint8_t*)Ws, slot_offsets, map, Y,
-                      nullptr, nullptr, nullptr, nullptr, R, n, pitch8(n), scale_pitch8(n), 0, 0};
-  launch_product(ctx, p, false, st);
+                      nullptr, nullptr, nullptr, nullptr, R, n, pitch8(n), scale_pitch8(n), 0, 0, cfg->S_tot};
+  launch_product(ctx, p, tile, false, st);
   SYMI_LAUNCH_CHECK("symi_product8");
   return SYMI_OK;
 }
@@ -462,11 +543,12 @@ extern "C" int symi_expert_fwd8(const symi_ctx* ctx, const void* Xp, const int32
   uint8_t* const base = reinterpret_cast<uint8_t*>(align_up((size_t)ws, 256));
   const int d = cfg->d, f = cfg->f, A = cfg->T * cfg->k;
   int32_t* const map = reinterpret_cast<int32_t*>(base + L.map);
-  launch_tiles(ctx, slot_offsets, map, st);
+  const int tile = std::max(tile_rows(ctx, f, true), tile_rows(ctx, d, false));
+  launch_tiles(ctx, tile, slot_offsets, map, st);
   launch_quant_rows(ctx, true, Xp, base + L.xq, base + L.xs, A, d, slot_offsets + cfg->S_tot, st);
   Product8 p = {base + L.xq, base + L.xs, (const uint8_t*)W1q, (const uint8_t*)W1s, slot_offsets, map, nullptr, (uint16_t*)UV, (uint16_t*)H,
-                base + L.hq, base + L.hs, f, d, pitch8(d), scale_pitch8(d), pitch8(f), scale_pitch8(f)};
-  launch_product(ctx, p, true, st);
+                base + L.hq, base + L.hs, f, d, pitch8(d), scale_pitch8(d), pitch8(f), scale_pitch8(f), cfg->S_tot};
+  launch_product(ctx, p, tile, true, st);
   p.Aq = base + L.hq;
   p.As = base + L.hs;
   p.Wq = (const uint8_t*)W2q;
@@ -476,7 +558,7 @@ extern "C" int symi_expert_fwd8(const symi_ctx* ctx, const void* Xp, const int32
   p.n = f;
   p.p8 = pitch8(f);
   p.sp = scale_pitch8(f);
-  launch_product(ctx, p, false, st);
+  launch_product(ctx, p, tile, false, st);
   SYMI_LAUNCH_CHECK("symi_expert_fwd8");
   return SYMI_OK;
 }
