@@ -1,13 +1,18 @@
 // symi_route_scored / symi_route_scored_bwd / symi_route_bias: routing by softmax or sigmoid scores, with a bias and groups.
 //
-// The choice is that of binary64, but hardly any token needs it: a token is chosen for in fp32, with the runner-up of the last choice, and where two
-// neighbours in that order, or two groups, are nearer than twice what fp32 can be off (nearest), or classes are missing, its wavefront goes
-// through it again in binary64 (choose_exactly).  Of 65536 tokens with 128 classes that is one in some thousand.  Without a bias classes are compared by their
-// logits, exactly.
+// The choice is that of binary64, but hardly any token needs it: classes are chosen in fp32, with the two behind the last choice, and where neighbours in
+// that order are nearer than twice what fp32 can be off (nearest), those few are put in the order of their values in binary64.  Where that does not settle it (the
+// second behind them is near too, the last group that stays and the first that does not are, a softmax, whose sum is needed, classes that are missing), the wavefront
+// goes through the whole row in binary64 (choose_exactly).  Of 65536 tokens with 128 classes the one is the case for some 0.2 %, the other for 0.01 %.  Without a bias
+// classes are compared by their logits, exactly.
 //
-// G lanes hold a token's classes, up to 32 each in pieces of 4: piece p = v G + g lies in lane g, so that loads are whole lines, and the k rounds of
+// G lanes hold a token's classes, up to 16 each in pieces of 4: piece p = v G + g lies in lane g, so that loads are whole lines, and the k rounds of
 // largest, runner-up, ... scan few lanes' registers, with a butterfly of log2 G steps in DPP operands.  Sums of exponentials are taken along a tree over the
 // pieces, the same for every G, so that a token's gates do not depend on its batch.
+//
+// Bound by instructions and their latency: 65536 tokens of 128 classes in 8 groups, sigmoid and bias, 48 us with the launches that clear the counts and move the bias,
+// against 7 of the bytes; taken apart, the rounds take 10, the groups 8, binary64 6, the counts' atomics 4, and 18 are launches, loads and scores.  16 tokens 12.5 us, of
+// which two launches are 8.
 #include <limits.h>
 #include <math.h>
 
@@ -18,6 +23,7 @@
 namespace symi {
 
 constexpr int SCORE_MOST = 16;          // wavefronts of a workgroup at most
+constexpr int SCORE_MAX_K = 16;
 constexpr int SCORE_LDS = 156 * 1024;   // of a workgroup at most
 constexpr int BWD_WAVES = 4;
 constexpr float LOG2E = 1.44269504f;
@@ -36,6 +42,8 @@ struct ScoreArgs {
   int32_t* hist;
   int T, E, k, renorm, sigmoid, groups, per, top_groups, group_top;   // per: classes of a group
   float scale;
+  int lanes;   // neighbouring lanes whose pieces of 4 make a group, where that is so, else 0
+  int shift;   // their logarithm
   int alone;   // one workgroup holds the whole batch and stores its counts
 };
 
@@ -43,26 +51,19 @@ struct ScoreArgs {
 struct ScoreLds {
   float* of;            // [tokens][E]: what groups are compared by; in choose_exactly [E] doubles
   float* group;         // [tokens][groups]
-  int* chosen;          // [tokens][k]; ~class: it only fills up
-  unsigned* kept;       // [tokens][2]: bits of the groups that stay
+  int* chosen;          // [tokens][k + 2]: the classes (~class: it only fills up), the one behind them, whether their order is to be looked at
   float2* softmax;      // [tokens]: largest logit, sum
-  unsigned* flags;      // [tokens]: 1: to be looked at exactly, 2: not a number
 };
-constexpr unsigned NEAR = 1, NOT_A_NUMBER = 2;
 __host__ __device__ inline int score_lds_of(int E, int tokens) { return ((tokens > 2 ? tokens * 4 : 8) * E + 15) / 16 * 16; }
 __host__ __device__ inline int score_lds_bytes(int E, int k, int groups, int tokens) {   // a multiple of 16
-  return score_lds_of(E, tokens) + (tokens * (20 + 4 * groups + 4 * k) + 15) / 16 * 16;
+  return score_lds_of(E, tokens) + (tokens * (8 + 4 * groups + 4 * (k + 2)) + 15) / 16 * 16;
 }
 __device__ __forceinline__ ScoreLds score_lds(char* p, int E, int k, int groups, int tokens) {
   ScoreLds L;
   L.of = reinterpret_cast<float*>(p);
   p += score_lds_of(E, tokens);
-  L.kept = reinterpret_cast<unsigned*>(p);
-  p += tokens * 8;
   L.softmax = reinterpret_cast<float2*>(p);
   p += tokens * 8;
-  L.flags = reinterpret_cast<unsigned*>(p);
-  p += tokens * 4;
   L.group = reinterpret_cast<float*>(p);
   p += tokens * groups * 4;
   L.chosen = reinterpret_cast<int*>(p);
@@ -198,6 +199,15 @@ __device__ __forceinline__ void choose_exactly(const ScoreArgs& a, const float* 
   }
 }
 
+// The two largest values of a lane's and its partner's.
+template <int CTRL>
+__device__ __forceinline__ void two_of(float& best, float& second) {
+  const float b = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(best), CTRL, 0xf, 0xf, false));
+  const float s = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(second), CTRL, 0xf, 0xf, false));
+  second = fmaxf(fminf(best, b), fmaxf(second, s));
+  best = fmaxf(best, b);
+}
+
 // How near two values compared in fp32 may be to each other for their order to be that of binary64.  In units of U32 a sigmoid is off by at most
 // 4 (an exponent of 2 |z| and 2, s (1 - s) |z| < 0.23, the sum and the reciprocal), a softmax by 45 (3 |x| + 2 of the exponential, |x| exp(-|x|) <
 // 0.37, and of the sum the mean of that, at most 3 ln E + 2, with 12 additions); adding the bias, of at most `bias`, rounds once more.  Twice that, and some.
@@ -287,13 +297,7 @@ __global__ __launch_bounds__(SCORE_MOST * 64) void score_kernel(ScoreArgs a) {
     auto score = [&](float x) {
       return a.sigmoid ? __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-x * LOG2E)) : __builtin_amdgcn_exp2f((x - top) * LOG2E) * inv_sum;
     };
-    if (g == 0) {
-      L.flags[sub] = 0;
-      L.softmax[sub] = make_float2(top, sum);
-      L.kept[2 * sub] = L.kept[2 * sub + 1] = 0;
-    }
-    wave_sync();
-    if (nan) atomicOr(&L.flags[sub], NOT_A_NUMBER);
+    bool look = false;      // exactly, at the whole row
 
     // what classes are compared by, in z's place; -inf: not to be chosen.  What groups are compared by goes to LDS.
 #pragma unroll
@@ -318,7 +322,20 @@ __global__ __launch_bounds__(SCORE_MOST * 64) void score_kernel(ScoreArgs a) {
         of[i] = !by_score && scored_groups && live ? s : y;
         z[4 * v + i] = y;
       }
-      if (grouped && c < E) {
+      if (grouped && a.lanes) {
+        // the two largest of the piece, then of the lanes that have the group's other pieces
+        float best = fmaxf(of[0], of[1]), second = fminf(of[0], of[1]);
+        const float b2 = fmaxf(of[2], of[3]), s2 = fminf(of[2], of[3]);
+        second = fmaxf(fminf(best, b2), fmaxf(second, s2));
+        best = fmaxf(best, b2);
+        if (a.lanes >= 2) two_of<0xb1>(best, second);
+        if (a.lanes >= 4) two_of<0x4e>(best, second);
+        if (a.lanes >= 8) two_of<0x141>(best, second);
+        if (a.lanes >= 16) two_of<0x140>(best, second);
+        const int gr = (v * G + g) >> a.shift;
+        if (gr < a.groups && (g & (a.lanes - 1)) == 0) L.group[sub * a.groups + gr] = a.group_top > 1 && second > -INFINITY ? best + second : best;
+        __builtin_amdgcn_sched_barrier(0);   // one piece after the other: side by side they take more registers than there are
+      } else if (grouped && c < E) {
         float* const to = L.of + sub * E + c;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -327,53 +344,63 @@ __global__ __launch_bounds__(SCORE_MOST * 64) void score_kernel(ScoreArgs a) {
     }
     if (grouped) {
       wave_sync();
-      const int pairs = TOKENS * a.groups;
-      for (int p = lane; p < pairs; p += 64) {
-        const int tok = p / a.groups, gr = p - tok * a.groups;
-        const float* const from = L.of + tok * E + gr * a.per;
-        float best = -INFINITY, second = -INFINITY;
-        int at = lane % a.per;              // every lane begins elsewhere: they would meet in the same banks
-        for (int i = 0; i < a.per; ++i) {
-          const float x = from[at];
-          second = fmaxf(second, fminf(best, x));
-          best = fmaxf(best, x);
-          at = at + 1 == a.per ? 0 : at + 1;
+      if (!a.lanes) {
+        const int pairs = TOKENS * a.groups;
+        for (int p = lane; p < pairs; p += 64) {
+          const int tok = p / a.groups, gr = p - tok * a.groups;
+          const float* const from = L.of + tok * E + gr * a.per;
+          float best = -INFINITY, second = -INFINITY;
+          int at = lane % a.per;              // every lane begins elsewhere: they would meet in the same banks
+          for (int i = 0; i < a.per; ++i) {
+            const float x = from[at];
+            second = fmaxf(second, fminf(best, x));
+            best = fmaxf(best, x);
+            at = at + 1 == a.per ? 0 : at + 1;
+          }
+          L.group[p] = a.group_top > 1 && second > -INFINITY ? best + second : best;
         }
-        L.group[p] = a.group_top > 1 && second > -INFINITY ? best + second : best;
+        wave_sync();
       }
-      wave_sync();
-      for (int p = lane; p < pairs; p += 64) {
-        const int tok = p / a.groups, gr = p - tok * a.groups;
-        const float mine_ = L.group[p];
+      // a token's lanes rank its groups, each every G-th
+      unsigned long long kept = 0;
+      const float* const of_token = L.group + sub * a.groups;
+      for (int g0 = 0; g0 < a.groups; g0 += G) {
+        const int gr = g0 + g;
+        const float mine_ = gr < a.groups ? of_token[gr] : -INFINITY;
         int rank = 0;
-        bool near = false;
+        bool close = false;         // one behind it is near
         for (int i = 0; i < a.groups; ++i) {
-          const float x = L.group[tok * a.groups + i];
-          rank += x > mine_ || (x == mine_ && i < gr);
-          near |= scored_groups && i != gr && mine_ > -INFINITY && !(fabsf(x - mine_) > 2.f * closest);
+          const float x = of_token[i];
+          const bool ahead = x > mine_ || (x == mine_ && i < gr);
+          rank += ahead;
+          close |= !ahead && i != gr && mine_ > -INFINITY && !(mine_ - x > 2.f * closest);
         }
-        if (rank < a.top_groups) atomicOr(&L.kept[2 * tok + (gr >> 5)], 1u << (gr & 31));
-        if (near) atomicOr(&L.flags[tok], NEAR);
+        look |= scored_groups && close && rank == a.top_groups - 1;
+        const unsigned long long in = __ballot(gr < a.groups && rank < a.top_groups) >> (sub * G);
+        kept |= (G == 64 ? in : in & ((1ull << (G & 63)) - 1)) << g0;
       }
-      wave_sync();
-      const unsigned lo = L.kept[2 * sub], hi = L.kept[2 * sub + 1];
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const int c = (v * G + g) * 4;
-        const unsigned ids = c < E ? *reinterpret_cast<const unsigned*>(group_of + c) : 0u;
+        if (a.lanes) {
+          const int gr = min((v * G + g) >> a.shift, 63);
+          if (!(kept >> gr & 1))
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const unsigned id = ids >> (8 * i) & 0xff;
-          if (!((id & 32 ? hi : lo) >> (id & 31) & 1)) z[4 * v + i] = -INFINITY;
+            for (int i = 0; i < 4; ++i) z[4 * v + i] = -INFINITY;
+        } else {
+          const unsigned ids = c < E ? *reinterpret_cast<const unsigned*>(group_of + c) : 0u;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!(kept >> (ids >> (8 * i) & 0xff) & 1)) z[4 * v + i] = -INFINITY;
         }
       }
     }
 
-    // the rounds; by score one more, for the distance to the first that is not chosen
+    // the rounds; by score two more: the first that is not chosen may change places with the last that is, the one behind it may not be near
     unsigned taken = 0;
-    bool near = false;
     float before = INFINITY;
-    const int rounds = a.k + (by_score && a.k < E ? 1 : 0);
+    bool order = false;     // two of the chosen and the first behind them are near
+    const int pitch = a.k + 2, rounds = by_score ? min(a.k + 2, E) : a.k;
     for (int j = 0; j < rounds; ++j) {
       float b = -INFINITY;
       int bc = 0;
@@ -387,32 +414,55 @@ __global__ __launch_bounds__(SCORE_MOST * 64) void score_kernel(ScoreArgs a) {
       int at = own;
       best_of<G>(b, at);
       if (at == own) taken |= 1u << bc;
-      if (j < a.k) {
-        near |= at == INT_MAX;                      // somebody has to fill up
-        if (g == 0) L.chosen[sub * a.k + j] = at;
+      if (j < a.k) look |= at == INT_MAX;           // somebody has to fill up
+      if (by_score && j > 0 && at != INT_MAX && !(before - b > closest)) {
+        if (j <= a.k) order = true;
+        else look |= order;
       }
-      if (by_score && j > 0 && at != INT_MAX) near |= !(before - b > closest);
+      if (j <= a.k && g == 0) L.chosen[sub * pitch + j] = at;
       before = b;
     }
-    if (near && g == 0) atomicOr(&L.flags[sub], NEAR);
+    if (rounds <= a.k && g == 0) L.chosen[sub * pitch + a.k] = INT_MAX;
+    look |= order && !(a.sigmoid && a.k < SCORE_MAX_K);
+    const unsigned long long lanes_of = (G == 64 ? ~0ull : (1ull << (G & 63)) - 1) << (sub * G);
+    const bool bad = (__ballot(nan) & lanes_of) != 0;
+    look = (__ballot(look) & lanes_of) != 0;
+    if (g == 0) {
+      L.softmax[sub] = make_float2(bad ? NAN : top, sum);   // NaN: the row is not a number
+      L.chosen[sub * pitch + a.k + 1] = order && !look;
+    }
     wave_sync();
-    unsigned long long again = __ballot(g == 0 && valid && (L.flags[sub] & NEAR));
+    unsigned long long again = __ballot(g == 0 && valid && look);
     while (again) {
       const int tok = (__ffsll((unsigned long long)again) - 1) / G;
       again &= again - 1;
-      choose_exactly(a, a.logits + (t0 + tok) * E, reinterpret_cast<double*>(L.of), L.chosen + tok * a.k);
+      choose_exactly(a, a.logits + (t0 + tok) * E, reinterpret_cast<double*>(L.of), L.chosen + tok * pitch);
       wave_sync();
     }
 
-    // gates relative to the largest of the k: 16 lanes a token
+    // 16 lanes a token: where values are near, the k and the first behind them in the order of binary64; then gates relative to the largest of the k
     const int j = lane & 15;
     for (int u = 0; u < TOKENS; u += 4) {
       const int tok = u + (lane >> 4);
       const long long tt = t0 + tok;
-      const bool here = tok < TOKENS && tt < a.T && j < a.k;
-      const int c = here ? L.chosen[tok * a.k + j] : -1;
-      const bool real = c >= 0;
-      const float x = real ? a.logits[tt * E + c] : 0.f;
+      const bool there = tok < TOKENS && tt < a.T;
+      const int c = there && j <= a.k ? L.chosen[tok * pitch + j] : INT_MAX;
+      const bool real_c = c >= 0 && c != INT_MAX;
+      const float x = real_c ? a.logits[tt * E + c] : 0.f;
+      int at = j;
+      if (__any(there && L.chosen[(there ? tok : 0) * pitch + a.k + 1])) {
+        const double y = real_c ? 1. / (1. + exp(-(double)x)) + (double)bias_s[c] : -(double)INFINITY;
+        int rank = 0;
+        for (int i = 0; i <= a.k; ++i) {
+          const double other = __shfl(y, i, 16);
+          const int oc = __shfl(c, i, 16);
+          rank += other > y || (other == y && oc < c);
+        }
+        if (there && L.chosen[tok * pitch + a.k + 1]) at = rank;
+      }
+      const bool here = there && at < a.k && j <= a.k;
+      const bool real = here && real_c;
+      const float2 q = L.softmax[there ? tok : 0];
       float gate;
       if (a.renorm) {
         const float low = a.sigmoid ? fminf(x, 0.f) : x;
@@ -428,13 +478,12 @@ __global__ __launch_bounds__(SCORE_MOST * 64) void score_kernel(ScoreArgs a) {
       } else if (a.sigmoid) {
         gate = real ? sigmoid_of(x) : 0.f;
       } else {
-        const float2 q = L.softmax[here ? tok : 0];
         gate = real ? expf(x - q.x) / q.y : 0.f;
       }
       if (here) {
         const int e = real ? c : ~c;
-        a.idx[tt * a.k + j] = e;
-        a.gate[tt * a.k + j] = L.flags[tok] & NOT_A_NUMBER ? NAN : a.scale * gate;
+        a.idx[tt * a.k + at] = e;
+        a.gate[tt * a.k + at] = q.x != q.x ? NAN : a.scale * gate;
         atomicAdd(&hist[e], 1);
       }
     }
@@ -545,14 +594,15 @@ static int check_score(const symi_cfg* c, const symi_score* hp, const char* who)
 }
 
 
-// Lanes of a token: few, with up to 32 classes each; a small batch is spread over more of them, so that the chip is filled.
+// Lanes of a token: few, with up to 16 classes each (32 need more registers than a workgroup of 16 wavefronts has: 65536 tokens of 128 classes 55 us, 16 each
+// 48); a small batch is spread over more of them, so that the chip is filled.
 static void score_shape(int E, int T, int& G, int& NV) {
   const int vecs = cdiv(E, 4);
   G = 1;
-  while (G * 8 < vecs) G <<= 1;
+  while (G * 4 < vecs) G <<= 1;
   while (G < vecs && G < 64 && (long long)T * G < 512LL * 256) G <<= 1;
   const int need = cdiv(vecs, G);
-  NV = need <= 1 ? 1 : need <= 2 ? 2 : need <= 4 ? 4 : 8;
+  NV = need <= 1 ? 1 : need <= 2 ? 2 : 4;
 }
 
 }  // namespace symi
@@ -570,12 +620,14 @@ extern "C" int symi_route_scored(const symi_ctx* ctx, const symi_score* hp, cons
   score_shape(E, T, G, NV);
   const int per_wave = 64 / G;
   const int E4 = cdiv(E, 4) * 4, of_all = E4 * 8 + cdiv(E4, 16) * 16, of_wave = score_lds_bytes(E, k, hp->groups, per_wave);
+  const int per = E / hp->groups, pieces = per % 4 ? 0 : per / 4;
+  const int lanes = pieces && !(pieces & (pieces - 1)) && pieces <= std::min(G, 16) ? pieces : 0;
   // a small batch: one workgroup, which needs no cleared counts
   const bool alone = T > 0 && (long long)T * E * (k + 2) <= 32768 && T <= SCORE_MOST * per_wave && of_all + cdiv(T, per_wave) * of_wave <= SCORE_LDS;
   if (!alone) launch_fill_i32(ctx, hist, E, 0, st);
   if (T > 0) {
     const ScoreArgs a = {logits, bias, idx, gate, hist, T, E, k, cfg->renorm, hp->score == SYMI_SIGMOID, hp->groups, E / hp->groups,
-                         hp->top_groups, hp->group_top, hp->scale, alone};
+                         hp->top_groups, hp->group_top, hp->scale, lanes, lanes ? __builtin_ctz(lanes) : 0, alone};
     // every workgroup adds its counts to the same E words, one after the other: as few of them as fill the chip
     int waves = alone ? cdiv(T, per_wave) : 1;
     while (!alone && waves < SCORE_MOST && cdiv(T, per_wave * waves) > ctx->cus && of_all + 2 * waves * of_wave <= SCORE_LDS) waves *= 2;
@@ -585,10 +637,9 @@ extern "C" int symi_route_scored(const symi_ctx* ctx, const symi_score* hp, cons
   case GG * 16 + NN:                                                                                       \
     SYMI_TIMED(ctx, K_SCORE, st, (score_kernel<GG, NN><<<grid, waves * 64, sh, st>>>(a)));                 \
     break;
-#define SYMI_SCORE_G(GG) SYMI_SCORE_CASE(GG, 1) SYMI_SCORE_CASE(GG, 2) SYMI_SCORE_CASE(GG, 4) SYMI_SCORE_CASE(GG, 8)
+#define SYMI_SCORE_G(GG) SYMI_SCORE_CASE(GG, 1) SYMI_SCORE_CASE(GG, 2) SYMI_SCORE_CASE(GG, 4)
     switch (G * 16 + NV) {
-      SYMI_SCORE_G(1) SYMI_SCORE_G(2) SYMI_SCORE_G(4) SYMI_SCORE_G(8) SYMI_SCORE_G(16) SYMI_SCORE_G(32)
-      SYMI_SCORE_CASE(64, 1) SYMI_SCORE_CASE(64, 2) SYMI_SCORE_CASE(64, 4)
+      SYMI_SCORE_G(1) SYMI_SCORE_G(2) SYMI_SCORE_G(4) SYMI_SCORE_G(8) SYMI_SCORE_G(16) SYMI_SCORE_G(32) SYMI_SCORE_G(64)
       default:
         set_error("symi_route_scored: no kernel for %d lanes x %d pieces per token", G, NV);
         return SYMI_EUNSUPPORTED;
