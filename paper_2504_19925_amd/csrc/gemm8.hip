@@ -76,14 +76,13 @@ __device__ __forceinline__ void gemm8_tile(const Product8& p, uint8_t* const lds
   const int slot_rows = EXPERT ? 2 * p.R : p.R, slot_blocks = (slot_rows + QB - 1) / QB;
   const int nk = pitch / QB, groups = (nk + 3) / 4;
 
-  // tile column -> weight row: as it is, or of every 64 the gate rows of 32 hidden units and their up rows
+  // tile column -> weight row, counted from n0 (32 bits of offset reach it): as it is, or of every 64 the gate rows of 32 hidden units and their up rows
   auto weight_row = [&](int c) {
-    if (!EXPERT) return min(n0 + c, p.R - 1);
-    const int hu = min(n0 + (c >> 6) * 32 + (c & 31), p.R - 1);
-    return ((c >> 5) & 1) * p.R + hu;
+    if (!EXPERT) return min(c, p.R - 1 - n0);
+    return ((c >> 5) & 1) * p.R + min((c >> 6) * 32 + (c & 31), p.R - 1 - n0);
   };
   const uint8_t* const a_base = p.Aq + (long long)row0 * pitch;
-  const uint8_t* const w_base = p.Wq + (long long)slot * slot_rows * pitch;
+  const uint8_t* const w_base = p.Wq + ((long long)slot * slot_rows + n0) * pitch;
   const int last = row1 - row0 - 1;
   // Loads: wavefront w, instruction j fills rows 8 LA w + 8 j .. of the left stage (64 w + 8 j of the right one), lane l row l / 8, chunk l % 8.
   // A scalar base a step, an offset a lane, and an immediate that counts in memory and in LDS: M0, the LDS base, stands in the middle of what an operand's
@@ -96,7 +95,7 @@ __device__ __forceinline__ void gemm8_tile(const Product8& p, uint8_t* const lds
     vo_w[j] = (unsigned)weight_row(64 * wave + 8 * j + (lane >> 3)) * (unsigned)pitch + chunk + 4096u - (unsigned)((j - 4) * 1024);
   }
   const unsigned vs_a = (unsigned)min(64 * wave + lane, last) * (unsigned)p.sp;
-  const unsigned vs_w = (unsigned)(weight_row(64 * wave + lane) / QB) * (unsigned)p.sp;
+  const unsigned vs_w = (unsigned)((n0 + weight_row(64 * wave + lane)) / QB) * (unsigned)p.sp;
   const uint8_t* const sa_base = p.As + (long long)row0 * p.sp;
   const uint8_t* const sw_base = p.Ws + (long long)slot * slot_blocks * p.sp;
   const unsigned base = (unsigned)(size_t)(void __attribute__((address_space(3)))*)lds;

@@ -247,3 +247,34 @@ def test_refusals():
     symi.symi_expert_fwd8(none, e, offs, w, w_s, w2, w2_s, None, None, e, scratch(none))
     symi.symi_product8(none, codes(0), scales(0), offs, w, w_s, 64, 64, e, scratch(none))
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("A", [3, 40], ids=["thin", "large"])
+def test_weights_beyond_four_gigabytes(A):
+    """Offsets into a slot's weight pass 32 bits: columns on both sides of that, and the last ones."""
+    n, R = 4104, 1040008                     # 4224 bytes a row: 4.39e9
+    ctx = context(A, 1, "bf16")
+    p, sp = symi.symi_pitch8(n), symi.symi_scale_pitch8(n)
+    assert p * R > 2 ** 32
+    g = gen(1)
+    aq, a_s, a = quant(ctx, whole(1, 1, A, n), 1)
+    wq = torch.zeros(1, R, p, dtype=torch.uint8, device="cuda")
+    w_s = torch.full((1, -(-R // 128), sp), 127, dtype=torch.uint8, device="cuda")
+    at = sorted({0, 127, 2 ** 32 // p - 1, 2 ** 32 // p, 2 ** 32 // p + 1, 2 ** 31 // p + 1, R - 9, R - 1})
+    few = torch.randint(-3, 4, (len(at), n), generator=g, device="cuda").float()
+    wq[0, at, :n] = few.to(torch.float8_e4m3fn).view(torch.uint8)
+    Y = torch.full((A, R), 640.0, dtype=torch.bfloat16, device="cuda")
+    _, offs = offsets_of([A])
+    symi.symi_product8(ctx, aq, a_s, offs, wq.view(torch.float8_e4m3fn), w_s, R, n, Y, scratch(ctx))
+    want = torch.from_numpy(a[0] @ Hn.npf(few).astype(np.float64).T).float().to(torch.bfloat16).cuda()
+    assert torch.equal(Y[:, at], want)
+    Y[:, at] = 0
+    assert not Y.any()
+
+
+def test_more_columns_than_a_launch_has_are_refused():
+    L, some = symi.lib(), 256                # refused before anything is read
+    for dtype in ("bf16", "f32"):
+        ctx = context(1, 1, dtype)
+        assert L.symi_product8(ctx.ptr, some, some, some, some, some, 65535 * 64 + 8, 1024, some, some, None) == -2
+        assert "tiles" in symi.symi_last_error()
