@@ -336,12 +336,67 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(const void* dY, const
   }
 }
 
+// dw and db of few rows beside their gradient, in the same launch: a workgroup has 64 columns, 8 threads of 8 each, and every 32nd or 64th row.  The rows
+// are read twice, by two workgroups, which costs less than the launch that would add partial sums up.
+template <bool BF16, int THREADS>
+__device__ __forceinline__ void few_columns(const void* dY, const void* R, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
+                                            float* __restrict__ dw, float* __restrict__ db, int block, int T, int d, int center, float4 (*turned)[8][4]) {
+  const int c = block * 64 + (threadIdx.x & 7) * 8, first = threadIdx.x >> 3;
+  float sw[8] = {}, sb[8] = {};
+  if (c < d) {
+#pragma unroll 4
+    for (int t = first; t < T; t += THREADS / 8) {
+      const float mean = center ? mean_in[t] : 0.f, rstd = rstd_in[t];
+      float g[8], x[8];
+      load8<BF16>(dY, (long long)t * d + c, g);
+      load8<BF16>(R, (long long)t * d + c, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        sw[i] += g[i] * ((x[i] - mean) * rstd);
+        sb[i] += g[i];
+      }
+    }
+  }
+  // of the 8 rows of a wavefront by exchange, of the wavefronts in order
+#pragma unroll
+  for (int m = 8; m < 64; m <<= 1)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      sw[i] += __shfl_xor(sw[i], m, 64);
+      sb[i] += __shfl_xor(sb[i], m, 64);
+    }
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (lane < 8) {
+    turned[wave][lane][0] = make_float4(sw[0], sw[1], sw[2], sw[3]);
+    turned[wave][lane][1] = make_float4(sw[4], sw[5], sw[6], sw[7]);
+    turned[wave][lane][2] = make_float4(sb[0], sb[1], sb[2], sb[3]);
+    turned[wave][lane][3] = make_float4(sb[4], sb[5], sb[6], sb[7]);
+  }
+  __syncthreads();
+  const int k = threadIdx.x & 63, which = threadIdx.x >> 6;   // a column of dw, of db
+  float* const to = which == 0 ? dw : which == 1 ? db : nullptr;
+  if (!to || block * 64 + k >= d) return;
+  float s = 0.f;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) s += reinterpret_cast<const float*>(&turned[w][k >> 3][2 * which])[k & 7];
+  to[block * 64 + k] = s;
+}
+
 // Gradient of the rows and the workgroup's sums for dw and db in one pass, a thread having the same columns of every row.  At any time the workgroups
-// are at neighbouring rows.
-template <bool BF16, int LANES, int NV, bool RES>
-__device__ __forceinline__ void norm_bwd_rows(const void* dY, const void* R, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
-                                              const float* __restrict__ w, const void* dR, void* dX, float* __restrict__ part_out, int T, int d,
-                                              int center, int want_w, int want_b, int group, int groups) {
+// are at neighbouring rows.  FEW: the first `columns` workgroups have the columns' sums, and the others leave theirs.
+template <bool BF16, int LANES, int NV, bool RES, bool FEW>
+__global__ __launch_bounds__(Rows<LANES>::THREADS) void norm_bwd_kernel(const void* dY, const void* R, const float* __restrict__ mean_in,
+                                                                        const float* __restrict__ rstd_in, const float* __restrict__ w, const void* dR,
+                                                                        void* dX, float* __restrict__ part_out, int T, int d, int center, int want_w,
+                                                                        int want_b, float* __restrict__ dw, float* __restrict__ db, int columns) {
+  if constexpr (FEW) {
+    if ((int)blockIdx.x < columns) {
+      __shared__ float4 turned[Rows<LANES>::THREADS / 64][8][4];
+      few_columns<BF16, Rows<LANES>::THREADS>(dY, R, mean_in, rstd_in, dw, db, blockIdx.x, T, d, center, turned);
+      return;
+    }
+  }
+  const int group = FEW ? blockIdx.x - columns : blockIdx.x, groups = FEW ? gridDim.x - columns : gridDim.x;
   using G = Rows<LANES>;
   __shared__ float part[4][16];
   const int l = threadIdx.x % LANES, sub = threadIdx.x / LANES, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -423,7 +478,7 @@ __device__ __forceinline__ void norm_bwd_rows(const void* dY, const void* R, con
       if (c < d && in) out.store(dX, t * d + c);
     }
   }
-  if (!want_w && !want_b) return;
+  if (FEW || (!want_w && !want_b)) return;
   // the sums of the rows that the workgroup had at once: of a wavefront by exchange, of its wavefronts one after the other by the first
   float* const to = part_out + (long long)group * 2 * d;
   if constexpr (LANES < 64) {
@@ -472,72 +527,6 @@ __device__ __forceinline__ void norm_bwd_rows(const void* dY, const void* R, con
         if (want_b) to[d + c + i] = sb[v][i];
       }
   }
-}
-
-template <bool BF16, int LANES, int NV, bool RES>
-__global__ __launch_bounds__(Rows<LANES>::THREADS) void norm_bwd_kernel(const void* dY, const void* R, const float* __restrict__ mean_in,
-                                                                        const float* __restrict__ rstd_in, const float* __restrict__ w, const void* dR,
-                                                                        void* dX, float* __restrict__ part_out, int T, int d, int center,
-                                                                        int want_w, int want_b) {
-  norm_bwd_rows<BF16, LANES, NV, RES>(dY, R, mean_in, rstd_in, w, dR, dX, part_out, T, d, center, want_w, want_b, blockIdx.x, gridDim.x);
-}
-
-// dw and db of few rows beside their gradient, in the same launch: a workgroup has 64 columns, 8 threads of 8 each, and every 32nd or 64th row.  The rows
-// are read twice, by two workgroups, which costs less than the launch that would add partial sums up.
-template <bool BF16, int THREADS>
-__device__ __forceinline__ void few_columns(const void* dY, const void* R, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
-                                            float* __restrict__ dw, float* __restrict__ db, int block, int T, int d, int center, float4 (*turned)[8][4]) {
-  const int c = block * 64 + (threadIdx.x & 7) * 8, first = threadIdx.x >> 3;
-  float sw[8] = {}, sb[8] = {};
-  if (c < d) {
-#pragma unroll 4
-    for (int t = first; t < T; t += THREADS / 8) {
-      const float mean = center ? mean_in[t] : 0.f, rstd = rstd_in[t];
-      float g[8], x[8];
-      load8<BF16>(dY, (long long)t * d + c, g);
-      load8<BF16>(R, (long long)t * d + c, x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        sw[i] += g[i] * ((x[i] - mean) * rstd);
-        sb[i] += g[i];
-      }
-    }
-  }
-  // of the 8 rows of a wavefront by exchange, of the wavefronts in order
-#pragma unroll
-  for (int m = 8; m < 64; m <<= 1)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      sw[i] += __shfl_xor(sw[i], m, 64);
-      sb[i] += __shfl_xor(sb[i], m, 64);
-    }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (lane < 8) {
-    turned[wave][lane][0] = make_float4(sw[0], sw[1], sw[2], sw[3]);
-    turned[wave][lane][1] = make_float4(sw[4], sw[5], sw[6], sw[7]);
-    turned[wave][lane][2] = make_float4(sb[0], sb[1], sb[2], sb[3]);
-    turned[wave][lane][3] = make_float4(sb[4], sb[5], sb[6], sb[7]);
-  }
-  __syncthreads();
-  const int k = threadIdx.x & 63, which = threadIdx.x >> 6;   // a column of dw, of db
-  float* const to = which == 0 ? dw : which == 1 ? db : nullptr;
-  if (!to || block * 64 + k >= d) return;
-  float s = 0.f;
-#pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) s += reinterpret_cast<const float*>(&turned[w][k >> 3][2 * which])[k & 7];
-  to[block * 64 + k] = s;
-}
-
-template <bool BF16, int LANES, int NV, bool RES>
-__global__ __launch_bounds__(Rows<LANES>::THREADS) void norm_few_kernel(const void* dY, const void* R, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
-                                                       const float* __restrict__ w, const void* dR, void* dX, float* __restrict__ dw,
-                                                       float* __restrict__ db, int T, int d, int center, int column_blocks) {
-  if ((int)blockIdx.x < column_blocks) {
-    __shared__ float4 turned[Rows<LANES>::THREADS / 64][8][4];
-    few_columns<BF16, Rows<LANES>::THREADS>(dY, R, mean_in, rstd_in, dw, db, blockIdx.x, T, d, center, turned);
-    return;
-  }
-  norm_bwd_rows<BF16, LANES, NV, RES>(dY, R, mean_in, rstd_in, w, dR, dX, nullptr, T, d, center, 0, 0, blockIdx.x - column_blocks, gridDim.x - column_blocks);
 }
 
 // Column sums of the partial sums: wavefront w of 16 takes every 16th chunk of 64 columns, and the wavefronts are added in order.
@@ -665,10 +654,10 @@ extern "C" int symi_norm_bwd(const symi_ctx* ctx, int center, const void* dY, co
 #define NORM_BWD(BB, LL, NN, RR)                                                                                                       \
   if (few) {                                                                                                                           \
     const int beside = dX == dY ? 0 : rows;                                                                                            \
-    SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_few_kernel<BB, LL, NN, RR><<<columns + beside, Rows<LL>::THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, dw, db, T, d, center, columns))); \
+    SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_kernel<BB, LL, NN, RR, true><<<columns + beside, Rows<LL>::THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, nullptr, T, d, center, 0, 0, dw, db, columns))); \
     if (beside) break;                                                                                                                 \
   }                                                                                                                                    \
-  SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_kernel<BB, LL, NN, RR><<<parts, Rows<LL>::THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, part, T, d, center, few ? 0 : want_w, few ? 0 : want_b)));
+  SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_kernel<BB, LL, NN, RR, false><<<parts, Rows<LL>::THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, part, T, d, center, few ? 0 : want_w, few ? 0 : want_b, nullptr, nullptr, 0)));
 #define NORM_CASE(LL, NN)                                                                                                              \
   case LL * 8 + NN:                                                                                                                    \
     if (bf16 && dR) { NORM_BWD(true, LL, NN, true) }                                                                                   \
