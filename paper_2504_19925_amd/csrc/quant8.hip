@@ -73,10 +73,12 @@ __global__ __launch_bounds__(Q_THREADS) void quant_rows_kernel(const void* __res
 // A workgroup a block of 128 x 128: 16 lanes a row, 16 rows at a time, all in registers until the largest is known.  128 weights of 2816 x 2048 in bf16 556 us, 4.0 TB/s.
 template <bool BF16>
 __global__ __launch_bounds__(Q_THREADS) void quant_blocks_kernel(const void* __restrict__ X, uint8_t* __restrict__ q, uint8_t* __restrict__ s,
-                                                                 int rows, int n, int p8, int sp, int rb) {
+                                                                 int rows, int n, int p8, int sp, int rb, unsigned blocks) {
   __shared__ int part[Q_THREADS / 64];
-  const int bc = blockIdx.x % sp;
-  const long long br_all = blockIdx.x / sp;
+  const unsigned at = flat_block();
+  if (at >= blocks) return;
+  const int bc = at % sp;
+  const long long br_all = at / sp;
   const int group = (int)(br_all / rb), br = (int)(br_all - (long long)group * rb);
   const int l16 = threadIdx.x & 15, c = bc * QB + l16 * 8;
   const long long si = br_all * sp + bc;
@@ -490,9 +492,9 @@ extern "C" int symi_quant8(const symi_ctx* ctx, const void* X, int groups, int r
       return SYMI_EUNSUPPORTED;
     }
     if (bf16)
-      SYMI_TIMED(ctx, K_QUANT8, st, (quant_blocks_kernel<true><<<(unsigned)blocks, Q_THREADS, 0, st>>>(X, (uint8_t*)q, (uint8_t*)s, rows, n, pitch8(n), sp, rb)));
+      SYMI_TIMED(ctx, K_QUANT8, st, (quant_blocks_kernel<true><<<flat_grid(blocks), Q_THREADS, 0, st>>>(X, (uint8_t*)q, (uint8_t*)s, rows, n, pitch8(n), sp, rb, (unsigned)blocks)));
     else
-      SYMI_TIMED(ctx, K_QUANT8, st, (quant_blocks_kernel<false><<<(unsigned)blocks, Q_THREADS, 0, st>>>(X, (uint8_t*)q, (uint8_t*)s, rows, n, pitch8(n), sp, rb)));
+      SYMI_TIMED(ctx, K_QUANT8, st, (quant_blocks_kernel<false><<<flat_grid(blocks), Q_THREADS, 0, st>>>(X, (uint8_t*)q, (uint8_t*)s, rows, n, pitch8(n), sp, rb, (unsigned)blocks)));
   }
   SYMI_LAUNCH_CHECK("symi_quant8");
   return SYMI_OK;

@@ -586,11 +586,6 @@ __global__ __launch_bounds__(256) void router_finish_kernel(RouterParams p, int 
 }
 
 // ---- fp32 configurations: plain FMAs
-// Workgroups in one row of up to 2^20 and as many rows as it takes: a dimension of a launch ends at 2^32 threads, which 2^20
-// tokens of d = 2048, E = 256 pass.  There are fewer than 2^32 workgroups of anything that fits the memory; those behind the last have no work.
-__device__ __forceinline__ unsigned flat_block() { return blockIdx.y * gridDim.x + blockIdx.x; }
-static dim3 flat_grid(long long n) { return n <= 1 << 20 ? dim3((unsigned)n) : dim3(1 << 20, cdiv(n, 1 << 20)); }
-
 // Eight lanes share the reductions of a token with four classes: pieces of eight indices dealt out in turn, 256 consecutive
 // bytes of X and of each row of Wr per load round, the eight sums added in a fixed tree.  Bound by latency: with one
 // thread per logit, a chain of d / 8 rounds, T = 139, E = 16, d = 288 took 11.5 us; error 1.4e-7 -> 0.6e-7.
