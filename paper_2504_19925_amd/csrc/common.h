@@ -50,7 +50,7 @@ static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; 
 static inline int cdiv(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 // Workgroups in one row of up to 2^20 and as many rows as it takes: a dimension of a launch ends at 2^32 threads (beyond that some workgroups are left out, without an
-// error), which 2^20 tokens of a gate network of d = 2048, E = 256 pass, 2^22 weights of a row each on their way to 8 bits.  There are fewer
+// error), which 2^20 tokens of a gate network of d = 2048, E = 256 pass, 2^22 weights of a row each on their way to 8 bits, 2^22 wide rows of a norm.  There are fewer
 // than 2^32 workgroups of anything that fits the memory; those behind the last have no work.
 __device__ __forceinline__ unsigned flat_block() { return blockIdx.y * gridDim.x + blockIdx.x; }
 static inline dim3 flat_grid(long long n) { return n <= 1 << 20 ? dim3((unsigned)n) : dim3(1 << 20, cdiv(n, 1 << 20)); }

@@ -124,13 +124,15 @@ __device__ __forceinline__ float block_sum(float x, float* part) {
   return s;
 }
 
-// Rows beyond that: one workgroup a row, read three times; a thread reads back what it wrote itself.
+// Rows of more than NORM_IN_REGS values: one workgroup a row, read three times; a thread reads back what it wrote itself.
 template <bool BF16>
 __global__ __launch_bounds__(WIDE_THREADS) void norm_wide_kernel(const void* X, const void* res, const float* __restrict__ w,
                                                                  const float* __restrict__ b, void* R, void* Y, float* __restrict__ mean_out,
-                                                                 float* __restrict__ rstd_out, int d, int center, float eps) {
+                                                                 float* __restrict__ rstd_out, int T, int d, int center, float eps) {
   __shared__ float part[WIDE_THREADS / 64];
-  const long long row = (long long)blockIdx.x * d;
+  const int t = flat_block();
+  if (t >= T) return;
+  const long long row = (long long)t * d;
   float s = 0.f;
   for (int c = threadIdx.x * 8; c < d; c += WIDE_THREADS * 8) {
     float x[8];
@@ -166,8 +168,8 @@ __global__ __launch_bounds__(WIDE_THREADS) void norm_wide_kernel(const void* X, 
     store8<BF16>(Y, row + c, x);
   }
   if (threadIdx.x == 0) {
-    if (mean_out) mean_out[blockIdx.x] = mean;
-    if (rstd_out) rstd_out[blockIdx.x] = rstd;
+    if (mean_out) mean_out[t] = mean;
+    if (rstd_out) rstd_out[t] = rstd;
   }
 }
 
@@ -278,10 +280,12 @@ __global__ __launch_bounds__(Rows<LANES>::THREADS) void norm_kernel(const void* 
 template <bool BF16>
 __global__ __launch_bounds__(WIDE_THREADS) void norm_bwd_wide_kernel(const void* dY, const void* R, const float* __restrict__ mean_in,
                                                                 const float* __restrict__ rstd_in, const float* __restrict__ w, const void* dR,
-                                                                void* dX, int d, int center) {
+                                                                void* dX, int T, int d, int center) {
   __shared__ float part[WIDE_THREADS / 64];
-  const long long row = (long long)blockIdx.x * d;
-  const float mean = center ? mean_in[blockIdx.x] : 0.f, rstd = rstd_in[blockIdx.x];
+  const int t = flat_block();
+  if (t >= T) return;
+  const long long row = (long long)t * d;
+  const float mean = center ? mean_in[t] : 0.f, rstd = rstd_in[t];
   float level = 0.f, along = 0.f;
   for (int c = threadIdx.x * 8; c < d; c += WIDE_THREADS * 8) {
     float g[8], x[8];
@@ -590,8 +594,8 @@ extern "C" int symi_norm_fwd(const symi_ctx* ctx, int center, float eps, const v
   const int T = cfg->T, d = cfg->d;
   const bool bf16 = cfg->dtype == SYMI_BF16;
   if (d > NORM_IN_REGS) {
-    if (bf16) SYMI_TIMED(ctx, K_NORM, st, (norm_wide_kernel<true><<<T, WIDE_THREADS, 0, st>>>(X, residual, w, b, R, Y, mean, rstd, d, center, eps)));
-    else SYMI_TIMED(ctx, K_NORM, st, (norm_wide_kernel<false><<<T, WIDE_THREADS, 0, st>>>(X, residual, w, b, R, Y, mean, rstd, d, center, eps)));
+    if (bf16) SYMI_TIMED(ctx, K_NORM, st, (norm_wide_kernel<true><<<flat_grid(T), WIDE_THREADS, 0, st>>>(X, residual, w, b, R, Y, mean, rstd, T, d, center, eps)));
+    else SYMI_TIMED(ctx, K_NORM, st, (norm_wide_kernel<false><<<flat_grid(T), WIDE_THREADS, 0, st>>>(X, residual, w, b, R, Y, mean, rstd, T, d, center, eps)));
   } else {
     int lanes, nv;
     norm_shape(d, lanes, nv);
@@ -638,11 +642,11 @@ extern "C" int symi_norm_bwd(const symi_ctx* ctx, int center, const void* dY, co
     if (bf16) {
       if (want_w || want_b)
         SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_columns_kernel<true><<<grid, 256, 0, st>>>(dY, R, mean, rstd, part, T, d, center, cdiv(T, parts), want_w, want_b)));
-      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_wide_kernel<true><<<T, WIDE_THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, d, center)));
+      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_wide_kernel<true><<<flat_grid(T), WIDE_THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, T, d, center)));
     } else {
       if (want_w || want_b)
         SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_columns_kernel<false><<<grid, 256, 0, st>>>(dY, R, mean, rstd, part, T, d, center, cdiv(T, parts), want_w, want_b)));
-      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_wide_kernel<false><<<T, WIDE_THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, d, center)));
+      SYMI_TIMED(ctx, K_NORM_BWD, st, (norm_bwd_wide_kernel<false><<<flat_grid(T), WIDE_THREADS, 0, st>>>(dY, R, mean, rstd, w, dR, dX, T, d, center)));
     }
   } else if (T > 0) {
     int lanes, nv;
