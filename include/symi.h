@@ -492,7 +492,7 @@ int symi_dequant8(const symi_ctx* ctx, const void* q, const void* s, int groups,
  *   the largest (some 1.5e-5 of a result, a hundredth of its rounding), in an fp32 context at half that rate without such a loss.
  *   Aq, As: [T k, n] with block = 1;  Wq, Ws: [S_tot, R, n] with block = 128;  slot_offsets [S_tot+1] as symi_dispatch's, up to T k;
  *   Y [T k, R] out in the activation dtype; rows outside the slots are not written.  R a multiple of 8, at most 2^22 (with few
- *   rows a slot at most 65535 * 64, else SYMI_EUNSUPPORTED).
+ *   rows a slot at most 65535 * 64, with many at most 2^24 - 9 tiles, which no memory holds, else SYMI_EUNSUPPORTED).
  *   ws: symi_workspace8_bytes(cfg) bytes of scratch, under the rules of symi_workspace_bytes (0 if cfg is invalid). */
 size_t symi_workspace8_bytes(const symi_cfg* cfg);
 int symi_product8(const symi_ctx* ctx, const void* Aq, const void* As, const int32_t* slot_offsets, const void* Wq,

@@ -402,10 +402,12 @@ static int tile_rows(const symi_ctx* ctx, int R, bool expert) {
   return (A / 128 + c->S_tot / 2) * cdiv(R, expert ? 128 : 256) <= ctx->cus ? 128 : 256;
 }
 
-// Whether a launch holds a product's tiles: columns of the thin ones are a grid's second coordinate.  (The number of the large ones has 31 bits for every valid
-// configuration: at most 65279 tiles of 256 rows by 2^14.)
-static int tiles_fit(int rows, int R, bool expert, const char* who) {
-  const bool fit = rows != THIN || cdiv(R, expert ? 128 : 64) <= 65535;
+// Whether a launch holds a product's tiles: columns of the thin ones are a grid's second coordinate; the large ones are workgroups of 256 threads in one dimension,
+// which ends at 2^32 threads.  (No such product fits the memory: 2^24 tiles are 0.5 TB of weights or a result of 1 TB.)
+static int tiles_fit(const symi_ctx* ctx, int rows, int R, bool expert, const char* who) {
+  const symi_cfg* const c = &ctx->cfg;
+  const long long tiles = ((long long)c->T * c->k / rows + c->S_tot) * cdiv(R, expert || c->dtype == SYMI_F32 ? 128 : 256);
+  const bool fit = rows == THIN ? cdiv(R, expert ? 128 : 64) <= 65535 : tiles < (1 << 24) - 8;
   if (fit) return SYMI_OK;
   set_error("%s: more tiles than a launch can have", who);
   return SYMI_EUNSUPPORTED;
@@ -530,7 +532,7 @@ extern "C" int symi_product8(const symi_ctx* ctx, const void* Aq, const void* As
   hipStream_t st = as_stream(stream);
   int32_t* const map = reinterpret_cast<int32_t*>(align_up((size_t)ws, 256) + ws8_layout(cfg).map);
   const int tile = tile_rows(ctx, R, false);
-  if (int rc = tiles_fit(tile, R, false, "symi_product8")) return rc;
+  if (int rc = tiles_fit(ctx, tile, R, false, "symi_product8")) return rc;
   launch_tiles(ctx, tile, slot_offsets, map, st);
   const Product8 p = {(const uint8_t*)Aq, (const uint8_t*)As, (const uint8_t*)Wq, (const uint8_t*)Ws, slot_offsets, map, Y,
                       nullptr, nullptr, nullptr, nullptr, R, n, pitch8(n), scale_pitch8(n), 0, 0, cfg->S_tot};
@@ -557,8 +559,8 @@ extern "C" int symi_expert_fwd8(const symi_ctx* ctx, const void* Xp, const int32
   const int d = cfg->d, f = cfg->f, A = cfg->T * cfg->k;
   int32_t* const map = reinterpret_cast<int32_t*>(base + L.map);
   const int tile = std::max(tile_rows(ctx, f, true), tile_rows(ctx, d, false));
-  if (int rc = tiles_fit(tile, f, true, "symi_expert_fwd8")) return rc;
-  if (int rc = tiles_fit(tile, d, false, "symi_expert_fwd8")) return rc;
+  if (int rc = tiles_fit(ctx, tile, f, true, "symi_expert_fwd8")) return rc;
+  if (int rc = tiles_fit(ctx, tile, d, false, "symi_expert_fwd8")) return rc;
   launch_tiles(ctx, tile, slot_offsets, map, st);
   launch_quant_rows(ctx, true, Xp, base + L.xq, base + L.xs, A, d, slot_offsets + cfg->S_tot, st);
   Product8 p = {base + L.xq, base + L.xs, (const uint8_t*)W1q, (const uint8_t*)W1s, slot_offsets, map, nullptr, (uint16_t*)UV, (uint16_t*)H,

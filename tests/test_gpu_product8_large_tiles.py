@@ -113,3 +113,15 @@ def test_blocks_of_zeros_beside_others(counts, R, dtype):
     want, _ = O.product(a[0], w, at)
     want = torch.from_numpy(want).float().to(ctx.torch_dtype)
     assert (Hn.npf(Y) == Hn.npf(want)).all() and np.abs(Hn.npf(want)).max() > 0
+
+
+def test_more_tiles_than_a_launch_has_threads_for_are_refused():
+    """2^24 workgroups of 256 threads.  Refused before anything is read."""
+    L, some = symi.lib(), 256
+    for dtype, T in (("bf16", 8000000), ("f32", 4000000)):
+        ctx = context(T, 1, dtype)
+        assert L.symi_product8(ctx.ptr, some, some, some, some, some, 1 << 22, 1024, some, some, None) == -2
+        assert "tiles" in symi.symi_last_error()
+    ctx = context(8000000, 4000, "bf16", d=256, f=1 << 19)
+    assert L.symi_expert_fwd8(ctx.ptr, some, some, some, some, some, some, None, None, some, some, None) == -2
+    assert "tiles" in symi.symi_last_error()
