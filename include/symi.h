@@ -489,7 +489,8 @@ int symi_dequant8(const symi_ctx* ctx, const void* q, const void* s, int groups,
 /* Products of 8-bit values over replica slots: for the rows [slot_offsets[p], slot_offsets[p+1]) of slot p
  *   Y[row, j] = sum over i < n of A[row, i] W[p, j, i]
  *   summed in fp32; in a bf16 context by the 8-bit matrix instruction, which drops of every 8 neighbouring products what is below 2^-13 of
- *   the largest (some 1.5e-5 of a result, a hundredth of its rounding), in an fp32 context at half that rate without such a loss.
+ *   the largest (at most 7 2^-13 of the sum of the products' sizes; some 1.5e-5 of a result, a hundredth of its rounding), in an fp32 context at half that rate
+ *   without such a loss.
  *   Aq, As: [T k, n] with block = 1;  Wq, Ws: [S_tot, R, n] with block = 128;  slot_offsets [S_tot+1] as symi_dispatch's, up to T k;
  *   Y [T k, R] out in the activation dtype; rows outside the slots are not written.  R a multiple of 8, at most 2^22 (with few
  *   rows a slot at most 65535 * 64, with many at most 2^24 - 9 tiles, which no memory holds, else SYMI_EUNSUPPORTED).
@@ -499,7 +500,9 @@ int symi_product8(const symi_ctx* ctx, const void* Aq, const void* As, const int
                   const void* Ws, int R, int n, void* Y, void* ws, void* stream);
 
 /* symi_expert_fwd in 8 bits, for bf16 contexts (fp32: SYMI_EUNSUPPORTED): Xp and the hidden units are rounded to 8 bits (block = 1) on their
- * way into the products, u, v and h are fp32 until they are stored.
+ *   way into the products, whose sums are those of symi_product8; u, v and h are fp32 until they are rounded or stored.  With T k <= 12 S_tot the first product has no
+ *   loss beyond fp32's; with more rows what the instruction drops moves some 4 of 10000 hidden units to a neighbouring code, and Yp is off by
+ *   2.0e-3 (2-norm) of the result that exact sums have, where its rounding to bf16 alone makes that 1.7e-3; with few hidden units (80) 2.3e-3.
  *   W1q, W1s: [S_tot, 2f, d], W2q, W2s: [S_tot, d, f] with block = 128 (symi_quant8 of W1_slots, W2_slots).
  *   UV, H: as symi_expert_fwd's (H: h rounded to bf16), for symi_expert_bwd, which takes the roundings to 8 bits as having gradient 1; NULL,
  *   both, where there is no backward pass.  symi_dequant8 gives the weights that the products saw.
