@@ -424,7 +424,8 @@ int symi_adamw_decode(const symi_ctx* ctx, const symi_adamw* opt, float* m, floa
  *   mean = sum R / d (center = 0: 0),  rstd = 1 / sqrt(sum (R - mean)^2 / d + eps),  Y = (R - mean) rstd w + b.
  *   X, residual, R, Y [T,d] in the activation dtype; w, b [d] f32 or NULL (1 and 0).  R may be X or residual.
  *   mean, rstd [T] f32 out, each NULL if it is not wanted (the backward pass needs them).  eps >= 0; with eps = 0 a row without any
- *   variation is NaN.  Statistics are fp32, the variance a sum of squares of differences.  A row's results do not depend on the batch. */
+ *   variation is NaN.  Statistics are fp32, the variance a sum of squares of differences (where that passes fp32's range, at differences
+ *   of some 1e19, less in wide rows, rstd is 0).  A row's results do not depend on the batch. */
 int symi_norm_fwd(const symi_ctx* ctx, int center, float eps, const void* X, const void* residual, const float* w,
                   const float* b, void* R, void* Y, float* mean, float* rstd, void* stream);
 
@@ -446,7 +447,8 @@ int symi_norm_bwd(const symi_ctx* ctx, int center, const void* dY, const void* R
  *   idx = the k classes with the largest c in them, best first
  *   gate = scale s (renorm: scale s / sum of the k)
  * The bias takes part in the choice only.  c and the groups' sums are compared as binary64 evaluates them, equal ones go to the lower
- * index; without a bias classes are compared by their logits, which is the same order.  A class whose logit is -inf is masked: it is
+ * index; without a bias classes, and groups with group_top = 1, are compared by their logits, which is the same order and tells scores apart that binary64 rounds to the
+ * same value.  A class whose logit is -inf is masked: it is
  * never chosen for its score.  Where fewer than k classes are left, the lowest of the others fill up, with gate 0: idx always
  * holds k different classes, and a row that is masked altogether has gates 0.  A row with a NaN logit, or in a softmax one of +inf, has
  * NaN for all its gates and any k classes; a bias of NaN or -inf masks its class.  Renormalised gates are quotients of scores taken relative to
@@ -490,7 +492,8 @@ int symi_dequant8(const symi_ctx* ctx, const void* q, const void* s, int groups,
  *   Y[row, j] = sum over i < n of A[row, i] W[p, j, i]
  *   summed in fp32; in a bf16 context by the 8-bit matrix instruction, which drops of every 8 neighbouring products what is below 2^-13 of
  *   the largest (at most 7 2^-13 of the sum of the products' sizes; some 1.5e-5 of a result, a hundredth of its rounding), in an fp32 context at half that rate
- *   without such a loss.
+ *   without such a loss.  (fp32, more than 32 rows a slot: a tile of 128 rows by 128 columns in which a power lies outside 2^-100 .. 2^100, that of a block of zeros among
+ *   them, takes about one and a half times as long: leave padding rows out of the slots.)
  *   Aq, As: [T k, n] with block = 1;  Wq, Ws: [S_tot, R, n] with block = 128;  slot_offsets [S_tot+1] as symi_dispatch's, up to T k;
  *   Y [T k, R] out in the activation dtype; rows outside the slots are not written.  R a multiple of 8, at most 2^22 (with few
  *   rows a slot at most 65535 * 64, with many at most 2^24 - 9 tiles, which no memory holds, else SYMI_EUNSUPPORTED).

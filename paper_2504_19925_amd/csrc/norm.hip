@@ -4,9 +4,9 @@
 // with xh = (R - mean) rstd and g = dY w: dX = rstd (g - sum g / d - xh sum(g xh) / d) + dR, dw = sum dY xh, db = sum dY.
 //
 // Bound by bytes: a row is read once, stays in registers from its sums to its results and is written once; w and b are read once a workgroup.
-// 65536 rows of 4096 in bf16 with a residual sum: forward 385 us (5.6 TB/s), gradients 390 us (5.5 TB/s, 9 of them the sums over the workgroups).  What
+// 65536 rows of 4096 in bf16 with a residual sum: forward 385 us (5.6 TB/s), gradients 392 us (5.5 TB/s, 5 of them the sums over the workgroups).  What
 // it takes for that is few rows at a time, next to each other in memory: the forward pass with 16 to 24 KB of loads on their way to a compute unit 385, with
-// twice as many 407; the gradients with 512 workgroups of every 512th row 390, with 1024 of them 407, with 512 of consecutive rows 424.
+// twice as many 407; the gradients with 512 workgroups of every 512th row 392, with 1024 of them 407, with 512 of consecutive rows 424.
 #include <math.h>
 
 #include <algorithm>

@@ -39,7 +39,7 @@ struct Product8 {
   void* Y;              // product: [rows, R]
   uint16_t *UV, *H;     // experts' first product, or nullptr
   uint8_t *Hq, *Hs;
-  int R, n, p8, sp;     // R: rows of a slot's weight (f in the experts' first product: gate and up rows each)
+  int R, p8, sp;        // R: rows of a slot's weight (f in the experts' first product: gate and up rows each)
   int hp8, hsp;         // pitches of Hq, Hs
   int slots;
 };

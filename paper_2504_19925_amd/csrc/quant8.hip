@@ -561,7 +561,7 @@ extern "C" int symi_product8(const symi_ctx* ctx, const void* Aq, const void* As
   if (int rc = tiles_fit(ctx, tile, R, false, "symi_product8")) return rc;
   launch_tiles(ctx, tile, slot_offsets, map, st);
   const Product8 p = {(const uint8_t*)Aq, (const uint8_t*)As, (const uint8_t*)Wq, (const uint8_t*)Ws, slot_offsets, map, Y,
-                      nullptr, nullptr, nullptr, nullptr, R, n, pitch8(n), scale_pitch8(n), 0, 0, cfg->S_tot};
+                      nullptr, nullptr, nullptr, nullptr, R, pitch8(n), scale_pitch8(n), 0, 0, cfg->S_tot};
   launch_product(ctx, p, tile, false, st);
   SYMI_LAUNCH_CHECK("symi_product8");
   return SYMI_OK;
@@ -590,7 +590,7 @@ extern "C" int symi_expert_fwd8(const symi_ctx* ctx, const void* Xp, const int32
   launch_tiles(ctx, tile, slot_offsets, map, st);
   launch_quant_rows(ctx, true, Xp, base + L.xq, base + L.xs, A, d, slot_offsets + cfg->S_tot, st);
   Product8 p = {base + L.xq, base + L.xs, (const uint8_t*)W1q, (const uint8_t*)W1s, slot_offsets, map, nullptr, (uint16_t*)UV, (uint16_t*)H,
-                base + L.hq, base + L.hs, f, d, pitch8(d), scale_pitch8(d), pitch8(f), scale_pitch8(f), cfg->S_tot};
+                base + L.hq, base + L.hs, f, pitch8(d), scale_pitch8(d), pitch8(f), scale_pitch8(f), cfg->S_tot};
   launch_product(ctx, p, tile, true, st);
   p.Aq = base + L.hq;
   p.As = base + L.hs;
@@ -598,7 +598,6 @@ extern "C" int symi_expert_fwd8(const symi_ctx* ctx, const void* Xp, const int32
   p.Ws = (const uint8_t*)W2s;
   p.Y = Yp;
   p.R = d;
-  p.n = f;
   p.p8 = pitch8(f);
   p.sp = scale_pitch8(f);
   launch_product(ctx, p, tile, false, st);

@@ -10,9 +10,9 @@
 // largest, runner-up, ... scan few lanes' registers, with a butterfly of log2 G steps in DPP operands.  Sums of exponentials are taken along a tree over the
 // pieces, the same for every G, so that a token's gates do not depend on its batch.
 //
-// Bound by instructions and their latency: 65536 tokens of 128 classes in 8 groups, sigmoid and bias, 48 us with the launches that clear the counts and move the bias,
-// against 7 of the bytes; taken apart, the rounds take 10, the groups 8, binary64 6, the counts' atomics 4, and 18 are launches, loads and scores.  16 tokens 12.5 us, of
-// which two launches are 8.
+// Bound by instructions and their latency: 65536 tokens of 128 classes in 8 groups, sigmoid and bias, 49 us with the launches that clear the counts and move the bias, against 7
+// of the bytes.  By calls with fewer choices, without groups, without a bias: a round takes 1.7, so the eight 14, the groups 8, the bias with its two rounds more 5, and 20 are launches,
+// loads, scores, gates and counts.  16 tokens 12.2 us, of which the kernel is 10.3, one workgroup's chain: 0.4 a round, the groups 1.4.
 #include <limits.h>
 #include <math.h>
 
