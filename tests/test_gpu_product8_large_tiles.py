@@ -115,6 +115,28 @@ def test_blocks_of_zeros_beside_others(counts, R, dtype):
     assert (Hn.npf(Y) == Hn.npf(want)).all() and np.abs(Hn.npf(want)).max() > 0
 
 
+@pytest.mark.parametrize("counts,d,f", [(COUNTS, 264, 1032), ([300, 2, 64, 200], 264, 136), ([3, 0, 9], 136, 264)], ids=["256", "128", "16"])
+def test_rows_and_weights_of_the_experts_that_are_not_finite(counts, d, f):
+    """A NaN or an infinity reaches the results of its row, or of its weight's slot, and no others."""
+    ctx, (X, offs, w1q, w1s, w2q, w2s), clean = check_experts(counts, d, f)
+    X, w1q, n = X.clone(), w1q.clone(), counts[0]
+    X[0, 3], X[2, d - 1] = float("nan"), -float("inf")
+    w1q.view(torch.uint8)[2, f + 5, 7] = 0x7F        # an up row of the third slot
+    bad = [torch.full_like(t, 640.0) for t in clean]
+    symi.symi_expert_fwd8(ctx, X, offs, w1q, w1s, w2q, w2s, *bad, scratch(ctx))
+    rows = torch.zeros(sum(counts), dtype=torch.bool, device="cuda")
+    rows[0] = rows[2] = True
+    third = slice(int(offs[2]), int(offs[3]))
+    UV, H, Y = bad
+    assert torch.isnan(UV[rows]).all() and torch.isnan(H[rows]).all() and torch.isnan(Y[rows]).all()
+    assert torch.isnan(UV[third, f + 5]).all() and torch.isnan(H[third, 5]).all() and torch.isnan(Y[third]).all()
+    rows[third] = True
+    assert all(torch.equal(t[~rows], c[~rows]) for t, c in zip(bad, clean)) and n > 2
+    others = torch.ones(2 * f, dtype=torch.bool, device="cuda")
+    others[f + 5] = False
+    assert torch.equal(UV[third][:, others], clean[0][third][:, others])
+
+
 def test_more_tiles_than_a_launch_has_threads_for_are_refused():
     """2^24 workgroups of 256 threads.  Refused before anything is read."""
     L, some = symi.lib(), 256
